@@ -47,10 +47,31 @@ enum {
 enum {
   PASTA_FLAG_HOST_ONLY = 1,      /* bookkeeping only: no CUDA call is ever made, compute entry points return BAD_STATE */
   PASTA_FLAG_NO_TENSOR_PATH = 2, /* route every stream through the warp-shuffle kernel (debugging / comparison) */
-  PASTA_FLAG_OUT_BF16 = 4        /* `out` of pasta_decode_attn, pasta_step_device and pasta_step_host is bf16 instead of
+  PASTA_FLAG_OUT_BF16 = 4,       /* `out` of pasta_decode_attn, pasta_step_device and pasta_step_host is bf16 instead of
                                     fp32 (same shape; the sums stay fp32, one rounding at the end; lse stays fp32).
                                     pasta_decode_attn_noalloc writes fp32 only and returns BAD_STATE on such a pool. */
+  PASTA_FLAG_KV_FP8 = 8          /* the pool holds K and V in 8 bits (see "8-bit pools" below): half the bytes per token */
 };
+
+/*
+ * 8-bit pools (no counterpart in the paper; PASTA_FLAG_KV_FP8).  K and V are held as e4m3 codes with one scale for K and
+ * one for V of every (layer, page of 16 tokens, kv head), each a power of two 2^e:
+ *   e = the smallest integer with amax <= 448 * 2^e over the page's elements, kept within [-64, 63] (a page of zeros: -64);
+ *   an element is held as code * 2^e, code = the e4m3 number nearest to x * 2^-e (ties to even, at most 448 in magnitude).
+ * A page fills one or several tokens at a time.  When new tokens need a larger e the codes already in the page are
+ * multiplied by 2^-(growth) and rounded once more, which changes only those that fall below 2^-6 of the new scale, by at
+ * most half a step of it (2^-10 of the new scale); so what a page holds depends, within that, on how its tokens were
+ * grouped into calls.  e does not shrink while a page fills; it starts anew when the page's first slot is written.
+ * With the rotary appends K is rotated in 64 bits, rounded to fp32 and then quantised (no bf16 rounding in between).
+ * An element that is not finite (after rotation) is stored as zero and pasta_pool_status reports
+ * PASTA_ERR_DEVICE_CHECK: everything in an 8-bit pool is finite.
+ * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16);
+ * pasta_kv_read returns the numbers held, which bf16 represents exactly.  pasta_kv_bytes is n_layers * (n_pages *
+ * n_kv_heads * (32 * head_dim + 2) bytes, the scales' part rounded up to 1024).  The attention runs on one kernel for
+ * head_dim 64 and 128 for requests of up to 128 stacked rows (threads x group) and 4095 streams; the sums are fp32 and the
+ * softmax weights are rounded to fp16 for the product with V.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the
+ * warp-shuffle kernel, which rounds no weight.
+ */
 
 /* thread states reported by pasta_pool_dump */
 enum { PASTA_THREAD_ACTIVE = 0, PASTA_THREAD_FINISHED = 1, PASTA_THREAD_MERGED = 2 };
@@ -205,6 +226,16 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *pool, int32_t layer_begin, int32_
                                  const void *q, void *out, float *lse, float scale, void *stream);
 
 /*
+ * (No counterpart in the paper: models that bound their attention scores.)  From the next call on, every attention of
+ * this pool (pasta_decode_attn, pasta_decode_attn_noalloc, pasta_step_device, pasta_step_host and _begin) caps its
+ * scores before masking and softmax:  s = q . k * scale  becomes  cap * tanh(s / cap);  lse is that of the capped scores.
+ * The tanh is good to cap * 2^-21.  cap = 0 (the state after pasta_pool_create) switches it off, otherwise 1e-3 <= cap <=
+ * 1e6 (INVALID_ARG outside, NaN included).  BAD_STATE on a host-only pool.  Launches already enqueued, or captured in a
+ * graph, keep the cap they were made with.
+ */
+pasta_status_t pasta_set_softcap(pasta_pool_t *pool, float cap);
+
+/*
  * Appends m tokens to one thread outside a decode step (prompt prefill, benchmark set-up):
  * reserves slots like m steps of that thread alone would, then copies k, v
  * (device bf16 [layer_count, m, n_kv_heads, head_dim]).  With layer_count == 0 only the
@@ -327,6 +358,11 @@ pasta_status_t pasta_dense_mask_attn(const void *k_pool, const void *v_pool, con
  */
 pasta_status_t pasta_kv_read(pasta_pool_t *pool, int32_t layer, int32_t req, int32_t stream_id,
                              int32_t start, int32_t m, void *k_out, void *v_out, void *stream);
+
+/* pasta_kv_read for layers [layer_begin, layer_begin + layer_count) at once: k_out, v_out [layer_count, m, n_kv_heads,
+ * head_dim]. */
+pasta_status_t pasta_kv_read_layers(pasta_pool_t *pool, int32_t layer_begin, int32_t layer_count, int32_t req,
+                                    int32_t stream_id, int32_t start, int32_t m, void *k_out, void *v_out, void *stream);
 
 /*
  * Serialises the bookkeeping state into host int32 words:

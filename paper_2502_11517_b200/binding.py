@@ -15,7 +15,7 @@ import numpy as np
 from .build import LIB
 
 OK, INVALID_ARG, OUT_OF_PAGES, BAD_STATE, CAPACITY, CUDA, DEVICE_CHECK, TIMEOUT = range(8)
-FLAG_HOST_ONLY, FLAG_NO_TENSOR_PATH, FLAG_OUT_BF16 = 1, 2, 4
+FLAG_HOST_ONLY, FLAG_NO_TENSOR_PATH, FLAG_OUT_BF16, FLAG_KV_FP8 = 1, 2, 4, 8
 _NAMES = ["OK", "INVALID_ARG", "OUT_OF_PAGES", "BAD_STATE", "CAPACITY", "CUDA", "DEVICE_CHECK", "TIMEOUT"]
 
 EXPORTS = [
@@ -30,7 +30,7 @@ EXPORTS = [
     "pasta_last_cuda_error", "pasta_debug_set_wait_limit", "pasta_debug_wait_expiry", "pasta_debug_hold_roles",
     "pasta_debug_stream_read", "pasta_step_host_begin", "pasta_step_host_wait",
     "pasta_dense_mask_scratch_bytes", "pasta_dense_append", "pasta_dense_mask_attn", "pasta_debug_set_tail",
-    "pasta_debug_set_launch_overlap",
+    "pasta_debug_set_launch_overlap", "pasta_set_softcap", "pasta_kv_read_layers",
 ]
 
 
@@ -288,7 +288,22 @@ class Pool:
                "pasta_debug_stream_read")
         return nbytes // 65536 * 65536 if mode else nbytes // 16 * 16
 
+    def set_softcap(self, cap: float) -> None:
+        """Caps the scores of this pool's attention from the next call on: s -> cap * tanh(s / cap); 0 switches it off."""
+        _check(lib().pasta_set_softcap(self._h, C.c_float(cap)), "pasta_set_softcap")
+
     # ---- introspection
+    def kv_read_layers(self, req: int, stream_id: int, start: int, m: int, layer_begin: int = 0,
+                       layer_count: Optional[int] = None, stream=None):
+        """K and V of tokens [start, start + m) of a stream for several layers: bf16 [layer_count, m, Hkv, d] each."""
+        import torch
+        cnt = self.n_layers - layer_begin if layer_count is None else layer_count
+        k = torch.empty((cnt, m, self.n_kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.kv.device)
+        v = torch.empty_like(k)
+        _check(lib().pasta_kv_read_layers(self._h, layer_begin, cnt, req, stream_id, start, m, _dev(k), _dev(v),
+                                          _stream(stream)), "pasta_kv_read_layers")
+        return k, v
+
     def kv_read(self, layer: int, req: int, stream_id: int, start: int, m: int, stream=None):
         import torch
         dev = self.kv.device

@@ -28,7 +28,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 struct Derived {
   int32_t group, max_queries, max_rows, layers_per_launch;
   int64_t max_words, staging_words;
-  size_t kv_bytes, layer_stride;
+  size_t kv_bytes, layer_stride, scale_off;      // scale_off: where a layer's scales begin (8-bit pools)
   size_t off_status, off_plan, off_plan2, off_run, off_ml, off_o, ws_bytes;
 };
 
@@ -59,7 +59,9 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                  2 * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
                  PU_WORDS * tail_units + 2 * nr * c.n_kv_heads + 8;
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
-  d->layer_stride = size_t(c.n_pages) * c.n_kv_heads * kv_block_bytes(c.head_dim);
+  const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0;
+  d->scale_off = size_t(c.n_pages) * c.n_kv_heads * (kv8 ? kv8_block_bytes(c.head_dim) : kv_block_bytes(c.head_dim));
+  d->layer_stride = d->scale_off + (kv8 ? align_up(size_t(c.n_pages) * c.n_kv_heads * 2, 1024) : 0);
   d->kv_bytes = d->layer_stride * c.n_layers;
   size_t off = 0;
   d->off_status = off; off += 256;
@@ -146,6 +148,9 @@ pasta_status_t upload(pasta_pool *p, const int32_t *src, size_t words, int32_t *
   return PASTA_OK;
 }
 
+// elements between the layers of a dense [layers, n, n_kv_heads, head_dim] array
+int64_t tokens_stride(const pasta_pool *p, int64_t n) { return n * p->cfg.n_kv_heads * p->cfg.head_dim; }
+
 PlanLimits limits_of(const pasta_pool *p) {
   PlanLimits l;
   l.n_q_heads = p->cfg.n_q_heads;
@@ -155,8 +160,14 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.max_rows = p->d.max_rows;
   l.max_words = p->d.max_words;
   l.grid = p->sm_count;
-  l.tensor_path = p->cfg.head_dim == 128 && !(p->cfg.flags & PASTA_FLAG_NO_TENSOR_PATH) && tensor_path_available();
+  l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & PASTA_FLAG_KV_FP8)) &&
+                  !(p->cfg.flags & PASTA_FLAG_NO_TENSOR_PATH) && tensor_path_available();
   l.tail_percent = p->tail_percent;
+  if (p->cfg.flags & PASTA_FLAG_KV_FP8) {      // that kernel runs one CTA per unit, three to an SM
+    l.grid = p->sm_count * 3;
+    l.tail_percent = 0;
+    l.even_cuts = true;
+  }
   l.tail_tiles = p->tail_tiles;
   return l;
 }
@@ -261,6 +272,9 @@ pasta_status_t pasta_pool_create(const pasta_pool_config_t *cfg, pasta_pool_t **
     p->pv.rows_per_layer = d.max_rows;
     p->pv.wait_limit = kWaitLimitCycles;
     p->pv.debug_hold = 0;
+    p->pv.softcap_log2 = 0.f;
+    p->pv.kv8 = (cfg->flags & PASTA_FLAG_KV_FP8) ? 1 : 0;
+    p->pv.scale_off = static_cast<int64_t>(d.scale_off);
   }
   *out = p;
   return PASTA_OK;
@@ -330,8 +344,13 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
-  PASTA_CUDA(launch_kv_append_rope(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], 0, n_app,
-                                   layer_begin, layer_count, k_new, v_new, theta, static_cast<cudaStream_t>(stream)));
+  if (p->pv.kv8)
+    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], 0, n_app, false, 0,
+                                 layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, theta,
+                                 static_cast<cudaStream_t>(stream)));
+  else
+    PASTA_CUDA(launch_kv_append_rope(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], 0, n_app,
+                                     layer_begin, layer_count, k_new, v_new, theta, static_cast<cudaStream_t>(stream)));
   p->launches += 1;
   return PASTA_OK;
 }
@@ -430,8 +449,12 @@ pasta_status_t pasta_kv_append(pasta_pool_t *p, int32_t layer_begin, int32_t lay
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
-  PASTA_CUDA(launch_kv_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], n_app, layer_begin, layer_count, k_new, v_new,
-                              static_cast<cudaStream_t>(stream)));
+  if (p->pv.kv8)
+    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, 0, n_app, false, 0, layer_begin, layer_count,
+                                 tokens_stride(p, n_app), k_new, v_new, 0.0, static_cast<cudaStream_t>(stream)));
+  else
+    PASTA_CUDA(launch_kv_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], n_app, layer_begin, layer_count, k_new, v_new,
+                                static_cast<cudaStream_t>(stream)));
   p->launches += 1;
   return PASTA_OK;
 }
@@ -458,7 +481,8 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
     uint8_t mask = 0;
     if (timed) PASTA_CUDA(cudaEventRecord(ev[0], st));
     if (p->hdr.w[PH_N_TUNITS] + p->hdr.w[PH_N_DUNITS] > 0) {
-      PASTA_CUDA(launch_attn_tensor(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
+      if (p->pv.kv8) PASTA_CUDA(launch_attn_kv8(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
+      else PASTA_CUDA(launch_attn_tensor(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
       p->launches += 1;
       mask |= 1;
     }
@@ -506,6 +530,14 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
     for (int32_t i = 0; i < cnt; ++i) { words[2 * i] = slots[begin + i].page; words[2 * i + 1] = slots[begin + i].offset; }
     s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
+    if (p->pv.kv8) {       // all layers in one launch, page by page
+      const size_t at = size_t(begin) * tok;
+      PASTA_CUDA(launch_kv8_append(p->pv, p->run_slots_dev, nullptr, pos0 + begin, cnt, true, words[1], layer_begin, layer_count,
+                                   tokens_stride(p, m), static_cast<const uint16_t *>(k) + at, static_cast<const uint16_t *>(v) + at,
+                                   theta, st));
+      p->launches += 1;
+      continue;
+    }
     for (int32_t l = 0; l < layer_count; ++l) {     // the run's layers are [layer_count, m, …]: one launch per layer and chunk
       const uint16_t *kl = static_cast<const uint16_t *>(k) + (size_t(l) * m + begin) * tok;
       const uint16_t *vl = static_cast<const uint16_t *>(v) + (size_t(l) * m + begin) * tok;
@@ -632,16 +664,17 @@ pasta_status_t pasta_step_host(pasta_pool_t *p, int32_t n, const int32_t *req_id
   return pasta_step_host_wait(p);
 }
 
-pasta_status_t pasta_kv_read(pasta_pool_t *p, int32_t layer, int32_t req, int32_t stream_id, int32_t start, int32_t m,
-                             void *k_out, void *v_out, void *stream) {
+pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_t layer_count, int32_t req, int32_t stream_id,
+                                    int32_t start, int32_t m, void *k_out, void *v_out, void *stream) {
   if (!p) return PASTA_ERR_INVALID_ARG;
   if (p->host_only) return PASTA_ERR_BAD_STATE;
   const Request *r = p->host.request(req);
-  if (!r || layer < 0 || layer >= p->cfg.n_layers || stream_id < 0 || stream_id >= static_cast<int32_t>(r->streams.size()))
+  if (!r || layer_begin < 0 || layer_count < 0 || layer_count > p->cfg.n_layers - layer_begin || stream_id < 0 ||
+      stream_id >= static_cast<int32_t>(r->streams.size()))
     return PASTA_ERR_INVALID_ARG;
   const Stream &sm = r->streams[stream_id];
-  if (start < 0 || m < 0 || start + m > sm.len) return PASTA_ERR_INVALID_ARG;
-  if (m == 0) return PASTA_OK;
+  if (start < 0 || m < 0 || start > sm.len - m) return PASTA_ERR_INVALID_ARG;
+  if (m == 0 || layer_count == 0) return PASTA_OK;
   if (!k_out || !v_out) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;
@@ -656,10 +689,24 @@ pasta_status_t pasta_kv_read(pasta_pool_t *p, int32_t layer, int32_t req, int32_
     }
     pasta_status_t s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
-    PASTA_CUDA(launch_kv_read(p->pv, p->run_slots_dev, cnt, layer, static_cast<uint16_t *>(k_out) + size_t(begin) * tok,
-                              static_cast<uint16_t *>(v_out) + size_t(begin) * tok, st));
-    p->launches += 1;
+    PASTA_CUDA(launch_kv_read_layers(p->pv, p->run_slots_dev, cnt, layer_begin, layer_count, tokens_stride(p, m),
+                                     static_cast<uint16_t *>(k_out) + size_t(begin) * tok,
+                                     static_cast<uint16_t *>(v_out) + size_t(begin) * tok, st));
+    p->launches += p->pv.kv8 ? 1 : layer_count;
   }
+  return PASTA_OK;
+}
+
+pasta_status_t pasta_kv_read(pasta_pool_t *p, int32_t layer, int32_t req, int32_t stream_id, int32_t start, int32_t m,
+                             void *k_out, void *v_out, void *stream) {
+  return pasta_kv_read_layers(p, layer, 1, req, stream_id, start, m, k_out, v_out, stream);
+}
+
+pasta_status_t pasta_set_softcap(pasta_pool_t *p, float cap) {
+  if (!p) return PASTA_ERR_INVALID_ARG;
+  if (p->host_only) return PASTA_ERR_BAD_STATE;
+  if (!(cap == 0.f || (cap >= 1e-3f && cap <= 1e6f))) return PASTA_ERR_INVALID_ARG;
+  p->pv.softcap_log2 = cap * 1.4426950408889634f;
   return PASTA_OK;
 }
 

@@ -263,6 +263,7 @@ struct TensorArgs {
   int32_t off_dunit, n_dunits;      // units no CTA owns in advance (per layer): taken from a counter at run time
   int32_t n_queries, layer_begin, layer_count;
   float scale_log2;
+  float cap_k2;                     // capped scores: 2 log2(e) / C (see softcap)
   void *out;                        // [layer_count, n_queries, Hq, 128], fp32 or bf16: rows of final units go here
   float *lse;                       // [layer_count, n_queries, Hq] or null
   int32_t out_bf16;
@@ -341,7 +342,7 @@ __device__ __forceinline__ bool next_unit(Walk &w, const TensorArgs &a, const in
   return true;
 }
 
-template <bool kShared>
+template <bool kShared, bool kCap>
 __global__ void __launch_bounds__(T_THREADS, 1)
 attn_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) {
   extern __shared__ uint8_t smem_raw[];
@@ -632,6 +633,12 @@ attn_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ 
               tmem_ld_wait32(raw_sc);
               tmem_ld_order32(raw_sc + 32);
             }
+            // capped scores are in log2 units from here on, plain ones still without their scale
+            const float scale = kCap ? 1.f : a.scale_log2;
+            if (kCap) {
+#pragma unroll
+              for (int j = 0; j < T_HALF; ++j) sc[j] = softcap(sc[j] * a.scale_log2, pv.softcap_log2, a.cap_k2);
+            }
             if (!full) {
 #pragma unroll
               for (int j = 0; j < T_HALF; ++j)
@@ -643,7 +650,7 @@ attn_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ 
               mx[0] = fmaxf(mx[0], sc[j]); mx[1] = fmaxf(mx[1], sc[j + 1]);
               mx[2] = fmaxf(mx[2], sc[j + 2]); mx[3] = fmaxf(mx[3], sc[j + 3]);
             }
-            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
             const bool need = mt > m_ref + 8.f;       // also true for the first visible tile (m_ref = -inf)
             const bool rescale = active && need && l > 0.f;
             if (__any_sync(0xffffffffu, rescale)) {
@@ -670,8 +677,8 @@ attn_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ 
 #pragma unroll
             for (int j = 0; j < T_HALF; j += 4) {
               float x0, x1, x2, x3;
-              fma2(x0, x1, sc[j], sc[j + 1], a.scale_log2, -ref);
-              fma2(x2, x3, sc[j + 2], sc[j + 3], a.scale_log2, -ref);
+              fma2(x0, x1, sc[j], sc[j + 1], scale, -ref);
+              fma2(x2, x3, sc[j + 2], sc[j + 3], scale, -ref);
               const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
               const uint32_t w0 = pack_bf16(p0, p1), w1 = pack_bf16(p2, p3);
               // l sums the weights as the MMA will read them (rounded to bf16), so that O / l stays a convex
@@ -822,12 +829,14 @@ bool tensor_path_available() { return true; }
 cudaError_t launch_attn_tensor(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                                const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
   if (pv.head_dim != 128) return cudaErrorInvalidValue;
-  static uint64_t prepared[2] = {0, 0};
-  const bool shared_units = h.w[PH_N_DUNITS] > 0;
+  static uint64_t prepared[4] = {0, 0, 0, 0};
+  const bool shared_units = h.w[PH_N_DUNITS] > 0, cap = pv.softcap_log2 > 0.f;
+  // four builds of the kernel: with and without the shared part of the walk (without it long runs are 0.7 % faster), with
+  // and without the cap on the scores
+  const auto kernel = cap ? (shared_units ? attn_tensor_kernel<true, true> : attn_tensor_kernel<false, true>)
+                          : (shared_units ? attn_tensor_kernel<true, false> : attn_tensor_kernel<false, false>);
   {
-    cudaError_t e = raise_smem_limit(shared_units ? reinterpret_cast<const void *>(attn_tensor_kernel<true>)
-                                                  : reinterpret_cast<const void *>(attn_tensor_kernel<false>),
-                                     T_SMEM_BYTES, &prepared[shared_units]);
+    cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), T_SMEM_BYTES, &prepared[2 * cap + shared_units]);
     if (e != cudaSuccess) return e;
   }
   const int grid = h.w[PH_T_GRID];
@@ -839,10 +848,9 @@ cudaError_t launch_attn_tensor(const PoolView &pv, const PlanHeader &h, int32_t 
   a.off_dunit = h.w[PH_OFF_DUNIT]; a.n_dunits = h.w[PH_N_DUNITS];
   a.n_queries = h.w[PH_N_QUERIES]; a.layer_begin = layer_begin; a.layer_count = layer_count;
   a.scale_log2 = scale_log2;
+  a.cap_k2 = cap ? 2.f * 1.4426950408889634f / pv.softcap_log2 : 0.f;
   a.out = out; a.lse = lse; a.out_bf16 = out_bf16 ? 1 : 0;
-  // two builds of the kernel: the one without the shared part of the walk is a little faster (0.7 % on long runs)
-  return launch_overlapped(shared_units ? attn_tensor_kernel<true> : attn_tensor_kernel<false>, dim3(grid), dim3(T_THREADS),
-                           T_SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
+  return launch_overlapped(kernel, dim3(grid), dim3(T_THREADS), T_SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
 }
 
 }  // namespace pasta

@@ -30,6 +30,29 @@ __device__ __forceinline__ int kv_chunk_offset(int NH, int kv, int r, int c) {
   return (((j * 2 + kv) * NH + half) << 10) + (r8 << 7) + ((c8 ^ r8) << 4);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Layout of one (page, kv head) block of an 8-bit pool (PASTA_FLAG_KV_FP8): e4m3 codes of K and V of 16 tokens,
+// D*32 bytes, one byte per element:
+//
+//   block = [token group j: 2][K, V: 2][8 rows x D bytes]
+//
+// A row holds one token's codes in 16-byte chunks; chunk c of row r (0..7) sits at chunk position c ^ r for D = 128 and at
+// c ^ (r >> 1) for D = 64 (the 128- and 64-byte swizzles), which keeps both ways the attention kernels read a block
+// free of bank conflicts: a lane per token along a row (K), and 16 tokens of one chunk at a time (V, transposed).
+// Behind a layer's blocks lie its scales: two signed bytes per (page, kv head), the exponents ek and ev of the page's
+// K and V; an element is code * 2^e.  Codes are never NaN (the append stores no such code), so bytes of a page beyond a
+// stream's end, whatever they are, vanish against zero weights.
+// ---------------------------------------------------------------------------------------------
+__host__ __device__ constexpr int kv8_block_bytes(int head_dim) { return head_dim * 32; }
+constexpr int kKv8ExpMin = -64, kKv8ExpMax = 63;     // range of a page's scale exponent
+
+// byte offset, inside an 8-bit block, of the 16-byte chunk `c` (16 elements) of token row `r` (0..15)
+template <int D>
+__device__ __forceinline__ int kv8_chunk_offset(int kv, int r, int c) {
+  const int j = r >> 3, r8 = r & 7;
+  return (j * 2 + kv) * (8 * D) + r8 * D + ((c ^ (D == 128 ? r8 : (r8 >> 1))) << 4);
+}
+
 struct PoolView {
   uint8_t *kv_base;
   int64_t layer_stride;      // bytes between layers
@@ -40,6 +63,9 @@ struct PoolView {
   float *part_o;             // partial unnormalised outputs [row][D]
   int64_t rows_per_layer;    // stride of the partial arrays between layers of one launch
   long long wait_limit;      // SM cycles a role waits for another role before it gives up (kWaitLimitCycles by default)
+  float softcap_log2;        // 0, or C = cap * log2(e): a score s (in log2 units) becomes C tanh(s / C)
+  int32_t kv8;               // 1: the pool holds 8-bit codes and scales (kv8_block_bytes, kv8_chunk_offset)
+  int64_t scale_off;         // bytes from a layer's start to its scales (8-bit pools)
   int32_t debug_hold;        // test hook, 0 in normal use: bit r set = role r of the tensor-core kernel never starts
 };
 
@@ -126,5 +152,27 @@ __device__ __forceinline__ float fast_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// Capped score: C tanh(s / C) with tanh(x) = 1 - 2 / (2^(2 x log2 e) + 1), s and C in log2 units, k2 = 2 log2(e) / C.
+// ex2 and rcp are good to a few units of the last place, so the result is off by less than 2^-21 C whatever s is (for
+// |s| much below C that is an absolute, not a relative bound, which is what an exponent needs).  Saturates to +-C.
+__device__ __forceinline__ float softcap(float s, float C, float k2) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fast_exp2(s * k2) + 1.f));
+  return fmaf(-2.f * C, r, C);
+}
+
+// two e4m3 codes (low and high byte of a 16-bit half of `x`) as two fp16: exact
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t x) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(x));
+  return r;
+}
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t x, uint32_t &lo, uint32_t &hi) {
+  lo = e4m3x2_to_f16x2(static_cast<uint16_t>(x));
+  hi = e4m3x2_to_f16x2(static_cast<uint16_t>(x >> 16));
+}
+// 2^e as fp32 for -126 <= e <= 127
+__device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }
 
 }  // namespace pasta

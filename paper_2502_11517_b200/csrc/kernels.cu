@@ -1,5 +1,6 @@
 // K1 (KV append), its inverse (read-back), K3 (warp-shuffle attention pass) and K4 (log-sum-exp merge).
 #include <algorithm>
+#include <cuda_fp16.h>
 #include "device_common.cuh"
 #include "kernels.hpp"
 
@@ -334,9 +335,9 @@ cudaError_t launch_kv_read(const PoolView &pv, const int32_t *slots, int32_t n_t
 constexpr int W_WARPS = 1;            // one warp per block: the block scheduler balances the units
 constexpr int W_STAGES = 2;
 
-template <int D, int G>
+template <int D, int G, bool kKv8>
 struct WarpSmem {
-  static constexpr int BLOCK = D * 64;
+  static constexpr int BLOCK = kKv8 ? kv8_block_bytes(D) : kv_block_bytes(D);
   static constexpr int Q_BYTES = G * D * 4;
   static constexpr int P_BYTES = 16 * G * 4;
   static constexpr int BAR_BYTES = 64;
@@ -344,15 +345,16 @@ struct WarpSmem {
   static constexpr int TOTAL = PER_WARP * W_WARPS;
 };
 
-template <int D, int G>
+// kKv8: the pool's 8-bit blocks; ek joins the score's scale, 2^ev the weights on their way to P.V.  kCap: capped scores.
+template <int D, int G, bool kKv8, bool kCap>
 __global__ void __launch_bounds__(W_WARPS * 32)
 attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wunits, int32_t t_rows,
                  int32_t n_queries, int32_t layer_begin, int32_t layer_count,
                  const __nv_bfloat16 *__restrict__ q, float scale_log2) {
-  using S = WarpSmem<D, G>;
+  using S = WarpSmem<D, G, kKv8>;
   constexpr int NH = D / 64;
   constexpr int E = D / 32;            // output elements per lane
-  constexpr int CH = D / 16;           // 16-byte chunks of a K row handled by one lane
+  constexpr int CH = kKv8 ? D / 32 : D / 16;           // 16-byte chunks of a K row handled by one lane
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   grid_dependency_wait();         // the kernel ahead in the stream (append or tensor-core pass) has completed
   grid_launch_dependents();
@@ -383,6 +385,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
   // stage never waits for global memory
   const int my_pg0 = lane < n_pg ? pg[lane] : 0;
   const int my_pg1 = lane + 32 < n_pg ? pg[lane + 32] : 0;
+  const float cap = pv.softcap_log2, cap_k2 = kCap ? 2.f * 1.4426950408889634f / cap : 0.f;
   __syncwarp();
   auto issue = [&](int i) {
     int page = i < 32 ? __shfl_sync(0xffffffffu, my_pg0, i) : i < 64 ? __shfl_sync(0xffffffffu, my_pg1, i - 32) : pg[i];
@@ -426,6 +429,13 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar0 + 8 * s, (i / W_STAGES) & 1, pv.wait_limit))) { ok = false; consumed = i; break; }
     const uint8_t *sp = stages + s * S::BLOCK;
     const int nv = min(PASTA_PAGE, n_tok - i * PASTA_PAGE);
+    float fk = 1.f, fv = 1.f;
+    if (kKv8) {
+      int page = i < 32 ? __shfl_sync(0xffffffffu, my_pg0, i) : i < 64 ? __shfl_sync(0xffffffffu, my_pg1, i - 32) : pg[i];
+      if (page < 0 || page >= pv.n_pages) page = 0;      // reported when the page was asked for
+      const int8_t *sc8 = reinterpret_cast<const int8_t *>(kv_layer + pv.scale_off) + (static_cast<int64_t>(page) * pv.n_kv_heads + g) * 2;
+      fk = pow2f(sc8[0]); fv = pow2f(sc8[1]);
+    }
 
     float acc[G];
 #pragma unroll
@@ -433,22 +443,41 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
 #pragma unroll
     for (int cc = 0; cc < CH; ++cc) {
       const int c = sub * CH + cc;
-      const uint4 kk = *reinterpret_cast<const uint4 *>(sp + kv_chunk_offset(NH, 0, r, c));
-      const float k0 = bf16_lo(kk.x), k1 = bf16_hi(kk.x), k2 = bf16_lo(kk.y), k3 = bf16_hi(kk.y);
-      const float k4 = bf16_lo(kk.z), k5 = bf16_hi(kk.z), k6 = bf16_lo(kk.w), k7 = bf16_hi(kk.w);
+      if constexpr (kKv8) {
+        const uint4 kk = *reinterpret_cast<const uint4 *>(sp + kv8_chunk_offset<D>(0, r, c));
+        const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w};
 #pragma unroll
-      for (int h = 0; h < G; ++h) {
-        const float4 qa = *reinterpret_cast<const float4 *>(q_s + h * D + c * 8);
-        const float4 qb = *reinterpret_cast<const float4 *>(q_s + h * D + c * 8 + 4);
-        acc[h] = fmaf(k0, qa.x, acc[h]); acc[h] = fmaf(k1, qa.y, acc[h]);
-        acc[h] = fmaf(k2, qa.z, acc[h]); acc[h] = fmaf(k3, qa.w, acc[h]);
-        acc[h] = fmaf(k4, qb.x, acc[h]); acc[h] = fmaf(k5, qb.y, acc[h]);
-        acc[h] = fmaf(k6, qb.z, acc[h]); acc[h] = fmaf(k7, qb.w, acc[h]);
+        for (int w = 0; w < 4; ++w) {
+          uint32_t lo, hi;
+          e4m3x4_to_f16x4(kw[w], lo, hi);
+          const float2 k01 = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), k23 = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+#pragma unroll
+          for (int h = 0; h < G; ++h) {
+            const float4 qa = *reinterpret_cast<const float4 *>(q_s + h * D + c * 16 + w * 4);
+            acc[h] = fmaf(k01.x, qa.x, acc[h]); acc[h] = fmaf(k01.y, qa.y, acc[h]);
+            acc[h] = fmaf(k23.x, qa.z, acc[h]); acc[h] = fmaf(k23.y, qa.w, acc[h]);
+          }
+        }
+      } else {
+        const uint4 kk = *reinterpret_cast<const uint4 *>(sp + kv_chunk_offset(NH, 0, r, c));
+        const float k0 = bf16_lo(kk.x), k1 = bf16_hi(kk.x), k2 = bf16_lo(kk.y), k3 = bf16_hi(kk.y);
+        const float k4 = bf16_lo(kk.z), k5 = bf16_hi(kk.z), k6 = bf16_lo(kk.w), k7 = bf16_hi(kk.w);
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+          const float4 qa = *reinterpret_cast<const float4 *>(q_s + h * D + c * 8);
+          const float4 qb = *reinterpret_cast<const float4 *>(q_s + h * D + c * 8 + 4);
+          acc[h] = fmaf(k0, qa.x, acc[h]); acc[h] = fmaf(k1, qa.y, acc[h]);
+          acc[h] = fmaf(k2, qa.z, acc[h]); acc[h] = fmaf(k3, qa.w, acc[h]);
+          acc[h] = fmaf(k4, qb.x, acc[h]); acc[h] = fmaf(k5, qb.y, acc[h]);
+          acc[h] = fmaf(k6, qb.z, acc[h]); acc[h] = fmaf(k7, qb.w, acc[h]);
+        }
       }
     }
 #pragma unroll
     for (int h = 0; h < G; ++h) {
       float sc = acc[h] + __shfl_xor_sync(0xffffffffu, acc[h], 16);
+      if (kKv8) sc *= fk;
+      if (kCap) sc = softcap(sc, cap, cap_k2);
       if (r >= nv) sc = -INFINITY;
       float mx = sc;
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
@@ -462,21 +491,32 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
       m[h] = m_new;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[h][e] *= corr;
-      if (sub == 0) p_s[r * G + h] = pj;
+      if (sub == 0) p_s[r * G + h] = kKv8 ? pj * fv : pj;
     }
     __syncwarp();
     {
-      const int c = (lane * E) >> 3;                // chunk that holds this lane's elements
-      const int within = ((lane * E) & 7) * 2;      // byte offset inside the chunk
+      constexpr int EC = kKv8 ? 16 : 8;             // elements of a 16-byte chunk
+      const int c = (lane * E) / EC;                // chunk that holds this lane's elements
+      const int within = ((lane * E) % EC) * (16 / EC);      // byte offset inside the chunk
       for (int r2 = 0; r2 < nv; ++r2) {
-        const uint8_t *vp = sp + kv_chunk_offset(NH, 1, r2, c) + within;
         float v[E];
-        if constexpr (E == 4) {
-          const uint2 vv = *reinterpret_cast<const uint2 *>(vp);
-          v[0] = bf16_lo(vv.x); v[1] = bf16_hi(vv.x); v[2] = bf16_lo(vv.y); v[3] = bf16_hi(vv.y);
+        if constexpr (kKv8) {
+          const uint8_t *vp = sp + kv8_chunk_offset<D>(1, r2, c) + within;
+          uint32_t lo, hi = 0;
+          if constexpr (E == 4) e4m3x4_to_f16x4(*reinterpret_cast<const uint32_t *>(vp), lo, hi);
+          else lo = e4m3x2_to_f16x2(*reinterpret_cast<const uint16_t *>(vp));
+          const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+          v[0] = a.x; v[1] = a.y;
+          if constexpr (E == 4) { v[2] = b.x; v[3] = b.y; }
         } else {
-          const uint32_t vv = *reinterpret_cast<const uint32_t *>(vp);
-          v[0] = bf16_lo(vv); v[1] = bf16_hi(vv);
+          const uint8_t *vp = sp + kv_chunk_offset(NH, 1, r2, c) + within;
+          if constexpr (E == 4) {
+            const uint2 vv = *reinterpret_cast<const uint2 *>(vp);
+            v[0] = bf16_lo(vv.x); v[1] = bf16_hi(vv.x); v[2] = bf16_lo(vv.y); v[3] = bf16_hi(vv.y);
+          } else {
+            const uint32_t vv = *reinterpret_cast<const uint32_t *>(vp);
+            v[0] = bf16_lo(vv); v[1] = bf16_hi(vv);
+          }
         }
 #pragma unroll
         for (int h = 0; h < G; ++h) {
@@ -513,32 +553,42 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
   }
 }
 
-template <int D, int G>
+template <int D, int G, bool kKv8, bool kCap>
 static cudaError_t launch_warp_t(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                                  const void *q, float scale_log2, cudaStream_t st) {
-  using S = WarpSmem<D, G>;
+  using S = WarpSmem<D, G, kKv8>;
   static uint64_t prepared = 0;
   {
-    cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_warp_kernel<D, G>), S::TOTAL, &prepared);
+    cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_warp_kernel<D, G, kKv8, kCap>), S::TOTAL, &prepared);
     if (e != cudaSuccess) return e;
   }
   const int64_t warps = static_cast<int64_t>(h.w[PH_N_WUNITS]) * layer_count;
   if (warps == 0) return cudaSuccess;
   const int64_t blocks = (warps + W_WARPS - 1) / W_WARPS;
-  return launch_overlapped(attn_warp_kernel<D, G>, dim3(static_cast<unsigned>(blocks)), dim3(W_WARPS * 32), S::TOTAL, st, pv,
+  return launch_overlapped(attn_warp_kernel<D, G, kKv8, kCap>, dim3(static_cast<unsigned>(blocks)), dim3(W_WARPS * 32), S::TOTAL, st, pv,
                            h.w[PH_OFF_WUNIT], h.w[PH_OFF_PAGES], h.w[PH_N_WUNITS], h.w[PH_T_ROWS], h.w[PH_N_QUERIES],
                            layer_begin, layer_count, static_cast<const __nv_bfloat16 *>(q), scale_log2);
 }
 
-cudaError_t launch_attn_warp(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
-                             const void *q, float scale_log2, cudaStream_t st) {
+template <bool kKv8, bool kCap>
+static cudaError_t launch_warp_k(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                                 const void *q, float scale_log2, cudaStream_t st) {
   const int G = pv.n_q_heads / pv.n_kv_heads;
 #define PASTA_W(DD, GG) \
-  if (pv.head_dim == DD && G == GG) return launch_warp_t<DD, GG>(pv, h, layer_begin, layer_count, q, scale_log2, st);
+  if (pv.head_dim == DD && G == GG) return launch_warp_t<DD, GG, kKv8, kCap>(pv, h, layer_begin, layer_count, q, scale_log2, st);
   PASTA_W(128, 1) PASTA_W(128, 2) PASTA_W(128, 4) PASTA_W(128, 8)
   PASTA_W(64, 1) PASTA_W(64, 2) PASTA_W(64, 4) PASTA_W(64, 8)
 #undef PASTA_W
   return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_attn_warp(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                             const void *q, float scale_log2, cudaStream_t st) {
+  const bool cap = pv.softcap_log2 > 0.f;
+  if (pv.kv8) return cap ? launch_warp_k<true, true>(pv, h, layer_begin, layer_count, q, scale_log2, st)
+                         : launch_warp_k<true, false>(pv, h, layer_begin, layer_count, q, scale_log2, st);
+  return cap ? launch_warp_k<false, true>(pv, h, layer_begin, layer_count, q, scale_log2, st)
+             : launch_warp_k<false, false>(pv, h, layer_begin, layer_count, q, scale_log2, st);
 }
 
 // =============================================================================================

@@ -10,6 +10,9 @@ namespace pasta {
 // one response with 10-tile runs: a CTA that walks a run alone needs 2.9 us per tile more, the merge kernel that cutting
 // brings with it 10.7 us, so cutting pays from the fourth tile on.
 constexpr int32_t kWholeRunSlackTiles = 3;
+// Even cuts (8-bit pools): pieces of at least this many tiles, and about this many pieces per resident CTA.
+constexpr int32_t kEvenMinTiles = 4;
+constexpr int32_t kEvenPerSlot = 2;
 
 
 namespace {
@@ -250,6 +253,20 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       }
       whole_runs = n_runs > 0 && n_runs <= grid && longest <= kept_tiles / grid + kWholeRunSlackTiles;
     }
+    // One CTA per unit (no persistent ranges): a run is cut into equal pieces of at most `piece` tiles, long enough to
+    // be worth a CTA's start and short enough for a few CTAs per slot, so that the block scheduler evens them out.
+    int32_t piece = 0;
+    if (lim.even_cuts) {
+      piece = static_cast<int32_t>(std::max<int64_t>(kEvenMinTiles, (all_tiles + int64_t(kEvenPerSlot) * grid - 1) / (int64_t(kEvenPerSlot) * grid)));
+      for (;; piece *= 2) {                 // the pieces' partial rows have to fit
+        int64_t rows_all = 0;
+        for (const TReq &t : treqs) {
+          const int64_t nt = (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
+          rows_all += (nt + piece - 1) / piece * t.n_threads * G * lim.n_kv_heads;
+        }
+        if (rows_all <= (wpieces.empty() ? lim.max_rows : lim.max_rows / 2) || piece >= (1 << 24)) break;
+      }
+    }
     int32_t run_no = 0;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t all = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
@@ -261,6 +278,17 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         int32_t begin = 0;
         while (begin < n_tiles) {
           const int32_t remaining = n_tiles - begin;
+          if (lim.even_cuts && !whole_runs) {
+            const int32_t n_pieces = (n_tiles + piece - 1) / piece;
+            for (int32_t k = 0; k < n_pieces; ++k) {
+              const int32_t b0 = static_cast<int32_t>(int64_t(n_tiles) * k / n_pieces);
+              const int32_t b1 = static_cast<int32_t>(int64_t(n_tiles) * (k + 1) / n_pieces);
+              tunits.push_back(TUnit{static_cast<int32_t>(ti), g, b0, b1, t_rows});
+              unit_cta.push_back(run_no++);
+              t_rows += rows;
+            }
+            break;
+          }
           if (whole_runs) {                      // one run, one unit, one CTA
             tunits.push_back(TUnit{static_cast<int32_t>(ti), g, 0, n_tiles, t_rows});
             unit_cta.push_back(run_no++);
@@ -397,6 +425,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   w[PH_MAGIC] = PASTA_PLAN_MAGIC;
   w[PH_N_DUNITS] = static_cast<int32_t>(dunits.size());
   w[PH_N_PARTIAL] = n_partial;
+  for (const TReq &t : treqs) w[PH_T_MAX_ROWS] = std::max(w[PH_T_MAX_ROWS], t.n_threads * G);
   w[PH_N_QUERIES] = n;
   w[PH_N_APPEND] = n_app;
   w[PH_N_TREQ] = static_cast<int32_t>(treqs.size());

@@ -16,6 +16,7 @@ struct PlanLimits {
   bool tensor_path;      // false: every stream goes to the warp-shuffle kernel
   int32_t tail_percent;  // share of every long run's tiles that is handed out at run time (0: everything is assigned)
   int32_t tail_tiles;    // tiles per unit of that share
+  bool even_cuts = false;   // t-units are launched one per CTA (8-bit pools): runs are cut into pieces of one length
 };
 
 // Plans the attention of one step: one query per element of `queries`, `slots` parallel to it.
