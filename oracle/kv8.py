@@ -75,8 +75,9 @@ def rotate(k: np.ndarray, positions, theta: float) -> np.ndarray:
     return np.concatenate([lo * c - hi * s, hi * c + lo * s], axis=-1).astype(np.float32)
 
 
-def decode_attention_capped(model, store, queries, q, scale=None, cap=0.0):
-    """`attention.decode_attention` with scores capped by cap * tanh(s / cap) (cap = 0: as they are)."""
+def decode_attention_capped(model, store, queries, q, scale=None, cap=0.0, spread=None):
+    """`attention.decode_attention` with scores capped by cap * tanh(s / cap) (cap = 0: as they are).  A list given as
+    `spread` receives, per query, (visible tokens) x (largest softmax weight of any head)."""
     q = _to_f32(q).astype(np.float64)
     out = np.zeros(q.shape)
     lse = np.zeros(q.shape[:2])
@@ -84,6 +85,7 @@ def decode_attention_capped(model, store, queries, q, scale=None, cap=0.0):
     scale = 1.0 / np.sqrt(q.shape[2]) if scale is None else scale
     for i, query in enumerate(queries):
         k, v = store.gather(model.visible_slots(*query))
+        top = 0.0
         for h in range(q.shape[1]):
             s = (k[:, h // group] @ q[i, h]) * scale
             if cap:
@@ -92,4 +94,7 @@ def decode_attention_capped(model, store, queries, q, scale=None, cap=0.0):
             w = np.exp(s - m)
             out[i, h] = w @ v[:, h // group] / w.sum()
             lse[i, h] = m + np.log(w.sum())
+            top = max(top, 1.0 / w.sum())
+        if spread is not None:
+            spread.append(top * len(k))
     return out, lse

@@ -163,8 +163,8 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & PASTA_FLAG_KV_FP8)) &&
                   !(p->cfg.flags & PASTA_FLAG_NO_TENSOR_PATH) && tensor_path_available();
   l.tail_percent = p->tail_percent;
-  if (p->cfg.flags & PASTA_FLAG_KV_FP8) {      // that kernel runs one CTA per unit, three to an SM
-    l.grid = p->sm_count * 3;
+  if ((p->cfg.flags & PASTA_FLAG_KV_FP8) && p->cfg.head_dim == 64) {      // that kernel runs one CTA per unit, six to an SM
+    l.grid = p->sm_count * 6;
     l.tail_percent = 0;
     l.even_cuts = true;
   }
@@ -481,7 +481,7 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
     uint8_t mask = 0;
     if (timed) PASTA_CUDA(cudaEventRecord(ev[0], st));
     if (p->hdr.w[PH_N_TUNITS] + p->hdr.w[PH_N_DUNITS] > 0) {
-      if (p->pv.kv8) PASTA_CUDA(launch_attn_kv8(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
+      if (kv8_block_kernel(p->pv)) PASTA_CUDA(launch_attn_kv8(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
       else PASTA_CUDA(launch_attn_tensor(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
       p->launches += 1;
       mask |= 1;

@@ -69,6 +69,9 @@ struct PoolView {
   int32_t debug_hold;        // test hook, 0 in normal use: bit r set = role r of the tensor-core kernel never starts
 };
 
+// Which kernel serves the t-units of an 8-bit pool: attn_kv8 for head_dim 64, the tcgen05 kernel for 128.
+inline bool kv8_block_kernel(const PoolView &pv) { return pv.kv8 && pv.head_dim == 64; }
+
 __device__ __forceinline__ void report(int32_t *status, int32_t code) { atomicMax(status, code); }
 // The status word is the first of 64 words the library keeps for itself.  Word 8 counts the shared units the CTAs of
 // the tensor-core kernel have taken in the current launch (the merge that follows puts it back to zero); words 16-17
@@ -171,6 +174,13 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t x) {
 __device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t x, uint32_t &lo, uint32_t &hi) {
   lo = e4m3x2_to_f16x2(static_cast<uint16_t>(x));
   hi = e4m3x2_to_f16x2(static_cast<uint16_t>(x >> 16));
+}
+// nearest e4m3 codes of four numbers (ties to even, magnitudes above 448 held there), a in the lowest byte
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 // 2^e as fp32 for -126 <= e <= 127
 __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }

@@ -26,13 +26,6 @@ constexpr int A_THREADS = 256, A_WARPS = A_THREADS / 32;
 
 struct Freqs { double f[64]; };          // theta^(-2i/D)
 
-__device__ __forceinline__ uint32_t quantise4(float a, float b, float c, float d) {
-  uint16_t lo, hi;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
-}
-
 // exponent of the scale for a largest magnitude given by its fp32 bits (finite)
 __device__ __forceinline__ int scale_exp(uint32_t amax_bits) {
   const int e = static_cast<int>(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);   // 448 = 1.75 * 2^8
@@ -54,7 +47,7 @@ __device__ __forceinline__ int grow_scale(uint8_t *block, int8_t *scale, int kv,
         uint32_t lo, hi;
         e4m3x4_to_f16x4(*at, lo, hi);
         const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
-        *at = quantise4(a.x * f, a.y * f, b.x * f, b.y * f);
+        *at = e4m3x4(a.x * f, a.y * f, b.x * f, b.y * f);
       }
     } else {
       e = old;
@@ -158,8 +151,8 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
               const float *z = y[it] + 8 * half;
               const int c8 = c + half * LPT;            // 8-element chunk of the row
               *reinterpret_cast<uint2 *>(block + kv8_chunk_offset<D>(0, off0 + r, c8 >> 1) + (c8 & 1) * 8) =
-                  make_uint2(quantise4(z[0] * inv, z[1] * inv, z[2] * inv, z[3] * inv),
-                             quantise4(z[4] * inv, z[5] * inv, z[6] * inv, z[7] * inv));
+                  make_uint2(e4m3x4(z[0] * inv, z[1] * inv, z[2] * inv, z[3] * inv),
+                             e4m3x4(z[4] * inv, z[5] * inv, z[6] * inv, z[7] * inv));
             }
           }
         }
@@ -197,8 +190,8 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
           const int r = it * TPI + lane / LPT;
           if (r < cnt)
             *reinterpret_cast<uint2 *>(block + kv8_chunk_offset<D>(kv, off0 + r, c >> 1) + (c & 1) * 8) =
-                make_uint2(quantise4(bf16_lo(x[it][0]) * inv, bf16_hi(x[it][0]) * inv, bf16_lo(x[it][1]) * inv, bf16_hi(x[it][1]) * inv),
-                           quantise4(bf16_lo(x[it][2]) * inv, bf16_hi(x[it][2]) * inv, bf16_lo(x[it][3]) * inv, bf16_hi(x[it][3]) * inv));
+                make_uint2(e4m3x4(bf16_lo(x[it][0]) * inv, bf16_hi(x[it][0]) * inv, bf16_lo(x[it][1]) * inv, bf16_hi(x[it][1]) * inv),
+                           e4m3x4(bf16_lo(x[it][2]) * inv, bf16_hi(x[it][2]) * inv, bf16_lo(x[it][3]) * inv, bf16_hi(x[it][3]) * inv));
         }
       }
       if (bad) report(pv.status, PASTA_ERR_DEVICE_CHECK);

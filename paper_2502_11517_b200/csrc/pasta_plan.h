@@ -68,6 +68,7 @@ enum {
   PH_OFF_DRANGE,      // per (t-request, kv head): first d-unit, one past the last
   PH_N_PARTIAL,       // units that leave partial rows for the merge: t-units and d-units that are not final, and all w-units
   PH_T_MAX_ROWS,      // most stacked rows (threads * group) of any t-request
+  PH_WHOLE_RUNS,      // 1: a small step, every run is one unit
   PH_WORDS = 32
 };
 

@@ -12,7 +12,8 @@ namespace pasta {
 constexpr int32_t kWholeRunSlackTiles = 3;
 // Even cuts (8-bit pools): pieces of at least this many tiles, and about this many pieces per resident CTA.
 constexpr int32_t kEvenMinTiles = 4;
-constexpr int32_t kEvenPerSlot = 2;
+constexpr int32_t kEvenPerSlot = 1;
+constexpr int32_t kEvenWholeSlackTiles = 12;
 
 
 namespace {
@@ -200,6 +201,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   trange.assign(treqs.size() * lim.n_kv_heads * 2, 0);
   drange.assign(treqs.size() * lim.n_kv_heads * 2, 0);
   int32_t t_rows = 0;
+  bool whole_runs = false;
   if (!treqs.empty()) {
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
     // run time (equal tile counts do not finish at the same time: SMs differ in the bandwidth they get).  Only when
@@ -240,7 +242,6 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     // have a CTA of its own and the longest run is hardly longer than an even share: a cut run leaves partial rows and
     // needs the merge kernel behind the attention kernel, whole runs are final units whose rows leave the attention
     // kernel as the output.
-    bool whole_runs = false;
     {
       int64_t n_runs = 0, kept_tiles = 0;
       int32_t longest = 0;
@@ -251,7 +252,10 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
           if (kept > 0) { ++n_runs; kept_tiles += kept; longest = std::max(longest, kept); }
         }
       }
-      whole_runs = n_runs > 0 && n_runs <= grid && longest <= kept_tiles / grid + kWholeRunSlackTiles;
+      // (8-bit pools: whole runs go to CTAs of six warps, a third as many to an SM)
+      const int32_t ctas = lim.even_cuts ? std::max(1, grid / 3) : grid;
+      whole_runs = n_runs > 0 && n_runs <= ctas &&
+                   longest <= kept_tiles / ctas + (lim.even_cuts ? kEvenWholeSlackTiles : kWholeRunSlackTiles);
     }
     // One CTA per unit (no persistent ranges): a run is cut into equal pieces of at most `piece` tiles, long enough to
     // be worth a CTA's start and short enough for a few CTAs per slot, so that the block scheduler evens them out.
@@ -425,6 +429,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   w[PH_MAGIC] = PASTA_PLAN_MAGIC;
   w[PH_N_DUNITS] = static_cast<int32_t>(dunits.size());
   w[PH_N_PARTIAL] = n_partial;
+  w[PH_WHOLE_RUNS] = whole_runs ? 1 : 0;
   for (const TReq &t : treqs) w[PH_T_MAX_ROWS] = std::max(w[PH_T_MAX_ROWS], t.n_threads * G);
   w[PH_N_QUERIES] = n;
   w[PH_N_APPEND] = n_app;

@@ -69,10 +69,11 @@ def test_caps_and_gains(lib, hq, hkv, d, flags, cap, gain):
     plain = out.clone()
     pool.set_softcap(cap)
     pool.decode_attn(q.cuda(), out, lse)
-    want, want_lse = decode_attention_capped(model, store, entries, q[0], cap=cap)
+    spread = []
+    want, want_lse = decode_attention_capped(model, store, entries, q[0], cap=cap, spread=spread)
     qf = q[0].float().numpy()
     if flags & lib.FLAG_KV_FP8:
-        compare(out[0], lse[0], want, want_lse, qf, store, cap=cap)
+        compare(out[0], lse[0], want, want_lse, qf, store, spread, cap=cap)
     else:
         ds = score_bound(qf, store.k, 1 / np.sqrt(d), cap)
         got = out[0].double().cpu().numpy()
