@@ -481,8 +481,7 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
     uint8_t mask = 0;
     if (timed) PASTA_CUDA(cudaEventRecord(ev[0], st));
     if (p->hdr.w[PH_N_TUNITS] + p->hdr.w[PH_N_DUNITS] > 0) {
-      if (kv8_block_kernel(p->pv)) PASTA_CUDA(launch_attn_kv8(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
-      else PASTA_CUDA(launch_attn_tensor(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
+      PASTA_CUDA(launch_attn_units(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
       p->launches += 1;
       mask |= 1;
     }

@@ -69,9 +69,6 @@ struct PoolView {
   int32_t debug_hold;        // test hook, 0 in normal use: bit r set = role r of the tensor-core kernel never starts
 };
 
-// Which kernel serves the t-units of an 8-bit pool: attn_kv8 for head_dim 64, the tcgen05 kernel for 128.
-inline bool kv8_block_kernel(const PoolView &pv) { return pv.kv8 && pv.head_dim == 64; }
-
 __device__ __forceinline__ void report(int32_t *status, int32_t code) { atomicMax(status, code); }
 // The status word is the first of 64 words the library keeps for itself.  Word 8 counts the shared units the CTAs of
 // the tensor-core kernel have taken in the current launch (the merge that follows puts it back to zero); words 16-17
@@ -113,6 +110,18 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// the same look at a phase without waiting at all (try_wait may suspend the thread for a while)
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
       : "r"(bar), "r"(parity)

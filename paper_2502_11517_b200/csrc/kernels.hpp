@@ -64,9 +64,15 @@ cudaError_t launch_attn_warp(const PoolView &pv, const PlanHeader &h, int32_t la
 // units the plan marks final go straight to out / lse (the layout launch_merge writes), all others to the partial rows.
 cudaError_t launch_attn_tensor(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                                const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
-// K2 of an 8-bit pool: every unit of the plan's t-requests, one CTA each (head_dim 64 or 128)
+// K2 of an 8-bit pool, head_dim 128: tensor-core kernel, persistent CTAs like launch_attn_tensor's
+cudaError_t launch_attn_kv8_tensor(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                                   const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
+// K2 of an 8-bit pool, head_dim 64: every unit of the plan's t-requests, one CTA each
 cudaError_t launch_attn_kv8(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                             const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
+// the kernel that serves this pool's t-units and d-units
+cudaError_t launch_attn_units(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count, const void *q,
+                              float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
 // K1 of an 8-bit pool: quantises the new tokens' K and V page by page.  slots: device, 2 words per token.  theta = 0:
 // no rotation; else K is rotated by pos (device array, or NULL for consecutive ids from pos0).  consecutive: the tokens
 // are one run of one stream whose first slot has offset first_offset.  k_new, v_new: [layer_count, n_tok, Hkv, D], layers

@@ -66,8 +66,7 @@ extern "C" pasta_status_t pasta_decode_attn_noalloc(pasta_pool_t *pool, int32_t 
   cudaError_t e = cudaSuccess;
   int launched = 0;
   if (hdr.w[PH_N_TUNITS] + hdr.w[PH_N_DUNITS] > 0) {
-    e = kv8_block_kernel(pv) ? launch_attn_kv8(pv, hdr, layer, 1, q, sc, out, lse, false, st)
-               : launch_attn_tensor(pv, hdr, layer, 1, q, sc, out, lse, false, st);
+    e = launch_attn_units(pv, hdr, layer, 1, q, sc, out, lse, false, st);
     ++launched;
   }
   if (e == cudaSuccess && hdr.w[PH_N_WUNITS] > 0) { e = launch_attn_warp(pv, hdr, layer, 1, q, sc, st); ++launched; }
