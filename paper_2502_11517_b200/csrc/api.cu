@@ -345,7 +345,7 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
   if (p->pv.kv8)
-    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], 0, n_app, false, 0,
+    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], n_app,
                                  layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, theta,
                                  static_cast<cudaStream_t>(stream)));
   else
@@ -450,7 +450,7 @@ pasta_status_t pasta_kv_append(pasta_pool_t *p, int32_t layer_begin, int32_t lay
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
   if (p->pv.kv8)
-    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, 0, n_app, false, 0, layer_begin, layer_count,
+    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, n_app, layer_begin, layer_count,
                                  tokens_stride(p, n_app), k_new, v_new, 0.0, static_cast<cudaStream_t>(stream)));
   else
     PASTA_CUDA(launch_kv_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], n_app, layer_begin, layer_count, k_new, v_new,
@@ -523,20 +523,18 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;      // elements per token
   std::vector<int32_t> words;
+  if (p->pv.kv8) {         // all layers in one launch, page by page
+    for (int32_t i = 0; i < m; i += PASTA_PAGE - slots[i].offset) words.push_back(slots[i].page);
+    PASTA_CUDA(launch_kv8_append_run(p->pv, words.data(), slots[0].offset, pos0, m, layer_begin, layer_count, tokens_stride(p, m), k, v,
+                                     theta, st, &p->launches));
+    return PASTA_OK;
+  }
   for (int32_t begin = 0; begin < m; begin += kRunChunk) {
     const int32_t cnt = std::min(kRunChunk, m - begin);
     words.resize(size_t(cnt) * 2);
     for (int32_t i = 0; i < cnt; ++i) { words[2 * i] = slots[begin + i].page; words[2 * i + 1] = slots[begin + i].offset; }
     s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
-    if (p->pv.kv8) {       // all layers in one launch, page by page
-      const size_t at = size_t(begin) * tok;
-      PASTA_CUDA(launch_kv8_append(p->pv, p->run_slots_dev, nullptr, pos0 + begin, cnt, true, words[1], layer_begin, layer_count,
-                                   tokens_stride(p, m), static_cast<const uint16_t *>(k) + at, static_cast<const uint16_t *>(v) + at,
-                                   theta, st));
-      p->launches += 1;
-      continue;
-    }
     for (int32_t l = 0; l < layer_count; ++l) {     // the run's layers are [layer_count, m, …]: one launch per layer and chunk
       const uint16_t *kl = static_cast<const uint16_t *>(k) + (size_t(l) * m + begin) * tok;
       const uint16_t *vl = static_cast<const uint16_t *>(v) + (size_t(l) * m + begin) * tok;
@@ -677,6 +675,11 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
   if (!k_out || !v_out) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;
+  if (p->pv.kv8) {
+    PASTA_CUDA(launch_kv8_read_run(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count,
+                                   tokens_stride(p, m), k_out, v_out, st, &p->launches));
+    return PASTA_OK;
+  }
   std::vector<int32_t> words;
   for (int32_t begin = 0; begin < m; begin += kRunChunk) {
     const int32_t cnt = std::min(kRunChunk, m - begin);
@@ -688,10 +691,10 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
     }
     pasta_status_t s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
-    PASTA_CUDA(launch_kv_read_layers(p->pv, p->run_slots_dev, cnt, layer_begin, layer_count, tokens_stride(p, m),
-                                     static_cast<uint16_t *>(k_out) + size_t(begin) * tok,
-                                     static_cast<uint16_t *>(v_out) + size_t(begin) * tok, st));
-    p->launches += p->pv.kv8 ? 1 : layer_count;
+    for (int32_t l = 0; l < layer_count; ++l)
+      PASTA_CUDA(launch_kv_read(p->pv, p->run_slots_dev, cnt, layer_begin + l, static_cast<uint16_t *>(k_out) + (size_t(l) * m + begin) * tok,
+                                static_cast<uint16_t *>(v_out) + (size_t(l) * m + begin) * tok, st));
+    p->launches += layer_count;
   }
   return PASTA_OK;
 }

@@ -24,7 +24,20 @@ namespace {
 
 constexpr int A_THREADS = 256, A_WARPS = A_THREADS / 32;
 
-struct Freqs { double f[64]; };          // theta^(-2i/D)
+// Rotation by angle i = f[i] times the position, f[i] = theta^(-2i/D); (c1[i], s1[i]) is the rotation by one position.
+struct Freqs { double f[64], c1[64], s1[64]; };
+// The pages of a run, as kernel arguments (a run needs no copy to the device before it); two sizes, since every launch
+// carries the whole array.
+template <int N> struct PageList { int32_t page[N]; };
+constexpr int kPagesSmall = 64, kPagesLarge = 2048;
+
+// Sines and cosines are kept times 2^896, and a bf16 number becomes the 64-bit number whose exponent field is its own: that
+// is the number times 2^-896, subnormal or not, for two integer instructions in place of a conversion (measured: 17 cycles
+// per warp for a conversion there and back, 2 for a multiplication).  Infinities and NaN are sorted out before.
+constexpr double kTurnScale = 0x1p896;
+__device__ __forceinline__ double scaled_down(uint32_t bits) {       // bits: fp32 bits of a bf16 number
+  return __hiloint2double((bits & 0x80000000u) | ((bits & 0x7fffffffu) >> 3), 0);
+}
 
 // exponent of the scale for a largest magnitude given by its fp32 bits (finite)
 __device__ __forceinline__ int scale_exp(uint32_t amax_bits) {
@@ -58,52 +71,20 @@ __device__ __forceinline__ int grow_scale(uint8_t *block, int8_t *scale, int kv,
   return e;
 }
 
-// One CTA per page group (the new tokens that fall into one page) and slice of the layers; a warp takes one (kv head, K or
-// V) at a time, holds the group's elements in registers, finds their largest magnitude, and writes the codes: every
-// element is read once.  The rotation's sines and cosines (64 bits) are worked out once per CTA for all heads and layers.
+// The new tokens that fall into one page (rows off0 .. off0 + cnt - 1 of it), layers ll .. ll_end - 1, by one CTA: a warp takes
+// one (kv head, K or V) at a time, holds the group's elements in registers, finds their largest magnitude, and writes the
+// codes, so every element is read once.  turn: (cos, sin) of token r, angle i = 8 c + e at r * H + e * (H / 8) + c.
 template <int D, bool kRope>
-__global__ void __launch_bounds__(A_THREADS)
-kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t pos0, int32_t n_tok,
-                  int32_t consecutive, int32_t first_offset, int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta,
-                  int64_t in_layer_stride, const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new,
-                  Freqs freqs) {
+__device__ __forceinline__ void append_page(const PoolView &pv, int page, int off0, int first, int cnt, int layer_begin, int ll, int ll_end,
+                                            int64_t in_layer_stride, const __nv_bfloat16 *__restrict__ k_new,
+                                            const __nv_bfloat16 *__restrict__ v_new, const double2 *turn) {
   constexpr int H = D / 2;
-  __shared__ double2 turn[kRope ? PASTA_PAGE * H : 1];       // (cos, sin) of token r, angle i = 8 c + e at r * H + e * (H / 8) + c
-  grid_launch_dependents();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int first, cnt;
-  if (consecutive) {
-    first = max(0, static_cast<int>(blockIdx.x) * PASTA_PAGE - first_offset);
-    cnt = min(n_tok, (static_cast<int>(blockIdx.x) + 1) * PASTA_PAGE - first_offset) - first;
-  } else {
-    // the CTA of a group's first token takes the group: a token continues one if its slot is the next of the same page
-    first = blockIdx.x;
-    const int page = slots[2 * first], off = slots[2 * first + 1];
-    if (first > 0 && slots[2 * first - 2] == page && slots[2 * first - 1] == off - 1) return;
-    const int a = first + lane;
-    const bool mine = lane < PASTA_PAGE && a < n_tok && slots[2 * a] == page && slots[2 * a + 1] == off + lane;
-    cnt = __ffs(~__ballot_sync(0xffffffffu, mine)) - 1;
-  }
-  const int page = slots[2 * first], off0 = slots[2 * first + 1];
-  if (page < 0 || page >= pv.n_pages || off0 < 0 || off0 + cnt > PASTA_PAGE || cnt < 1) {
-    if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
-    return;
-  }
-  if (kRope) {
-    for (int x = tid; x < cnt * H; x += A_THREADS) {
-      const int r = x / H, i = x % H;
-      double sn, cs;
-      sincos(static_cast<double>(pos ? pos[first + r] : pos0 + first + r) * freqs.f[i], &sn, &cs);
-      turn[r * H + (i & 7) * (H / 8) + (i >> 3)] = make_double2(cs, sn);
-    }
-    __syncthreads();
-  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int Hkv = pv.n_kv_heads;
-  const int ll_end = min(layer_count, (static_cast<int>(blockIdx.y) + 1) * layers_per_cta);
-  for (int ll = blockIdx.y * layers_per_cta; ll < ll_end; ++ll) {
+  for (; ll < ll_end; ++ll) {
     uint8_t *layer = pv.kv_base + (layer_begin + ll) * pv.layer_stride;
     for (int item = warp; item < 2 * Hkv; item += A_WARPS) {
-      const int g = item >> 1, kv = item & 1;
+      const int g = item >> 1, kv = (item ^ (item / A_WARPS)) & 1;      // a warp's items are K and V in turn
       const __nv_bfloat16 *src = (kv ? v_new : k_new) + ll * in_layer_stride + (static_cast<int64_t>(first) * Hkv + g) * D;
       const int64_t at = static_cast<int64_t>(page) * Hkv + g;
       uint8_t *block = layer + at * kv8_block_bytes(D);
@@ -121,12 +102,25 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
           if (r < cnt) {
             const uint4 *row = reinterpret_cast<const uint4 *>(src + static_cast<int64_t>(r) * Hkv * D);
             const uint4 lo4 = __ldg(row + c), hi4 = __ldg(row + c + LPT);
-            const uint32_t lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+            uint32_t lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+            uint32_t m2 = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m2 = __vmaxu2(m2, __vmaxu2(lo[w] & 0x7fff7fffu, hi[w] & 0x7fff7fffu));
+            if ((m2 & 0xffffu) >= 0x7f80u || m2 >= 0x7f800000u) {     // a pair with a number that is not finite: both are zeros
+              bad = true;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                const uint32_t x2 = __vmaxu2(lo[w] & 0x7fff7fffu, hi[w] & 0x7fff7fffu);
+                const uint32_t keep = ((x2 & 0xffffu) >= 0x7f80u ? 0u : 0xffffu) | (x2 >= 0x7f800000u ? 0u : 0xffff0000u);
+                lo[w] &= keep;
+                hi[w] &= keep;
+              }
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const double2 t = turn[r * H + e * (H / 8) + c];
-              const double a = (e & 1) ? bf16_hi(lo[e >> 1]) : bf16_lo(lo[e >> 1]);
-              const double b = (e & 1) ? bf16_hi(hi[e >> 1]) : bf16_lo(hi[e >> 1]);
+              const double a = scaled_down((e & 1) ? lo[e >> 1] & 0xffff0000u : lo[e >> 1] << 16);
+              const double b = scaled_down((e & 1) ? hi[e >> 1] & 0xffff0000u : hi[e >> 1] << 16);
               y[it][e] = static_cast<float>(a * t.x - b * t.y);
               y[it][8 + e] = static_cast<float>(b * t.x + a * t.y);
             }
@@ -199,83 +193,248 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
   }
 }
 
-// One thread per 8 elements of one (token, kv head, K or V): 8 bytes in, 16 bytes out.  blockIdx.y = layer.
-template <int D>
-__global__ void __launch_bounds__(256)
-kv8_read_kernel(PoolView pv, const int32_t *__restrict__ slots, int32_t n_tok, int32_t layer_begin, int64_t out_layer_stride,
-                __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out) {
-  constexpr int CH = D / 8;
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  const int c = static_cast<int>(idx % CH);
-  const int64_t row = idx / CH;                     // (kv, token, head)
-  const int64_t per = static_cast<int64_t>(n_tok) * pv.n_kv_heads;
-  if (row >= 2 * per) return;
-  const int kv = row >= per;
-  const int64_t th = row - kv * per;
-  const int a = static_cast<int>(th / pv.n_kv_heads), g = static_cast<int>(th % pv.n_kv_heads);
-  const int page = slots[2 * a], off = slots[2 * a + 1];
-  if (page < 0 || page >= pv.n_pages || off < 0 || off >= PASTA_PAGE) {
-    report(pv.status, PASTA_ERR_DEVICE_CHECK);
+// Tokens of a step: slots[2 i], slots[2 i + 1] are token i's page and row.  One CTA per group of tokens that are neighbours in
+// one page (the CTA of a group's first token takes it) and slice of the layers; the sines and cosines (64 bits) are worked
+// out once per CTA for all heads and layers.
+template <int D, bool kRope>
+__global__ void __launch_bounds__(A_THREADS, kRope ? 2 : 3)
+kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t n_tok,
+                  int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
+                  const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ Freqs freqs) {
+  constexpr int H = D / 2;
+  __shared__ double2 turn[kRope ? PASTA_PAGE * H : 1];
+  grid_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int first = blockIdx.x;
+  const int page = slots[2 * first], off0 = slots[2 * first + 1];
+  if (first > 0 && slots[2 * first - 2] == page && slots[2 * first - 1] == off0 - 1) return;
+  const int a = first + lane;
+  const bool mine = lane < PASTA_PAGE && a < n_tok && slots[2 * a] == page && slots[2 * a + 1] == off0 + lane;
+  const int cnt = __ffs(~__ballot_sync(0xffffffffu, mine)) - 1;
+  if (page < 0 || page >= pv.n_pages || off0 < 0 || off0 + cnt > PASTA_PAGE || cnt < 1) {
+    if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
     return;
   }
-  const uint8_t *layer = pv.kv_base + (layer_begin + static_cast<int64_t>(blockIdx.y)) * pv.layer_stride;
-  const int64_t at = static_cast<int64_t>(page) * pv.n_kv_heads + g;
-  const float f = pow2f(*(reinterpret_cast<const int8_t *>(layer + pv.scale_off) + at * 2 + kv));
-  const uint2 q = *reinterpret_cast<const uint2 *>(layer + at * kv8_block_bytes(D) + kv8_chunk_offset<D>(kv, off, c >> 1) + (c & 1) * 8);
-  uint32_t h[4], o[4];
-  e4m3x4_to_f16x4(q.x, h[0], h[1]);
-  e4m3x4_to_f16x4(q.y, h[2], h[3]);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h[w]));
-    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * f, v.y * f);      // exact: four significant bits
-    o[w] = *reinterpret_cast<const uint32_t *>(&b);
+  if (kRope) {
+    for (int x = tid; x < cnt * H; x += A_THREADS) {
+      const int r = x / H, i = x % H;
+      double sn, cs;
+      sincos(static_cast<double>(pos[first + r]) * freqs.f[i], &sn, &cs);
+      turn[r * H + (i & 7) * (H / 8) + (i >> 3)] = make_double2(cs * kTurnScale, sn * kTurnScale);
+    }
+    __syncthreads();
   }
-  __nv_bfloat16 *dst = (kv ? v_out : k_out) + blockIdx.y * out_layer_stride + th * D + c * 8;
-  *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+  const int ll = blockIdx.y * layers_per_cta;
+  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, turn);
 }
 
-}  // namespace
+// A run: n_tok tokens of one stream at consecutive positions, the first at row first_offset of the first page.  One CTA per
+// page and slice of the layers.  A thread works out the sine and cosine of one angle at every fourth token and turns it on by
+// one position at a time for the three behind it: three products, each good to a few times 2^-53.
+template <int D, bool kRope, int N>
+__global__ void __launch_bounds__(A_THREADS, kRope ? 2 : 3)
+kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
+                      int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
+                      const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ Freqs freqs) {
+  constexpr int H = D / 2;
+  __shared__ double2 turn[kRope ? PASTA_PAGE * H : 1];
+  grid_launch_dependents();
+  const int tid = threadIdx.x;
+  const int first = max(0, static_cast<int>(blockIdx.x) * PASTA_PAGE - first_offset);
+  const int cnt = min(n_tok, (static_cast<int>(blockIdx.x) + 1) * PASTA_PAGE - first_offset) - first;
+  const int page = pages.page[blockIdx.x], off0 = blockIdx.x == 0 ? first_offset : 0;
+  if (page < 0 || page >= pv.n_pages || cnt < 1) {
+    if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    return;
+  }
+  if (kRope) {
+    for (int x = tid; x < PASTA_PAGE / 4 * H; x += A_THREADS) {
+      const int r = x / H * 4, i = x % H;
+      double2 *at = turn + r * H + (i & 7) * (H / 8) + (i >> 3);
+      double sn = 0, cs = 0;
+      if (r < cnt) sincos(static_cast<double>(pos0 + first + r) * freqs.f[i], &sn, &cs);
+      cs *= kTurnScale;
+      sn *= kTurnScale;
+      const double c1 = freqs.c1[i], s1 = freqs.s1[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (r + j < cnt) at[j * H] = make_double2(cs, sn);
+        const double next = cs * c1 - sn * s1;
+        sn = sn * c1 + cs * s1;
+        cs = next;
+      }
+    }
+    __syncthreads();
+  }
+  const int ll = blockIdx.y * layers_per_cta;
+  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, turn);
+}
 
-cudaError_t launch_kv8_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t pos0, int32_t n_tok,
-                              bool consecutive, int32_t first_offset, int32_t layer_begin, int32_t layer_count,
-                              int64_t in_layer_stride, const void *k_new, const void *v_new, double theta, cudaStream_t st) {
-  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
-  const int groups = consecutive ? (first_offset + n_tok + PASTA_PAGE - 1) / PASTA_PAGE : n_tok;
-  // all layers of a group in one CTA share its sines and cosines; split them only as far as the GPU has to be filled
+// A run read back: one CTA per page and layer (blockIdx.y), a warp per (kv head, K or V); a lane turns 16 codes into 32 bytes.
+template <int D, int N>
+__global__ void __launch_bounds__(A_THREADS, 4)
+kv8_read_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t n_tok, int32_t first_offset, int32_t layer_begin,
+                int64_t out_layer_stride, __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out) {
+  constexpr int LPT = D / 16, TPI = 32 / LPT, NI = PASTA_PAGE / TPI;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane % LPT;
+  const int first = static_cast<int>(blockIdx.x) * PASTA_PAGE - first_offset;       // token of the page's first row
+  const int page = pages.page[blockIdx.x];
+  if (page < 0 || page >= pv.n_pages) {
+    if (threadIdx.x == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    return;
+  }
+  const int Hkv = pv.n_kv_heads;
+  const uint8_t *layer = pv.kv_base + (layer_begin + static_cast<int64_t>(blockIdx.y)) * pv.layer_stride;
+  for (int item = warp; item < 2 * Hkv; item += A_WARPS) {
+    const int g = item >> 1, kv = item & 1;
+    const int64_t at = static_cast<int64_t>(page) * Hkv + g;
+    const uint8_t *block = layer + at * kv8_block_bytes(D);
+    const int ex = *(reinterpret_cast<const int8_t *>(layer + pv.scale_off) + at * 2 + kv);
+    __nv_bfloat16 *out = (kv ? v_out : k_out) + blockIdx.y * out_layer_stride + g * D + c * 16;
+    uint4 q[NI];
+#pragma unroll
+    for (int it = 0; it < NI; ++it)
+      q[it] = *reinterpret_cast<const uint4 *>(block + kv8_chunk_offset<D>(kv, it * TPI + lane / LPT, c));
+    const float f = pow2f(ex);
+#pragma unroll
+    for (int it = 0; it < NI; ++it) {
+      const int t = first + it * TPI + lane / LPT;
+      if (t < 0 || t >= n_tok) continue;
+      const uint32_t w[4] = {q[it].x, q[it].y, q[it].z, q[it].w};
+      uint32_t o[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t h[2];
+        e4m3x4_to_f16x4(w[i], h[0], h[1]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * f, v.y * f);          // exact: four significant bits
+          o[2 * i + j] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+      }
+      uint4 *dst = reinterpret_cast<uint4 *>(out + static_cast<int64_t>(t) * Hkv * D);
+      dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+  }
+}
+
+// the frequencies of a theta, worked out again only when it changes (one table per host thread)
+const Freqs &freqs_of(double theta, int head_dim) {
+  static thread_local Freqs fr;
+  static thread_local double of = 0;
+  static thread_local int dim = 0;
+  if (of != theta || dim != head_dim) {
+    for (int i = 0; i < head_dim / 2; ++i) {
+      fr.f[i] = std::exp2(-2.0 * i / head_dim * std::log2(theta));
+      fr.c1[i] = std::cos(fr.f[i]);
+      fr.s1[i] = std::sin(fr.f[i]);
+    }
+    of = theta;
+    dim = head_dim;
+  }
+  return fr;
+}
+
+// layers per CTA: all layers of a page in one CTA share its sines and cosines; split only as far as the GPU has to be filled
+int layers_per_cta(int groups, int layer_count) {
   const int want = 148 * 4;
   const int slices = std::min(layer_count, std::max(1, (want + groups - 1) / groups));
-  const int per = (layer_count + slices - 1) / slices;
-  const dim3 grid(groups, (layer_count + per - 1) / per);
-  Freqs fr{};
-  if (theta > 0)
-    for (int i = 0; i < pv.head_dim / 2; ++i) fr.f[i] = std::exp2(-2.0 * i / pv.head_dim * std::log2(theta));
-  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
-#define PASTA_A8(DD, RR)                                                                                                     \
-  kv8_append_kernel<DD, RR><<<grid, A_THREADS, 0, st>>>(pv, slots, pos, pos0, n_tok, consecutive ? 1 : 0, first_offset,       \
-                                                        layer_begin, layer_count, per, in_layer_stride, k, v, fr)
+  return (layer_count + slices - 1) / slices;
+}
+
+template <int N>
+PageList<N> list_of(const int32_t *pages, int n) {
+  PageList<N> list;
+  std::copy(pages, pages + n, list.page);
+  return list;
+}
+
+template <int N>
+cudaError_t launch_append_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
+                                int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const __nv_bfloat16 *k,
+                                const __nv_bfloat16 *v, double theta, cudaStream_t st) {
+  const PageList<N> list = list_of<N>(pages, n_pages);
+  const int per = layers_per_cta(n_pages, layer_count);
+  const dim3 grid(n_pages, (layer_count + per - 1) / per);
+  const Freqs &fr = freqs_of(theta > 0 ? theta : 2.0, pv.head_dim);
+#define PASTA_A8(DD, RR)                                                                                                \
+  kv8_append_run_kernel<DD, RR, N><<<grid, A_THREADS, 0, st>>>(pv, list, pos0, n_tok, first_offset, layer_begin, layer_count, per, \
+                                                               in_layer_stride, k, v, fr)
   if (pv.head_dim == 128) { if (theta > 0) PASTA_A8(128, true); else PASTA_A8(128, false); }
   else { if (theta > 0) PASTA_A8(64, true); else PASTA_A8(64, false); }
 #undef PASTA_A8
   return cudaGetLastError();
 }
 
-cudaError_t launch_kv_read_layers(const PoolView &pv, const int32_t *slots, int32_t n_tok, int32_t layer_begin,
-                                  int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st) {
-  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
-  __nv_bfloat16 *k = static_cast<__nv_bfloat16 *>(k_out), *v = static_cast<__nv_bfloat16 *>(v_out);
-  if (!pv.kv8) {
-    for (int32_t l = 0; l < layer_count; ++l) {
-      const cudaError_t e = launch_kv_read(pv, slots, n_tok, layer_begin + l, k + l * out_layer_stride, v + l * out_layer_stride, st);
-      if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
-  }
-  const int64_t threads = 2 * static_cast<int64_t>(n_tok) * pv.n_kv_heads * (pv.head_dim / 8);
-  const dim3 grid(static_cast<unsigned>((threads + 255) / 256), layer_count);
-  if (pv.head_dim == 128) kv8_read_kernel<128><<<grid, 256, 0, st>>>(pv, slots, n_tok, layer_begin, out_layer_stride, k, v);
-  else kv8_read_kernel<64><<<grid, 256, 0, st>>>(pv, slots, n_tok, layer_begin, out_layer_stride, k, v);
+template <int N>
+cudaError_t launch_read_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t n_tok, int32_t first_offset,
+                              int32_t layer_begin, int32_t layer_count, int64_t out_layer_stride, __nv_bfloat16 *k, __nv_bfloat16 *v,
+                              cudaStream_t st) {
+  const PageList<N> list = list_of<N>(pages, n_pages);
+  const dim3 grid(n_pages, layer_count);
+  if (pv.head_dim == 128) kv8_read_kernel<128, N><<<grid, A_THREADS, 0, st>>>(pv, list, n_tok, first_offset, layer_begin, out_layer_stride, k, v);
+  else kv8_read_kernel<64, N><<<grid, A_THREADS, 0, st>>>(pv, list, n_tok, first_offset, layer_begin, out_layer_stride, k, v);
   return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
+                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new, double theta,
+                              cudaStream_t st) {
+  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
+  const int per = layers_per_cta(n_tok, layer_count);
+  const dim3 grid(n_tok, (layer_count + per - 1) / per);
+  const Freqs &fr = freqs_of(theta > 0 ? theta : 2.0, pv.head_dim);
+  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
+#define PASTA_A8(DD, RR) \
+  kv8_append_kernel<DD, RR><<<grid, A_THREADS, 0, st>>>(pv, slots, pos, n_tok, layer_begin, layer_count, per, in_layer_stride, k, v, fr)
+  if (pv.head_dim == 128) { if (theta > 0) PASTA_A8(128, true); else PASTA_A8(128, false); }
+  else { if (theta > 0) PASTA_A8(64, true); else PASTA_A8(64, false); }
+#undef PASTA_A8
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv8_append_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                  const void *v_new, double theta, cudaStream_t st, int64_t *launches) {
+  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const cudaError_t e = n <= kPagesSmall
+        ? launch_append_pages<kPagesSmall>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, theta, st)
+        : launch_append_pages<kPagesLarge>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, theta, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_kv8_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
+                                int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st,
+                                int64_t *launches) {
+  __nv_bfloat16 *k = static_cast<__nv_bfloat16 *>(k_out), *v = static_cast<__nv_bfloat16 *>(v_out);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const cudaError_t e = n <= kPagesSmall
+        ? launch_read_pages<kPagesSmall>(pv, pages, n, cnt, first_offset, layer_begin, layer_count, out_layer_stride, k + done * tok, v + done * tok, st)
+        : launch_read_pages<kPagesLarge>(pv, pages, n, cnt, first_offset, layer_begin, layer_count, out_layer_stride, k + done * tok, v + done * tok, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace pasta

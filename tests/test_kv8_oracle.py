@@ -1,6 +1,8 @@
 """CPU tests of the 8-bit cache's and the capped scores' oracle, of the plans made for an 8-bit pool, and of refusals."""
 import ctypes
 
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -88,6 +90,7 @@ def test_plan_of_an_8bit_pool_cuts_evenly(maker):
 def test_plan_of_an_8bit_pool_respects_the_partial_rows():
     """Few partial rows: the pieces get longer until they fit, whole runs at the least."""
     script = cfg4_long_prefix(1, 3000, 16)
+    script = dataclasses.replace(script, geometry=dataclasses.replace(script.geometry, head_dim=64))
     rows = 17 * script.geometry.n_q_heads
     for factor in (1, 2, 3, 8):
         check_script(script, flags=binding.FLAG_KV_FP8, max_partial_rows=rows * factor)
