@@ -511,28 +511,33 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers) return PASTA_ERR_INVALID_ARG;
   if (layer_count > 0 && p->host_only) return PASTA_ERR_BAD_STATE;
   if (layer_count > 0 && m > 0 && (!k || !v)) return PASTA_ERR_INVALID_ARG;
-  std::vector<Slot> slots;
+  Slot slot{};
   const Request *rq = p->host.request(req);
   const int32_t pos0 = (rq && thread >= 0 && thread < static_cast<int32_t>(rq->threads.size())) ? rq->threads[thread].pos_next : 0;
   // consecutive position ids are assumed below: not so while the main thread owes a jump behind a pending promise
   if (theta > 0.f && m > 1 && thread == 0 && rq && rq->threads[0].pos_skip != 0) return PASTA_ERR_BAD_STATE;
-  pasta_status_t s = p->host.reserve_run(req, thread, m, &slots);
+  pasta_status_t s = p->host.reserve_run(req, thread, m, &slot);
   if (s != PASTA_OK) return s;
   p->plan_valid = false;
   if (layer_count == 0 || m == 0) return PASTA_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;      // elements per token
-  std::vector<int32_t> words;
+  const std::vector<int32_t> &pages = rq->streams[thread].pages;
+  const int32_t at0 = rq->streams[thread].len - m;      // the run's first token within its stream
   if (p->pv.kv8) {         // all layers in one launch, page by page
-    for (int32_t i = 0; i < m; i += PASTA_PAGE - slots[i].offset) words.push_back(slots[i].page);
-    PASTA_CUDA(launch_kv8_append_run(p->pv, words.data(), slots[0].offset, pos0, m, layer_begin, layer_count, tokens_stride(p, m), k, v,
-                                     theta, st, &p->launches));
+    PASTA_CUDA(launch_kv8_append_run(p->pv, pages.data() + at0 / PASTA_PAGE, slot.offset, pos0, m, layer_begin, layer_count,
+                                     tokens_stride(p, m), k, v, theta, st, &p->launches));
     return PASTA_OK;
   }
+  std::vector<int32_t> words;
   for (int32_t begin = 0; begin < m; begin += kRunChunk) {
     const int32_t cnt = std::min(kRunChunk, m - begin);
     words.resize(size_t(cnt) * 2);
-    for (int32_t i = 0; i < cnt; ++i) { words[2 * i] = slots[begin + i].page; words[2 * i + 1] = slots[begin + i].offset; }
+    for (int32_t i = 0; i < cnt; ++i) {
+      const int32_t t = at0 + begin + i;
+      words[2 * i] = pages[t / PASTA_PAGE];
+      words[2 * i + 1] = t % PASTA_PAGE;
+    }
     s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
     for (int32_t l = 0; l < layer_count; ++l) {     // the run's layers are [layer_count, m, …]: one launch per layer and chunk

@@ -71,6 +71,12 @@ __device__ __forceinline__ int grow_scale(uint8_t *block, int8_t *scale, int kv,
   return e;
 }
 
+// Rows of one layer on their way into L2 while the CTA works on something else (16-byte aligned, as the loads require).
+__device__ __forceinline__ void prefetch_rows(const __nv_bfloat16 *k_new, const __nv_bfloat16 *v_new, int64_t at, int bytes) {
+  if (threadIdx.x < 2)
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((threadIdx.x ? v_new : k_new) + at), "r"(bytes) : "memory");
+}
+
 // The new tokens that fall into one page (rows off0 .. off0 + cnt - 1 of it), layers ll .. ll_end - 1, by one CTA: a warp takes
 // one (kv head, K or V) at a time, holds the group's elements in registers, finds their largest magnitude, and writes the
 // codes, so every element is read once.  turn: (cos, sin) of token r, angle i = 8 c + e at r * H + e * (H / 8) + c.
@@ -82,6 +88,7 @@ __device__ __forceinline__ void append_page(const PoolView &pv, int page, int of
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int Hkv = pv.n_kv_heads;
   for (; ll < ll_end; ++ll) {
+    if (ll + 1 < ll_end) prefetch_rows(k_new, v_new, (ll + 1) * in_layer_stride + static_cast<int64_t>(first) * Hkv * D, cnt * Hkv * D * 2);
     uint8_t *layer = pv.kv_base + (layer_begin + ll) * pv.layer_stride;
     for (int item = warp; item < 2 * Hkv; item += A_WARPS) {
       const int g = item >> 1, kv = (item ^ (item / A_WARPS)) & 1;      // a warp's items are K and V in turn
@@ -247,6 +254,8 @@ kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, in
     if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
     return;
   }
+  const int ll = blockIdx.y * layers_per_cta;
+  prefetch_rows(k_new, v_new, ll * in_layer_stride + static_cast<int64_t>(first) * pv.n_kv_heads * D, cnt * pv.n_kv_heads * D * 2);
   if (kRope) {
     for (int x = tid; x < PASTA_PAGE / 4 * H; x += A_THREADS) {
       const int r = x / H * 4, i = x % H;
@@ -266,7 +275,6 @@ kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, in
     }
     __syncthreads();
   }
-  const int ll = blockIdx.y * layers_per_cta;
   append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, turn);
 }
 

@@ -206,7 +206,7 @@ pasta_status_t HostPool::reserve_step(const std::vector<StepEntry> &entries, std
   return PASTA_OK;
 }
 
-pasta_status_t HostPool::reserve_run(int32_t req, int32_t thread, int32_t m, std::vector<Slot> *slots) {
+pasta_status_t HostPool::reserve_run(int32_t req, int32_t thread, int32_t m, Slot *first) {
   Request *r = live(req);
   if (!r || thread < 0 || thread >= static_cast<int32_t>(r->threads.size()) || m < 0)
     return PASTA_ERR_INVALID_ARG;
@@ -217,9 +217,18 @@ pasta_status_t HostPool::reserve_run(int32_t req, int32_t thread, int32_t m, std
   const int64_t need = (n + m + P - 1) / P - (n + P - 1) / P;
   if (need > static_cast<int64_t>(free_.size())) return PASTA_ERR_OUT_OF_PAGES;
   if (m > 0 && !can_extend(*r, thread)) return PASTA_ERR_CAPACITY;
-  slots->clear();
-  slots->reserve(m);
-  for (int32_t i = 0; i < m; ++i) slots->push_back(append_one(*r, thread));
+  if (m == 0) return PASTA_OK;
+  *first = append_one(*r, thread);              // its view entry and position are the run's; the rest only lengthens them
+  Stream &s = r->streams[thread];
+  for (int64_t k = 1; k < need + (n % P == 0 ? 0 : 1); ++k) {
+    s.pages.push_back(free_.front());
+    free_.pop_front();
+  }
+  s.len += m - 1;
+  Thread &th = r->threads[thread];
+  th.pos_next += m - 1;
+  if (m > 1) th.pos_last = th.pos_next - 1;
+  th.view.back().len += m - 1;
   return PASTA_OK;
 }
 

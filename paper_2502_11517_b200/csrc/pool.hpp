@@ -88,7 +88,9 @@ class HostPool {
   // Takes a reserve_step back: lengths, page lists, views and position counters as they were, the pages back at
   // the front of the free sequence in the order they had.
   void undo_step(const std::vector<StepUndo> &undo);
-  pasta_status_t reserve_run(int32_t req, int32_t thread, int32_t m, std::vector<Slot> *slots);
+  // m consecutive tokens of one thread; *first: where the first of them goes (untouched when m = 0).  Work per page, not per
+  // token.
+  pasta_status_t reserve_run(int32_t req, int32_t thread, int32_t m, Slot *first);
 
   const Request *request(int32_t req) const;
   int32_t page_size() const { return page_size_; }
