@@ -23,9 +23,9 @@
 // A copy's weights for columns it does not answer for are zeros.  The two halves of a tile belong to two softmax groups, as in
 // attn_tensor.cu; each copy of a row in each group has its own reference, sum and accumulator row, so nothing is exchanged
 // between the softmax warps until the unit's epilogue.  Measured (us; one softmax thread per row and half tile throughout in
-// brackets): 64 requests of 4 to 36 rows 178 (197), 68 rows behind long prefixes 231 (219), short capped responses 199 (231).
+// brackets): 64 requests of 4 to 36 rows 167 (197), 68 rows behind long prefixes 200, short capped responses 188 (231).
 //
-// Warp roles (384 threads): warp 0 producer (4 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
+// Warp roles (384 threads): warp 0 producer (4 or 5 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
 // of P.V, two score buffers in TMEM), warps 2-3 build the Q operand, warps 4-7 and 8-11 the two softmax groups.  Every wait is
 // bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
 #include <cuda_fp16.h>
@@ -37,7 +37,6 @@ namespace pasta {
 namespace {
 
 constexpr int F_THREADS = 384;
-constexpr int F_STAGES = 4;
 constexpr int F_WARPS = 8;                                      // softmax: two groups of four warps
 constexpr int F_HALF = T_TILE / 2;                              // columns of one softmax group
 constexpr int F_FACTORS = 4;                                    // units whose rows' score factors are kept
@@ -45,25 +44,31 @@ constexpr int F_BLOCK = kv8_block_bytes(128);
 constexpr int F_STAGE_BYTES = PASTA_TILE_PAGES * F_BLOCK;       // 32 KB
 constexpr int F_Q_TERM = 128 * 128, F_Q_BYTES = 2 * F_Q_TERM;   // 32 KB: two terms
 constexpr int F_SUM_BYTES = 16384;                              // per group: where the copies' accumulators are added up
-constexpr int OFF_Q = 0;
-constexpr int OFF_STAGE = OFF_Q + F_Q_BYTES;
-constexpr int OFF_SUM = OFF_STAGE + F_STAGES * F_STAGE_BYTES;
-constexpr int OFF_BAR = OFF_SUM + 2 * F_SUM_BYTES;
+
+// Shared memory and barriers (8 bytes each).  The room that copies' accumulators take to be added up is a stage's.
+template <int NC>
+struct F {
+  static constexpr int STAGES = NC < 64 ? 4 : 5;
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_STAGE = OFF_Q + F_Q_BYTES;
+  static constexpr int OFF_SUM = OFF_STAGE + STAGES * F_STAGE_BYTES;
+  static constexpr int OFF_BAR = OFF_SUM + (NC < 64 ? 2 * F_SUM_BYTES : 0);
 // barriers (8 bytes each)
-constexpr int B_FULL = 0, B_EMPTY = B_FULL + F_STAGES, B_SFULL = B_EMPTY + F_STAGES, B_PFULL = B_SFULL + 2,      // PFULL[2 b + group]
-              B_QFULL = B_PFULL + 4, B_QFREE = B_QFULL + 1, B_OFULL = B_QFREE + 1, B_OFREE = B_OFULL + 1,
-              B_MLFULL = B_OFREE + 1, B_SUM = B_MLFULL + 1,     // [group] the epilogue's additions
-              B_FACTORS = B_SUM + 2,                            // the rows' score factors of unit uc % F_FACTORS are there
-              B_DRAIN = B_FACTORS + F_FACTORS,                  // only used when a role gave up
-              B_COUNT = B_DRAIN + 1;
-constexpr int OFF_META = OFF_BAR + 8 * ((B_COUNT + 1) & ~1);    // per stage: 8 page metas
-constexpr int OFF_SCALE = OFF_META + F_STAGES * 32;             // per stage: 8 pages' exponents, ek + (ev << 8)
-constexpr int OFF_MISC = OFF_SCALE + F_STAGES * 32;             // tmem base, abort flag, shared units taken, their records
-constexpr int OFF_ML = OFF_MISC + 16 + 64 * T_RING;             // [unit parity][warp][lane] (reference, sum) for the epilogue
-constexpr int OFF_FACTORS = OFF_ML + 2 * F_WARPS * 256;         // [F_FACTORS][128] floats
-constexpr int F_SMEM_BYTES = OFF_FACTORS + F_FACTORS * 512 + 1024;      // slack to align the base to 1024
-static_assert(OFF_META % 16 == 0 && OFF_MISC % 16 == 0, "records are read as int4");
-static_assert(F_SMEM_BYTES <= 232448, "shared memory budget");
+  static constexpr int B_FULL = 0, B_EMPTY = B_FULL + STAGES, B_SFULL = B_EMPTY + STAGES, B_PFULL = B_SFULL + 2,      // PFULL[2 b + group]
+                B_QFULL = B_PFULL + 4, B_QFREE = B_QFULL + 1, B_OFULL = B_QFREE + 1, B_OFREE = B_OFULL + 1,
+                B_MLFULL = B_OFREE + 1, B_SUM = B_MLFULL + 1,     // [group] the epilogue's additions
+                B_FACTORS = B_SUM + 2,                            // the rows' score factors of unit uc % F_FACTORS are there
+                B_DRAIN = B_FACTORS + F_FACTORS,                  // only used when a role gave up
+                B_COUNT = B_DRAIN + 1;
+  static constexpr int OFF_META = OFF_BAR + 8 * ((B_COUNT + 1) & ~1);    // per stage: 8 page metas
+  static constexpr int OFF_SCALE = OFF_META + STAGES * 32;             // per stage: 8 pages' exponents, ek + (ev << 8)
+  static constexpr int OFF_MISC = OFF_SCALE + STAGES * 32;             // tmem base, abort flag, shared units taken, their records
+  static constexpr int OFF_ML = OFF_MISC + 16 + 64 * T_RING;             // [unit parity][warp][lane] (reference, sum) for the epilogue
+  static constexpr int OFF_FACTORS = OFF_ML + 2 * F_WARPS * 256;         // [F_FACTORS][128] floats
+  static constexpr int SMEM_BYTES = OFF_FACTORS + F_FACTORS * 512 + 1024;      // slack to align the base to 1024
+  static_assert(OFF_META % 16 == 0 && OFF_MISC % 16 == 0, "records are read as int4");
+  static_assert(SMEM_BYTES <= 232448, "shared memory budget");
+};
 
 // TMEM columns: S[b] at 128 b (group g's half at 64 g, its P in the first 32 of that: two terms of 16), O_g at 256 + 128 g
 constexpr uint32_t COL_S = 0, COL_O = 256;
@@ -114,20 +119,6 @@ __device__ __forceinline__ void split4(float a, float b, float c, float d, uint3
   lo = l0 | (static_cast<uint32_t>(l1) << 16);
 }
 
-// The same for four weights 2^8 w0 .. 2^8 w3 (0 <= w <= 1), by the bits: w as fp16 has its exponent where e4m3's would be
-// for 2^8 w (fp16's bias is 8 larger), so bits 7..14 of the fp16 are the e4m3 code of the truncated number, subnormals
-// included.  hi truncates, lo is the exact rest rounded to the nearest code (half a code's step is added before its bits are
-// taken).  Half the pipe time of the conversion instructions (14 simple instructions for four weights).
-__device__ __forceinline__ void split4_weights(float w0, float w1, float w2, float w3, uint32_t &hi, uint32_t &lo) {
-  const __half2 g0 = __floats2half2_rn(w0, w2), g1 = __floats2half2_rn(w1, w3);
-  const uint32_t b0 = *reinterpret_cast<const uint32_t *>(&g0), b1 = *reinterpret_cast<const uint32_t *>(&g1);
-  const uint32_t t0 = b0 & 0xff80ff80u, t1 = b1 & 0xff80ff80u;
-  const __half2 r0 = __hsub2(g0, *reinterpret_cast<const __half2 *>(&t0)), r1 = __hsub2(g1, *reinterpret_cast<const __half2 *>(&t1));
-  const uint32_t c0 = *reinterpret_cast<const uint32_t *>(&r0) + 0x00400040u, c1 = *reinterpret_cast<const uint32_t *>(&r1) + 0x00400040u;
-  hi = ((b0 >> 7) & 0x00ff00ffu) | ((b1 << 1) & 0xff00ff00u);
-  lo = ((c0 >> 7) & 0x00ff00ffu) | ((c1 << 1) & 0xff00ff00u);
-}
-
 // A wait of a whole warp in which one lane polls: a poll of 32 lanes on one barrier word is served lane by lane by the
 // shared memory that the MMAs read their operands from.
 __device__ __forceinline__ bool warp_wait1(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
@@ -142,6 +133,8 @@ __device__ __forceinline__ bool warp_wait1(uint32_t bar, uint32_t parity, volati
 template <int NC, bool kCap>
 __global__ void __launch_bounds__(F_THREADS, 1)
 attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) {
+  using L = F<NC>;
+  constexpr int F_STAGES = L::STAGES;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -149,34 +142,34 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = pv.n_q_heads / pv.n_kv_heads;
   const int g_shift = 31 - __clz(G);                              // G is 1, 2, 4 or 8
-  const uint32_t bar = base + OFF_BAR;
-  int32_t *meta_s = reinterpret_cast<int32_t *>(sm + OFF_META);
-  int32_t *scale_s = reinterpret_cast<int32_t *>(sm + OFF_SCALE);
-  uint32_t *misc = reinterpret_cast<uint32_t *>(sm + OFF_MISC);
-  float *factor_s = reinterpret_cast<float *>(sm + OFF_FACTORS);
-  float2 *ml_s = reinterpret_cast<float2 *>(sm + OFF_ML);
+  const uint32_t bar = base + L::OFF_BAR;
+  int32_t *meta_s = reinterpret_cast<int32_t *>(sm + L::OFF_META);
+  int32_t *scale_s = reinterpret_cast<int32_t *>(sm + L::OFF_SCALE);
+  uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);
+  float *factor_s = reinterpret_cast<float *>(sm + L::OFF_FACTORS);
+  float2 *ml_s = reinterpret_cast<float2 *>(sm + L::OFF_ML);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(misc + 1);
   const int32_t *plan = pv.plan;
 
   // ---- set-up (operand bytes that no copy fills meet zero weights, so they only have to be finite: see attn_tensor.cu)
   if (tid == 0) {
-    for (int s = 0; s < F_STAGES; ++s) { mbar_init(bar + 8 * (B_FULL + s), 2); mbar_init(bar + 8 * (B_EMPTY + s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(bar + 8 * (B_SFULL + b), 1); mbar_init(bar + 8 * (B_SUM + b), 4); }
-    for (int b = 0; b < 4; ++b) mbar_init(bar + 8 * (B_PFULL + b), 4);
-    mbar_init(bar + 8 * B_QFULL, 2);
-    mbar_init(bar + 8 * B_QFREE, 1);
-    mbar_init(bar + 8 * B_OFULL, 1);
-    mbar_init(bar + 8 * B_OFREE, F_WARPS);
-    mbar_init(bar + 8 * B_MLFULL, F_WARPS);
-    for (int f = 0; f < F_FACTORS; ++f) mbar_init(bar + 8 * (B_FACTORS + f), 2);
-    mbar_init(bar + 8 * B_DRAIN, 1);
+    for (int s = 0; s < F_STAGES; ++s) { mbar_init(bar + 8 * (L::B_FULL + s), 2); mbar_init(bar + 8 * (L::B_EMPTY + s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(bar + 8 * (L::B_SFULL + b), 1); mbar_init(bar + 8 * (L::B_SUM + b), 4); }
+    for (int b = 0; b < 4; ++b) mbar_init(bar + 8 * (L::B_PFULL + b), 4);
+    mbar_init(bar + 8 * L::B_QFULL, 2);
+    mbar_init(bar + 8 * L::B_QFREE, 1);
+    mbar_init(bar + 8 * L::B_OFULL, 1);
+    mbar_init(bar + 8 * L::B_OFREE, F_WARPS);
+    mbar_init(bar + 8 * L::B_MLFULL, F_WARPS);
+    for (int f = 0; f < F_FACTORS; ++f) mbar_init(bar + 8 * (L::B_FACTORS + f), 2);
+    mbar_init(bar + 8 * L::B_DRAIN, 1);
     misc[1] = 0;
     misc[2] = 0;
     mbar_init_fence();
   }
   fence_proxy_async();
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + OFF_MISC), "r"(TMEM_COLS)
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::OFF_MISC), "r"(TMEM_COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -233,18 +226,18 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         const int s = i % F_STAGES;
         const int n_valid = min(PASTA_TILE_PAGES, x.n_pages - tile * PASTA_TILE_PAGES);
         if (i < F_STAGES && n_valid < PASTA_TILE_PAGES) {       // first use of this stage and some slots stay empty
-          uint4 *slot = reinterpret_cast<uint4 *>(sm + OFF_STAGE + s * F_STAGE_BYTES + n_valid * F_BLOCK);
+          uint4 *slot = reinterpret_cast<uint4 *>(sm + L::OFF_STAGE + s * F_STAGE_BYTES + n_valid * F_BLOCK);
           for (int j = lane; j < (PASTA_TILE_PAGES - n_valid) * (F_BLOCK / 16); j += 32) slot[j] = make_uint4(0, 0, 0, 0);
           fence_proxy_async();
         }
         __syncwarp();
-        if (lane == 0) mbar_expect_tx(bar + 8 * (B_FULL + s), n_valid * F_BLOCK);
+        if (lane == 0) mbar_expect_tx(bar + 8 * (L::B_FULL + s), n_valid * F_BLOCK);
         __syncwarp();
         const int first = ((tile - x.tile_begin) & 3) * PASTA_TILE_PAGES, r = lane - first;
         if (r >= 0 && r < n_valid)
-          bulk_g2s_stream(base + OFF_STAGE + s * F_STAGE_BYTES + r * F_BLOCK,
+          bulk_g2s_stream(base + L::OFF_STAGE + s * F_STAGE_BYTES + r * F_BLOCK,
                           kv_layer + (static_cast<int64_t>(page) * pv.n_kv_heads + x.g) * F_BLOCK, F_BLOCK,
-                          bar + 8 * (B_FULL + s), policy);
+                          bar + 8 * (L::B_FULL + s), policy);
       };
       auto store_scales = [&](int tile, uint32_t i) {
         const int s = i % F_STAGES, first = ((tile - x.tile_begin) & 3) * PASTA_TILE_PAGES, r = lane - first;
@@ -253,7 +246,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           scale_s[s * PASTA_TILE_PAGES + r] = sc;
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar + 8 * (B_FULL + s));
+        if (lane == 0) mbar_arrive(bar + 8 * (L::B_FULL + s));
       };
       int copied = x.tile_begin;                  // tiles of this unit whose copies have been issued
       for (int tile = x.tile_begin; tile < x.tile_end; ++tile, ++it) {
@@ -264,13 +257,13 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           ask(tile + 8, n2_page, n2_meta);
         }
         if (copied == tile) {
-          if (!warp_wait1(bar + 8 * (B_EMPTY + it % F_STAGES), ((it / F_STAGES) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
+          if (!warp_wait1(bar + 8 * (L::B_EMPTY + it % F_STAGES), ((it / F_STAGES) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
           copies(tile, it);
           ++copied;
           // the first batch: further tiles whose stages are free already, before the scales are waited for
           for (; tile == x.tile_begin && copied < min(x.tile_end, tile + 4); ++copied) {
             const uint32_t i = it + (copied - tile);
-            int free = lane == 0 ? mbar_test_wait(bar + 8 * (B_EMPTY + i % F_STAGES), ((i / F_STAGES) & 1) ^ 1) : 0;
+            int free = lane == 0 ? mbar_test_wait(bar + 8 * (L::B_EMPTY + i % F_STAGES), ((i / F_STAGES) & 1) ^ 1) : 0;
             if (!__shfl_sync(0xffffffffu, free, 0)) break;
             copies(copied, i);
           }
@@ -281,7 +274,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       }
       if (!ok)                                    // so that every stage with copies in flight becomes full for the tear-down
         for (uint32_t i = it; i < prod_it; ++i)
-          if (lane == 0) mbar_arrive(bar + 8 * (B_FULL + i % F_STAGES));
+          if (lane == 0) mbar_arrive(bar + 8 * (L::B_FULL + i % F_STAGES));
     }
   } else if (warp == 1) {
     // ================================================================ MMA issue (one thread)
@@ -294,34 +287,34 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       for (; ok && next_unit<false, true>(wk, a, plan, u0, u1, ring, counter, lane, false, abort_flag, limit, ok, x, ll); ++uc) {
         const int nt = x.tile_end - x.tile_begin;
         const uint32_t m_bits = unit_m64<NC>(x.n_threads << g_shift) ? IDESC_M64 : IDESC_M128;
-        if (!wait_or_abort(bar + 8 * B_QFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
+        if (!wait_or_abort(bar + 8 * L::B_QFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
         tc_fence_after();
         for (int k = 0; k <= nt && ok; ++k) {
           if (k < nt) {
             // ---- S[b] = Q . K^T for tile `it` (S[b] was last used by tile it - 2, whose P.V was issued before this)
             const uint32_t s = it % F_STAGES, b = it & 1;
-            if (!wait_or_abort(bar + 8 * (B_FULL + s), (it / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
+            if (!wait_or_abort(bar + 8 * (L::B_FULL + s), (it / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t k_addr = base + OFF_STAGE + s * F_STAGE_BYTES;
+            const uint32_t k_addr = base + L::OFF_STAGE + s * F_STAGE_BYTES;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {     // the two terms of Q one after the other, four steps of 32 elements each
               const uint32_t term = ks >> 2, kk = ks & 3;
-              mma8_ss(tmem + COL_S + b * T_TILE, smem_desc(base + OFF_Q + term * F_Q_TERM + kk * 32, 16, 1024),
+              mma8_ss(tmem + COL_S + b * T_TILE, smem_desc(base + L::OFF_Q + term * F_Q_TERM + kk * 32, 16, 1024),
                       smem_desc(k_addr + kk * 32, 16, 2048), IDESC_QK8 | m_bits, ks > 0);
             }
-            mma_commit(bar + 8 * (B_SFULL + b));
-            if (k == nt - 1) mma_commit(bar + 8 * B_QFREE);       // the Q operand may be replaced once these finish
+            mma_commit(bar + 8 * (L::B_SFULL + b));
+            if (k == nt - 1) mma_commit(bar + 8 * L::B_QFREE);       // the Q operand may be replaced once these finish
           }
           if (k > 0) {
             // ---- O_g += P_g . V_g for both halves of tile `it - 1` (when k == nt, `it` already points past it)
             const uint32_t j = it - 1;
             const uint32_t s = j % F_STAGES, b = j & 1;
             if (k == 1 && uc > 0) {   // the unit's first P.V overwrites the accumulators: the previous unit's rows must be read out
-              if (!wait_or_abort(bar + 8 * B_OFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
+              if (!wait_or_abort(bar + 8 * L::B_OFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
             }
-            const uint32_t v_addr = base + OFF_STAGE + s * F_STAGE_BYTES + 1024;
+            const uint32_t v_addr = base + L::OFF_STAGE + s * F_STAGE_BYTES + 1024;
             for (uint32_t g = 0; g < 2 && ok; ++g) {
-              if (!wait_or_abort(bar + 8 * (B_PFULL + 2 * b + g), (j >> 1) & 1, abort_flag, limit)) { ok = false; break; }
+              if (!wait_or_abort(bar + 8 * (L::B_PFULL + 2 * b + g), (j >> 1) & 1, abort_flag, limit)) { ok = false; break; }
               tc_fence_after();
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks) {   // steps of 32 tokens (two pages), the two terms of the weights
@@ -331,8 +324,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
               }
             }
             if (!ok) break;
-            mma_commit(bar + 8 * (B_EMPTY + s));
-            if (k == nt) mma_commit(bar + 8 * B_OFULL);
+            mma_commit(bar + 8 * (L::B_EMPTY + s));
+            if (k == nt) mma_commit(bar + 8 * L::B_OFULL);
           }
           if (k < nt) ++it;
         }
@@ -380,7 +373,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           split4(bf16_lo(val[c].z) * f, bf16_hi(val[c].z) * f, bf16_lo(val[c].w) * f, bf16_hi(val[c].w) * f, h1, l1);
           val[c] = make_uint4(h0, h1, l0, l1);
         }
-        if (r0 == 0 && uc > 0 && !warp_wait1(bar + 8 * B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
+        if (r0 == 0 && uc > 0 && !warp_wait1(bar + 8 * L::B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
         // A row's factor is read by the softmax threads of this unit.  The place of unit uc is written again for unit uc + 4,
         // after Q.K^T of unit uc + 3 and hence P.V of unit uc + 2 has been issued: the softmax of unit uc is long over.
         if (half == 0 && row < rows) factor_s[(uc % F_FACTORS) * 128 + row] = fmaxf(a.scale_log2 * pow2f(-up), 1e-30f);
@@ -388,7 +381,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
 #pragma unroll
           for (int copy = 0; copy < COPIES; ++copy) {
             const int at_row = copy * copy_rows + row, r8 = at_row & 7;
-            uint8_t *dst = sm + OFF_Q + at_row * 128;
+            uint8_t *dst = sm + L::OFF_Q + at_row * 128;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {         // 16 codes of a term: two of val's entries
               const int at = ((half * 4 + c) ^ r8) << 4;
@@ -401,8 +394,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(bar + 8 * (B_FACTORS + uc % F_FACTORS));
-        mbar_arrive(bar + 8 * B_QFULL);
+        mbar_arrive(bar + 8 * (L::B_FACTORS + uc % F_FACTORS));
+        mbar_arrive(bar + 8 * L::B_QFULL);
       }
     }
   } else {
@@ -428,13 +421,13 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       const bool warp_active = NC < 64 || (m64 ? wq * 16 : wq * 32) < rows;
       const int vis_at = a.off_vis + x.vis_off + (active ? row >> g_shift : 0) * x.n_streams;
       const int vis0 = plan[vis_at];
-      if (!warp_wait1(bar + 8 * (B_FACTORS + uc % F_FACTORS), (uc / F_FACTORS) & 1, abort_flag, limit)) { ok = false; break; }
+      if (!warp_wait1(bar + 8 * (L::B_FACTORS + uc % F_FACTORS), (uc / F_FACTORS) & 1, abort_flag, limit)) { ok = false; break; }
       const float factor = active ? factor_s[(uc % F_FACTORS) * 128 + row] : 1.f;
       float ref = -INFINITY, l = 0.f;
       for (int k = 0; k < nt; ++k, ++it) {
         const uint32_t s = it % F_STAGES, b = it & 1;
         const uint32_t s_addr = tmem + lane_addr + COL_S + b * T_TILE + grp * F_HALF;
-        if (!warp_wait1(bar + 8 * (B_FULL + s), (it / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
+        if (!warp_wait1(bar + 8 * (L::B_FULL + s), (it / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
         int thr[PAGES], sc2[PAGES];
         bool full = true;
 #pragma unroll
@@ -454,7 +447,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             full = full && t == PASTA_PAGE;
           }
         }
-        if (!warp_wait1(bar + 8 * (B_SFULL + b), (it >> 1) & 1, abort_flag, limit)) { ok = false; break; }
+        if (!warp_wait1(bar + 8 * (L::B_SFULL + b), (it >> 1) & 1, abort_flag, limit)) { ok = false; break; }
         tc_fence_after();
         if (warp_active) {
           float sc[NC], c_pg[PAGES], mt = -INFINITY;
@@ -501,7 +494,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           if (__any_sync(0xffffffffu, rescale)) {
             // O_g and l are relative to ref: move them to the new reference.  The accumulator is quiet once the P.V of the
             // previous tile has finished, which is what releases that tile's stage.
-            if (!warp_wait1(bar + 8 * (B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
+            if (!warp_wait1(bar + 8 * (L::B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
             tc_fence_after();
             const float f = rescale ? fast_exp2(ref - (mt - 4.f)) : 1.f;
 #pragma unroll 1
@@ -524,7 +517,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
 #pragma unroll
           for (int pg = 0; pg < PAGES; ++pg) {
             const int ev = static_cast<int8_t>(sc2[pg] >> 8);
-            const float add = static_cast<float>(ev) - rf - 8.f;      // weights leave exp2 as 2^-8 of what the MMA reads
+            const float add = static_cast<float>(ev) - rf;
             float ls[2] = {0.f, 0.f};
             uint32_t hi[4], lo[4];
 #pragma unroll
@@ -535,9 +528,9 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
               const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
               add2(ls[0], ls[1], p0, p1);
               add2(ls[0], ls[1], p2, p3);
-              split4_weights(p0, p1, p2, p3, hi[j >> 2], lo[j >> 2]);
+              split4(p0, p1, p2, p3, hi[j >> 2], lo[j >> 2]);
             }
-            l = fmaf(ls[0] + ls[1], pow2f(8 - ev), l);
+            l = fmaf(ls[0] + ls[1], pow2f(-ev), l);
             tmem_st4(s_addr + 4 * (page0 + pg), hi[0], hi[1], hi[2], hi[3]);
             tmem_st4(s_addr + 16 + 4 * (page0 + pg), lo[0], lo[1], lo[2], lo[3]);
           }
@@ -550,7 +543,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar + 8 * (B_PFULL + 2 * b + grp));
+        if (lane == 0) mbar_arrive(bar + 8 * (L::B_PFULL + 2 * b + grp));
       }
       if (!ok) break;
 
@@ -561,8 +554,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       const int qn = active && keeps && fin ? plan[a.off_tq + x.tq_off + (row >> g_shift)] : 0;
       ml_s[((uc & 1) * F_WARPS + warp - 4) * 32 + lane] = make_float2(ref, l);
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar + 8 * B_MLFULL);
-      if (!warp_wait1(bar + 8 * B_MLFULL, uc & 1, abort_flag, limit) || !warp_wait1(bar + 8 * B_OFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
+      if (lane == 0) mbar_arrive(bar + 8 * L::B_MLFULL);
+      if (!warp_wait1(bar + 8 * L::B_MLFULL, uc & 1, abort_flag, limit) || !warp_wait1(bar + 8 * L::B_OFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
       tc_fence_after();
       if (warp_active) {
         constexpr int COPIES = 64 / NC;
@@ -590,7 +583,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             f1 = part[2 * i + 1].y > 0.f ? fast_exp2(part[2 * i + 1].x - m_all) * inv : 0.f;
           }
         const uint32_t o_addr = tmem + lane_addr + COL_O + grp * 64;
-        float *slots = reinterpret_cast<float *>(sm + OFF_SUM + grp * F_SUM_BYTES) + lane;
+        float *slots = reinterpret_cast<float *>(sm + L::OFF_SUM + grp * F_SUM_BYTES) + lane;
         auto folded = [&](int h, float *v) {      // 16 of the group's columns, both accumulators
           uint32_t r0[16], r1[16];
           tmem_ld16_issue(o_addr + h, r0);
@@ -602,8 +595,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         };
         auto meet = [&](uint32_t n) {             // the group's four warps; n: how many times before this
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar + 8 * (B_SUM + grp));
-          return warp_wait1(bar + 8 * (B_SUM + grp), n & 1, abort_flag, limit);
+          if (lane == 0) mbar_arrive(bar + 8 * (L::B_SUM + grp));
+          return warp_wait1(bar + 8 * (L::B_SUM + grp), n & 1, abort_flag, limit);
         };
         if (NC < 64) {
           if (wq >= 2) {
@@ -665,7 +658,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar + 8 * B_OFREE);
+      if (lane == 0) mbar_arrive(bar + 8 * L::B_OFREE);
     }
   }
 
@@ -676,11 +669,11 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
     // see attn_tensor.cu: what is still in flight for this CTA (bulk copies, MMAs) ends on its own and is waited for
     if (warp == 0 && lane == 0) {
       for (uint32_t j = (prod_it > F_STAGES ? prod_it - F_STAGES : 0); j < prod_it; ++j)
-        mbar_wait_bounded(bar + 8 * (B_FULL + j % F_STAGES), (j / F_STAGES) & 1);
+        mbar_wait_bounded(bar + 8 * (L::B_FULL + j % F_STAGES), (j / F_STAGES) & 1);
     }
     if (warp == 1 && lane == 0) {
-      mma_commit(bar + 8 * B_DRAIN);
-      mbar_wait_bounded(bar + 8 * B_DRAIN, 0);
+      mma_commit(bar + 8 * L::B_DRAIN);
+      mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
     }
     if (tid == 0) report(pv.status, PASTA_ERR_TIMEOUT);
     tc_fence_before();
@@ -693,16 +686,13 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
 
 }  // namespace
 
-cudaError_t launch_attn_kv8_tensor(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
-                                   const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
-  if (pv.head_dim != 128) return cudaErrorInvalidValue;
-  static uint64_t prepared[6] = {0, 0, 0, 0, 0, 0};
+template <int NC>
+static cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                            const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
+  static uint64_t prepared[2] = {0, 0};
   const bool cap = pv.softcap_log2 > 0.f;
-  const int rows = h.w[PH_T_MAX_ROWS], size = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
-  const auto kernel = size == 0 ? (cap ? attn_kv8_tensor_kernel<16, true> : attn_kv8_tensor_kernel<16, false>)
-                      : size == 1 ? (cap ? attn_kv8_tensor_kernel<32, true> : attn_kv8_tensor_kernel<32, false>)
-                                  : (cap ? attn_kv8_tensor_kernel<64, true> : attn_kv8_tensor_kernel<64, false>);
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), F_SMEM_BYTES, &prepared[2 * size + cap]);
+  const auto kernel = cap ? attn_kv8_tensor_kernel<NC, true> : attn_kv8_tensor_kernel<NC, false>;
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), F<NC>::SMEM_BYTES, &prepared[cap]);
   if (e != cudaSuccess) return e;
   const int grid = h.w[PH_T_GRID];
   if (grid == 0 || layer_count == 0) return cudaSuccess;
@@ -715,7 +705,16 @@ cudaError_t launch_attn_kv8_tensor(const PoolView &pv, const PlanHeader &h, int3
   a.scale_log2 = scale_log2;
   a.cap_k2 = cap ? 2.f * 1.4426950408889634f / pv.softcap_log2 : 0.f;
   a.out = out; a.lse = lse; a.out_bf16 = out_bf16 ? 1 : 0;
-  return launch_overlapped(kernel, dim3(grid), dim3(F_THREADS), F_SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
+  return launch_overlapped(kernel, dim3(grid), dim3(F_THREADS), F<NC>::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
+}
+
+cudaError_t launch_attn_kv8_tensor(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                                   const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
+  if (pv.head_dim != 128) return cudaErrorInvalidValue;
+  const int rows = h.w[PH_T_MAX_ROWS];
+  return rows <= 32 ? launch_t<16>(pv, h, layer_begin, layer_count, q, scale_log2, out, lse, out_bf16, st)
+       : rows <= 64 ? launch_t<32>(pv, h, layer_begin, layer_count, q, scale_log2, out, lse, out_bf16, st)
+                    : launch_t<64>(pv, h, layer_begin, layer_count, q, scale_log2, out, lse, out_bf16, st);
 }
 
 }  // namespace pasta
