@@ -470,7 +470,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = fmaxf(factor * pow2f(static_cast<int8_t>(sc2[pg] & 0xff)), 1e-37f);   // never 0: it meets -inf
           if (kCap) {
 #pragma unroll
-            for (int j = 0; j < NC; ++j) sc[j] = softcap(sc[j] * c_pg[j >> 4], cap, a.cap_k2);
+            for (int j = 0; j < NC; ++j) sc[j] *= c_pg[j >> 4] * a.cap_inv;
+            softcap_columns<NC>(sc, cap, active);
 #pragma unroll
             for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = 1.f;    // capped scores are in log2 units from here on
           }
@@ -703,7 +704,7 @@ static cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, int32_t lay
   a.off_dunit = h.w[PH_OFF_DUNIT]; a.n_dunits = h.w[PH_N_DUNITS];
   a.n_queries = h.w[PH_N_QUERIES]; a.layer_begin = layer_begin; a.layer_count = layer_count;
   a.scale_log2 = scale_log2;
-  a.cap_k2 = cap ? 2.f * 1.4426950408889634f / pv.softcap_log2 : 0.f;
+  a.cap_inv = cap ? 1.f / pv.softcap_log2 : 0.f;
   a.out = out; a.lse = lse; a.out_bf16 = out_bf16 ? 1 : 0;
   return launch_overlapped(kernel, dim3(grid), dim3(F_THREADS), F<NC>::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
 }

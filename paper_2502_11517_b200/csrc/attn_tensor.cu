@@ -352,10 +352,11 @@ attn_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ 
               tmem_ld_order32(raw_sc + 32);
             }
             // capped scores are in log2 units from here on, plain ones still without their scale
-            const float scale = kCap ? 1.f : a.scale_log2;
+            const float scale = kCap ? 1.f : a.scale_log2, cap_scale = a.scale_log2 * a.cap_inv;
             if (kCap) {
 #pragma unroll
-              for (int j = 0; j < T_HALF; ++j) sc[j] = softcap(sc[j] * a.scale_log2, pv.softcap_log2, a.cap_k2);
+              for (int j = 0; j < T_HALF; ++j) sc[j] *= cap_scale;
+              softcap_columns<T_HALF>(sc, pv.softcap_log2, active);
             }
             if (!full) {
 #pragma unroll
@@ -566,7 +567,7 @@ cudaError_t launch_attn_tensor(const PoolView &pv, const PlanHeader &h, int32_t 
   a.off_dunit = h.w[PH_OFF_DUNIT]; a.n_dunits = h.w[PH_N_DUNITS];
   a.n_queries = h.w[PH_N_QUERIES]; a.layer_begin = layer_begin; a.layer_count = layer_count;
   a.scale_log2 = scale_log2;
-  a.cap_k2 = cap ? 2.f * 1.4426950408889634f / pv.softcap_log2 : 0.f;
+  a.cap_inv = cap ? 1.f / pv.softcap_log2 : 0.f;
   a.out = out; a.lse = lse; a.out_bf16 = out_bf16 ? 1 : 0;
   return launch_overlapped(kernel, dim3(grid), dim3(T_THREADS), T_SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
 }

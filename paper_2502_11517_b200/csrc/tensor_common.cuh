@@ -158,6 +158,55 @@ __device__ __forceinline__ void add2(float &s0, float &s1, float p0, float p1) {
       "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
       : "+f"(s0), "+f"(s1) : "f"(p0), "f"(p1));
 }
+// {a0, a1} = {a0, a1} * {b0, b1} + {c, c}
+__device__ __forceinline__ void horner2(float &a0, float &a1, float b0, float b1, float c) {
+  asm("{\n\t.reg .b64 ra, rb, rc;\n\t"
+      "mov.b64 ra, {%0, %1};\n\tmov.b64 rb, {%2, %3};\n\tmov.b64 rc, {%4, %4};\n\t"
+      "fma.rn.f32x2 ra, ra, rb, rc;\n\tmov.b64 {%0, %1}, ra;\n\t}"
+      : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1), "f"(c));
+}
+// {x0, x1} = {a0, a1} * {b0, b1}
+__device__ __forceinline__ void mul2(float &x0, float &x1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
+      "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// x[j] = C tanh(x[j]) for the N scores of every thread of a warp; x = score / C, C in log2 units.
+// The formula with ex2 and rcp (softcap) takes two of the special-function unit's slots, 16 cycles per column and warp, on top
+// of the weight's one; the exponential units are what bounds a capped tile.  Scores that a cap is meant for mostly lie well
+// inside it, so a warp whose scores all have |x| <= 1 takes a polynomial on the FMA pipe instead (9 packed operations for two
+// columns): tanh(x) / x interpolated at seven Chebyshev nodes in x^2 over [0, 1], off by less than 2^-24 there, 2^-23 as
+// evaluated in fp32; softcap's own bound is 2^-21.  Rows that are not active do not count.
+template <int N>
+__device__ __forceinline__ void softcap_columns(float *x, float C, bool active) {
+  float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    m0 = fmaxf(m0, fabsf(x[j]));
+    m1 = fmaxf(m1, fabsf(x[j + 1]));
+  }
+  if (__any_sync(0xffffffffu, active && fmaxf(m0, m1) > 1.f)) {
+    const float k2 = 2.f * 1.4426950408889634f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = softcap(x[j], C, k2);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+      float u0, u1, t0 = 1.0380251e-3f, t1 = 1.0380251e-3f;
+      mul2(u0, u1, x[j], x[j + 1], x[j], x[j + 1]);
+      horner2(t0, t1, u0, u1, -6.1943247e-3f);
+      horner2(t0, t1, u0, u1, 2.0279707e-2f);
+      horner2(t0, t1, u0, u1, -5.3451646e-2f);
+      horner2(t0, t1, u0, u1, 0.13325076f);
+      horner2(t0, t1, u0, u1, -0.33332828f);
+      horner2(t0, t1, u0, u1, 0.99999994f);
+      mul2(t0, t1, t0, t1, x[j], x[j + 1]);
+      mul2(x[j], x[j + 1], t0, t1, C, C);
+    }
+  }
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -211,7 +260,7 @@ struct TensorArgs {
   int32_t off_dunit, n_dunits;      // units no CTA owns in advance (per layer): taken from a counter at run time
   int32_t n_queries, layer_begin, layer_count;
   float scale_log2;
-  float cap_k2;                     // capped scores: 2 log2(e) / C (see softcap)
+  float cap_inv;                    // capped scores: 1 / C, C in log2 units
   void *out;                        // [layer_count, n_queries, Hq, 128], fp32 or bf16: rows of final units go here
   float *lse;                       // [layer_count, n_queries, Hq] or null
   int32_t out_bf16;
