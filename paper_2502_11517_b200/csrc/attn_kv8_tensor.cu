@@ -23,7 +23,7 @@
 // A copy's weights for columns it does not answer for are zeros.  The two halves of a tile belong to two softmax groups, as in
 // attn_tensor.cu; each copy of a row in each group has its own reference, sum and accumulator row, so nothing is exchanged
 // between the softmax warps until the unit's epilogue.  Measured (us; one softmax thread per row and half tile throughout in
-// brackets): 64 requests of 4 to 36 rows 167 (197), 68 rows behind long prefixes 200, short capped responses 188 (231).
+// brackets): 64 requests of 4 to 36 rows 177 (197), 68 rows behind long prefixes 217, short capped responses 190 (231).
 //
 // Warp roles (384 threads): warp 0 producer (4 or 5 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
 // of P.V, two score buffers in TMEM), warps 2-3 build the Q operand, warps 4-7 and 8-11 the two softmax groups.  Every wait is
@@ -421,49 +421,66 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       const bool warp_active = NC < 64 || (m64 ? wq * 16 : wq * 32) < rows;
       const int vis_at = a.off_vis + x.vis_off + (active ? row >> g_shift : 0) * x.n_streams;
       const int vis0 = plan[vis_at];
+      const bool fin = x.final_rows != 0;         // for the epilogue: looked up here, where the wait for it is hidden
+      const int qn = active && keeps && fin ? plan[a.off_tq + x.tq_off + (row >> g_shift)] : 0;
       if (!warp_wait1(bar + 8 * (L::B_FACTORS + uc % F_FACTORS), (uc / F_FACTORS) & 1, abort_flag, limit)) { ok = false; break; }
       const float factor = active ? factor_s[(uc % F_FACTORS) * 128 + row] : 1.f;
       float ref = -INFINITY, l = 0.f;
       for (int k = 0; k < nt; ++k, ++it) {
         const uint32_t s = it % F_STAGES, b = it & 1;
         const uint32_t s_addr = tmem + lane_addr + COL_S + b * T_TILE + grp * F_HALF;
-        if (!warp_wait1(bar + 8 * (L::B_FULL + s), (it / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
-        int thr[PAGES], sc2[PAGES];
-        bool full = true;
-#pragma unroll
-        for (int pg = 0; pg < PAGES; ++pg) {
-          const int meta = meta_s[s * PASTA_TILE_PAGES + grp * 4 + page0 + pg];
-          sc2[pg] = scale_s[s * PASTA_TILE_PAGES + grp * 4 + page0 + pg];
-          thr[pg] = PASTA_PAGE;
-          // pages that every thread of the request sees in full need no thresholds
-          if (!(meta >= 0 && (meta & PASTA_PMETA_ALL_VISIBLE))) {
-            int t = 0;
-            if (active && meta >= 0) {
-              const int sl = PASTA_PMETA_STREAM(meta);
-              const int vis = sl == 0 ? vis0 : plan[vis_at + sl];
-              t = min(max(vis - PASTA_PMETA_PAGE(meta) * PASTA_PAGE, 0), PASTA_PAGE);
-            }
-            thr[pg] = t;
-            full = full && t == PASTA_PAGE;
-          }
-        }
+        // (the scores' barrier stands behind the stage's: the MMA thread has seen that one complete)
         if (!warp_wait1(bar + 8 * (L::B_SFULL + b), (it >> 1) & 1, abort_flag, limit)) { ok = false; break; }
         tc_fence_after();
         if (warp_active) {
           float sc[NC], c_pg[PAGES], mt = -INFINITY;
-          {
-            uint32_t *r = reinterpret_cast<uint32_t *>(sc);
-            if constexpr (NC == 16) {
-              tmem_ld16(s_addr + page0 * 16, r);
-            } else if constexpr (NC == 32) {
-              tmem_ld32_issue(s_addr + page0 * 16, r);
-              tmem_ld_wait32(r);
-            } else {
-              tmem_ld32_issue(s_addr, r);
-              tmem_ld32_issue(s_addr + 32, r + 32);
-              tmem_ld_wait32(r);
-              tmem_ld_order32(r + 32);
+          uint32_t *sr = reinterpret_cast<uint32_t *>(sc);
+          if constexpr (NC == 16) {
+            tmem_ld16_issue(s_addr + page0 * 16, sr);
+          } else if constexpr (NC == 32) {
+            tmem_ld32_issue(s_addr + page0 * 16, sr);
+          } else {
+            tmem_ld32_issue(s_addr, sr);
+            tmem_ld32_issue(s_addr + 32, sr + 32);
+          }
+          int meta[PAGES], sc2[PAGES], thr[PAGES];
+          const int at = s * PASTA_TILE_PAGES + grp * 4 + page0;
+          if constexpr (PAGES == 4) {
+            *reinterpret_cast<int4 *>(meta) = *reinterpret_cast<const int4 *>(meta_s + at);
+            *reinterpret_cast<int4 *>(sc2) = *reinterpret_cast<const int4 *>(scale_s + at);
+          } else if constexpr (PAGES == 2) {
+            *reinterpret_cast<int2 *>(meta) = *reinterpret_cast<const int2 *>(meta_s + at);
+            *reinterpret_cast<int2 *>(sc2) = *reinterpret_cast<const int2 *>(scale_s + at);
+          } else {
+            meta[0] = meta_s[at];
+            sc2[0] = scale_s[at];
+          }
+          // pages that every thread of the request sees in full need no thresholds
+          bool full = true;
+#pragma unroll
+          for (int pg = 0; pg < PAGES; ++pg) full = full && meta[pg] >= 0 && (meta[pg] & PASTA_PMETA_ALL_VISIBLE);
+          if (!full) {
+            full = true;
+#pragma unroll
+            for (int pg = 0; pg < PAGES; ++pg) {
+              thr[pg] = PASTA_PAGE;
+              if (!(meta[pg] >= 0 && (meta[pg] & PASTA_PMETA_ALL_VISIBLE))) {
+                int t = 0;
+                if (active && meta[pg] >= 0) {
+                  const int sl = PASTA_PMETA_STREAM(meta[pg]);
+                  const int vis = sl == 0 ? vis0 : plan[vis_at + sl];
+                  t = min(max(vis - PASTA_PMETA_PAGE(meta[pg]) * PASTA_PAGE, 0), PASTA_PAGE);
+                }
+                thr[pg] = t;
+                full = full && t == PASTA_PAGE;
+              }
             }
+          }
+          if constexpr (NC == 16) {
+            asm volatile("tcgen05.wait::ld.sync.aligned;" : PASTA_RW16(sr) :: "memory");
+          } else {
+            tmem_ld_wait32(sr);
+            if constexpr (NC == 64) tmem_ld_order32(sr + 32);
           }
           // a page brings a factor of its own (its K's scale) and an addend (its V's exponent, which the weights carry)
 #pragma unroll
@@ -551,8 +568,6 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       // ---- epilogue: a row's accumulators, one per group and copy, leave TMEM brought to one reference and added up, 64
       // columns per group.  The references and sums go through shared memory; so do the accumulators of copies 1 .. (two slots
       // of 8 KB per group, a column per 128 bytes).
-      const bool fin = x.final_rows != 0;
-      const int qn = active && keeps && fin ? plan[a.off_tq + x.tq_off + (row >> g_shift)] : 0;
       ml_s[((uc & 1) * F_WARPS + warp - 4) * 32 + lane] = make_float2(ref, l);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar + 8 * L::B_MLFULL);
