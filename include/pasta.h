@@ -67,10 +67,11 @@ enum {
  * PASTA_ERR_DEVICE_CHECK: everything in an 8-bit pool is finite.
  * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16);
  * pasta_kv_read returns the numbers held, which bf16 represents exactly.  pasta_kv_bytes is n_layers * (n_pages *
- * n_kv_heads * (32 * head_dim + 2) bytes, the scales' part rounded up to 1024).  The attention runs on one kernel for
- * head_dim 64 and 128 for requests of up to 128 stacked rows (threads x group) and 4095 streams; the sums are fp32 and the
- * softmax weights are rounded to fp16 for the product with V.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the
- * warp-shuffle kernel, which rounds no weight.
+ * n_kv_heads * (32 * head_dim + 2) bytes, the scales' part rounded up to 1024).  Requests of up to 128 stacked rows (threads
+ * x group) and 4095 streams run on tensor cores, sums in fp32: with head_dim 128 queries and softmax weights enter as two e4m3
+ * terms each (8 significant bits; a query's element is off by at most 2^-17 of its row's largest, a weight by 2^-8 of
+ * itself), with head_dim 64 queries as fp16 of rows scaled by a power of two and weights as fp16.  PASTA_FLAG_NO_TENSOR_PATH
+ * and larger requests take the warp-shuffle kernel, which rounds no weight.
  */
 
 /* thread states reported by pasta_pool_dump */

@@ -1,4 +1,4 @@
-// K2 of an 8-bit pool: split-K decode attention over e4m3 codes with one scale per (page, kv head).
+// K2 of an 8-bit pool, head_dim 64: split-K decode attention over e4m3 codes with one scale per (page, kv head).
 //
 //   s[r, j]  = q_r . (2^ek Kcode_j) * scale                     (optionally capped: C tanh(s / C))
 //   p'[r, j] = 2^(s log2e + ev - ref_r)                         ev: the scale exponent of the page's V, folded into the weight
@@ -7,11 +7,13 @@
 // Folding ev into the exponent makes p' the size of the token's contribution, so the running reference ref_r (raised only
 // when exceeded by more than 2^8) bounds what goes through fp16, whatever the pages' scales are.
 //
-// What bounds it: bytes.  A page of one kv head is 32 D bytes (4 KB at D = 128), which an SM gets in about 176 cycles of
-// the measured copy bandwidth.  Codes become fp16 exactly (cvt e4m3x2, 2 cycles per warp and scheduler), Q.K^T and P.V
-// are fp16 mma.sync with fp32 sums (8 cycles per m16n8k16): 64 cycles of matrix pipe per page and 16 rows, and about as
-// many of issue.  The rows of a request (threads x group) are 4 to 36 in the usual steps.  (The e4m3 form of mma.sync is
-// slower here: 850 instructions per page and 16 rows were counted with it, against 300.)
+// What bounds it.  A page of one kv head is 2 KB, which an SM gets in about 88 cycles of the measured copy bandwidth.  Codes
+// become fp16 exactly (cvt e4m3x2, 2 cycles per warp and scheduler), Q.K^T and P.V are fp16 mma.sync with fp32 sums (8 cycles
+// per m16n8k16): 32 cycles of matrix pipe per page and 16 rows, and several times that of issue, which is what is left:
+// 32 requests of 8 to 20 rows, 2 layers, 75 MB: 31.9 us, 38 % of the copy bandwidth, against 12.2 us for the bytes.
+// (mma.sync because a row of codes is 64 bytes and the steps have few rows: the e4m3 form of mma.sync is slower, 850
+// instructions per page and 16 rows were counted with it at head_dim 128 against 300 here; tcgen05 at head_dim 128 comes out
+// even with this kernel below 64 rows and ahead above, see attn_kv8_tensor.cu.)
 //
 // One CTA of W warps per (unit, layer, group of row tiles).  A row tile is 16 stacked rows; the group's `tiles` row tiles are
 // spread over the warps, warp w = lane_of_pages * tiles + tile, so that W / tiles pairs of pages are worked on at a time and
@@ -35,6 +37,7 @@ namespace pasta {
 
 namespace {
 
+constexpr int D = 64;                      // head_dim
 constexpr int E_LAG = 1;                   // stages a shared ring is refilled behind the one being worked on
 
 struct Kv8Args {
@@ -63,7 +66,7 @@ __host__ __device__ constexpr int kv8_max_groups(int tiles) {            // CTAs
   return most;
 }
 
-template <int D, int W>
+template <int W>
 struct Kv8Smem {
   static constexpr int STAGES = 2 * W;                               // of the CTA, two pages each
   static constexpr int BLOCK = kv8_block_bytes(D);
@@ -102,10 +105,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-template <int D, int W, bool kCap>
+template <int W, bool kCap>
 __global__ void __launch_bounds__(32 * W, 12 / W)
 attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
-  using S = Kv8Smem<D, W>;
+  using S = Kv8Smem<W>;
   constexpr int KS = D / 16, NT = D / 8;                          // k-steps of Q.K^T, output tiles of P.V
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -239,7 +242,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
       for (int h = 0; h < D / 64; ++h) {
         uint4 kk[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) kk[j] = lds128(blk + pg * S::BLOCK + kv8_chunk_offset<D>(0, tok + 2 * j, D == 128 ? 2 * tq + h : tq));
+        for (int j = 0; j < 2; ++j) kk[j] = lds128(blk + pg * S::BLOCK + kv8_chunk_offset<D>(0, tok + 2 * j, tq));
         const uint32_t kw[2][4] = {{kk[0].x, kk[0].y, kk[0].z, kk[0].w}, {kk[1].x, kk[1].y, kk[1].z, kk[1].w}};
 #pragma unroll
         for (int w = 0; w < 4; ++w)
@@ -259,7 +262,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
       float mx = -INFINITY;
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
-        const float c = c1[h] * pow2f(static_cast<int8_t>(sc2[pg] & 0xff)), fev = static_cast<float>(static_cast<int8_t>(sc2[pg] >> 8));
+        const float c = code_factor(c1[h], static_cast<int8_t>(sc2[pg] & 0xff)), fev = static_cast<float>(static_cast<int8_t>(sc2[pg] >> 8));
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -437,14 +440,14 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
   }
 }
 
-template <int D, int W, bool kCap>
+template <int W, bool kCap>
 cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, Kv8Args a, int32_t layer_count, const void *q, cudaStream_t st) {
-  using S = Kv8Smem<D, W>;
+  using S = Kv8Smem<W>;
   static uint64_t prepared = 0;
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_kv8_kernel<D, W, kCap>), S::TOTAL, &prepared);
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_kv8_kernel<W, kCap>), S::TOTAL, &prepared);
   if (e != cudaSuccess) return e;
   a.groups = kv8_max_groups<W>((h.w[PH_T_MAX_ROWS] + 15) / 16);
-  return launch_overlapped(attn_kv8_kernel<D, W, kCap>, dim3(h.w[PH_N_TUNITS] * a.groups, layer_count), dim3(32 * W), S::TOTAL, st,
+  return launch_overlapped(attn_kv8_kernel<W, kCap>, dim3(h.w[PH_N_TUNITS] * a.groups, layer_count), dim3(32 * W), S::TOTAL, st,
                            pv, a, static_cast<const __nv_bfloat16 *>(q));
 }
 
@@ -452,15 +455,15 @@ cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, Kv8Args a, int32_t
 
 cudaError_t launch_attn_kv8(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                             const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
+  if (pv.head_dim != D) return cudaErrorInvalidValue;
   if (h.w[PH_N_TUNITS] == 0 || layer_count == 0) return cudaSuccess;
   const Kv8Args a{h.w[PH_OFF_TUNIT], h.w[PH_OFF_PAGES], h.w[PH_OFF_PMETA], h.w[PH_OFF_VIS], h.w[PH_OFF_TQ],
                   h.w[PH_N_QUERIES], layer_begin, 1, scale_log2, out, lse, out_bf16 ? 1 : 0};
   const bool cap = pv.softcap_log2 > 0.f;
   const bool wide = h.w[PH_WHOLE_RUNS] != 0;
-#define PASTA_E(DD, WW, CC) \
-  if (pv.head_dim == DD && wide == (WW == 6) && cap == CC) return launch_t<DD, WW, CC>(pv, h, a, layer_count, q, st);
-  PASTA_E(128, 2, false) PASTA_E(128, 2, true) PASTA_E(128, 6, false) PASTA_E(128, 6, true)
-  PASTA_E(64, 2, false) PASTA_E(64, 2, true) PASTA_E(64, 6, false) PASTA_E(64, 6, true)
+#define PASTA_E(WW, CC) \
+  if (wide == (WW == 6) && cap == CC) return launch_t<WW, CC>(pv, h, a, layer_count, q, st);
+  PASTA_E(2, false) PASTA_E(2, true) PASTA_E(6, false) PASTA_E(6, true)
 #undef PASTA_E
   return cudaErrorInvalidValue;
 }

@@ -484,7 +484,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           }
           // a page brings a factor of its own (its K's scale) and an addend (its V's exponent, which the weights carry)
 #pragma unroll
-          for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = fmaxf(factor * pow2f(static_cast<int8_t>(sc2[pg] & 0xff)), 1e-37f);   // never 0: it meets -inf
+          for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = fmaxf(code_factor(factor, static_cast<int8_t>(sc2[pg] & 0xff)), 1e-37f);   // never 0: it meets -inf
           if (kCap) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) sc[j] *= c_pg[j >> 4] * a.cap_inv;

@@ -10,8 +10,12 @@ namespace pasta {
 // one response with 10-tile runs: a CTA that walks a run alone needs 2.9 us per tile more, the merge kernel that cutting
 // brings with it 10.7 us, so cutting pays from the fourth tile on.
 constexpr int32_t kWholeRunSlackTiles = 3;
-// Even cuts (8-bit pools): pieces of at least this many tiles, and about this many pieces per resident CTA.
-constexpr int32_t kEvenMinTiles = 4;
+// Even cuts (8-bit pools, head_dim 64): pieces of at least 2 tiles and about one per resident CTA, and runs left whole while
+// the longest is at most 12 tiles longer than an even share (they then go to CTAs of six warps, which walk a tile in a third
+// of the time).  Measured, us for 1, 4, 12, 32 and 100 responses of 8 to 20 rows: 12.0, 18.0, 17.7, 30.6, 75.3; pieces of at
+// least 8 tiles 12.0, 20.8, 17.6, 30.7, 75.1; two pieces per CTA 14.8, 18.3, 17.7, 30.7, 79.0; a slack of 3 tiles 15.3, 16.0,
+// 19.6, 32.6, 75.5.
+constexpr int32_t kEvenMinTiles = 2;
 constexpr int32_t kEvenPerSlot = 1;
 constexpr int32_t kEvenWholeSlackTiles = 12;
 

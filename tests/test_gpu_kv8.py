@@ -301,6 +301,120 @@ def test_values_that_are_not_finite_are_stored_as_zero_and_reported(lib):
     assert pool.status() == lib.DEVICE_CHECK
 
 
+@pytest.mark.parametrize("d,theta,runs", [(64, 10000.0, [5, 2048 * 16 + 200]), (64, 0.0, [11, 65 * 16, 2048 * 16]),
+                                          (128, 500000.0, [1, 63 * 16, 16, 64 * 16 + 15])])
+def test_runs_of_more_pages_than_a_launch_carries(lib, d, theta, runs):
+    """Runs around and beyond the two sizes of page list, starting inside a page."""
+    n = sum(runs)
+    pool = _pool(lib, n // 16 + 1, hq=1, hkv=1, d=d)
+    model, store = PoolModel(n // 16 + 1, 16), Kv8Store(n // 16 + 1, 16, 1, d)
+    pool.request_begin(); model.request_begin()
+    at = 0
+    for i, m in enumerate(runs):
+        k, v = _randn((1, m, 1, d), 30 + i, gain=2.0 ** i), _randn((1, m, 1, d), 40 + i)
+        slots = model.append_run(0, 0, m)
+        if theta:
+            pool.kv_append_run_rope(0, 0, m, k.cuda(), v.cuda(), theta)
+            store.write(slots, rotate(k[0], np.arange(at, at + m), theta), v[0])
+        else:
+            pool.kv_append_run(0, 0, m, k.cuda(), v.cuda())
+            store.write(slots, k[0], v[0])
+        at += m
+    held_equals(pool, model, {0: store}, [0])
+    k, v = pool.kv_read_layers(0, 0, 7, n - 9)                        # a part, neither end on a page
+    slots = [(p, o) for p, o in model.visible_slots(0, 0)][7:n - 2]
+    wk, wv = store.gather(slots)
+    assert np.array_equal(k[0].double().cpu().numpy(), wk) and np.array_equal(v[0].double().cpu().numpy(), wv)
+    assert pool.status() == 0
+
+
+@pytest.mark.parametrize("theta", [0.0, 10000.0])
+def test_numbers_at_the_ends_of_the_range(lib, theta):
+    """Zeros, subnormal, smallest and largest bf16 numbers, alone in a page and side by side; a rotation that leaves fp32."""
+    import torch
+    sizes = [0.0, 2.0 ** -133, 2.0 ** -127, 2.0 ** -126, 2.0 ** -70, 1.0, 2.0 ** 60, 2.0 ** 72, 2.0 ** 100, 3.3e38]
+    n = 16 * (len(sizes) + 1)
+    pool = _pool(lib, n // 16)
+    model, store = PoolModel(n // 16, 16), Kv8Store(n // 16, 16, 2, 128)
+    pool.request_begin(); model.request_begin()
+    g = torch.Generator().manual_seed(3)
+    unit = 1.0 - 2.0 * torch.randint(0, 2, (1, n, 2, 128), generator=g)
+    gain = torch.tensor(sizes + [1.0]).repeat_interleave(16).reshape(1, n, 1, 1).repeat(1, 1, 2, 1)
+    gain[0, -16:, 0, 0] = torch.tensor((sizes * 2)[:16])               # the last page mixes them
+    k, v = (unit * gain).to(torch.bfloat16), (unit.flip(1) * gain).to(torch.bfloat16)
+    slots = model.append_run(0, 0, n)
+    if theta:
+        pool.kv_append_run_rope(0, 0, n, k.cuda(), v.cuda(), theta)
+        with np.errstate(over="ignore"):
+            store.write(slots, rotate(k[0], np.arange(n), theta), v[0])
+    else:
+        pool.kv_append_run(0, 0, n, k.cuda(), v.cuda())
+        store.write(slots, k[0], v[0])
+    held_equals(pool, model, {0: store}, [0])
+    assert (pool.status() == lib.DEVICE_CHECK) == (store.nonfinite > 0)
+
+
+@pytest.mark.parametrize("d,flags", [(64, 0), (128, 0), (128, 2)])
+def test_query_rows_of_any_size(lib, d, flags):
+    """Rows of zeros, subnormal and huge numbers.  Over K = 0 every score is 0, so each row is the mean of V, whatever is in q."""
+    import torch
+    hq, n = 8, 50
+    pool = _pool(lib, 8, threads=2, hq=hq, hkv=2, d=d, flags=flags)
+    k, v = torch.zeros((1, n, 2, d), dtype=torch.bfloat16), _randn((1, n, 2, d), 2)
+    pool.request_begin()
+    pool.kv_append_run(0, 0, n, k.cuda(), v.cuda())
+    sizes = torch.tensor([0.0, 2.0 ** -133, 2.0 ** -126, 2.0 ** -60, 1.0, 2.0 ** 60, 2.0 ** 120, 3.3e38]).reshape(1, 1, hq, 1)
+    q = ((1.0 - 2.0 * (torch.arange(d) % 2)) * sizes).to(torch.bfloat16)
+    pool.step_begin([0], [0], [0])
+    out = torch.empty((1, 1, hq, d), device="cuda"); lse = torch.empty((1, 1, hq), device="cuda")
+    pool.decode_attn(q.cuda(), out, lse)
+    _, held = pool.kv_read(0, 0, 0, 0, n)
+    mean = held.double().mean(0).repeat_interleave(4, 0)
+    # equal weights 1 / n: each rounded as above, by at most 2^-8 of itself
+    assert (out[0, 0].double() - mean).abs().max() <= (2.0 ** -8 + 2.0 ** -20) * held.double().abs().max()
+    assert (lse[0, 0].double() - np.log(n)).abs().max() <= 2.0 ** -18
+    assert pool.status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_pools_at_once_on_two_streams(lib, d):
+    """Steps of two pools enqueued in turn on two streams, and one of them captured and replayed beside the other's calls."""
+    import torch
+    T, L, n = 9, 2, 700
+    tensors, pools, refs = [], [], []
+    for i in range(2):
+        pool = _pool(lib, 80, threads=T, hq=8, hkv=2, d=d, layers=L, max_step_queries=T)
+        pool.request_begin()
+        pool.kv_append_run(0, 0, n + 50 * i, _randn((L, n + 50 * i, 2, d), i).cuda(), _randn((L, n + 50 * i, 2, d), 10 + i).cuda())
+        for _ in range(T - 1):
+            pool.thread_spawn(0)
+        kn, vn, q = (_randn((L, T, h, d), s + i).cuda() for h, s in ((2, 20), (2, 30), (8, 40)))
+        pool.step_begin([0] * T, list(range(T)))
+        pool.kv_append(kn, vn)
+        out = torch.empty((L, T, 8, d), device="cuda")
+        pool.decode_attn(q, out)
+        torch.cuda.synchronize()
+        pools.append(pool); tensors.append(q); refs.append(out)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.full_like(refs[i], 7.0) for _ in range(12)] for i in range(2)]
+    for j in range(12):
+        for i in range(2):
+            pools[i].decode_attn(tensors[i], outs[i][j], stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, refs[i]) for i in range(2) for o in outs[i])
+    graph, captured = torch.cuda.CUDAGraph(), torch.zeros_like(refs[0])
+    with torch.cuda.graph(graph):
+        pools[0].decode_attn(tensors[0], captured)
+    other = torch.zeros_like(refs[1])
+    for _ in range(5):
+        with torch.cuda.stream(streams[0]):
+            graph.replay()
+        pools[1].decode_attn(tensors[1], other, stream=streams[1])
+    torch.cuda.synchronize()
+    assert torch.equal(captured, refs[0]) and torch.equal(other, refs[1])
+    assert pools[0].status() == 0 and pools[1].status() == 0
+
+
 def test_every_way_to_run_a_step_gives_the_same(lib):
     """decode_attn on another stream, captured and replayed, per layer, without workspace, through step_device and step_host,
     with launches that do not overlap, and with bf16 outputs."""
