@@ -23,11 +23,12 @@
 // A copy's weights for columns it does not answer for are zeros.  The two halves of a tile belong to two softmax groups, as in
 // attn_tensor.cu; each copy of a row in each group has its own reference, sum and accumulator row, so nothing is exchanged
 // between the softmax warps until the unit's epilogue.  Measured (us; one softmax thread per row and half tile throughout in
-// brackets): 64 requests of 4 to 36 rows 177 (197), 68 rows behind long prefixes 217, short capped responses 190 (231).
+// brackets): 64 requests of 4 to 36 rows 165 (197), 68 rows behind long prefixes 211 (219), short capped responses 163 (231).
 //
 // Warp roles (384 threads): warp 0 producer (4 or 5 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
 // of P.V, two score buffers in TMEM), warps 2-3 build the Q operand, warps 4-7 and 8-11 the two softmax groups.  Every wait is
-// bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
+// bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.  (All lanes of a warp poll: one lane that polls and tells
+// the others costs 150 cycles more a wait, 178, 218 and 188 us in the cases above.)
 #include <cuda_fp16.h>
 
 #include "tensor_common.cuh"
@@ -117,16 +118,6 @@ __device__ __forceinline__ void split4(float a, float b, float c, float d, uint3
   asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l1) : "r"(*reinterpret_cast<const uint32_t *>(&g1)));
   hi = h0 | (static_cast<uint32_t>(h1) << 16);
   lo = l0 | (static_cast<uint32_t>(l1) << 16);
-}
-
-// A wait of a whole warp in which one lane polls: a poll of 32 lanes on one barrier word is served lane by lane by the
-// shared memory that the MMAs read their operands from.
-__device__ __forceinline__ bool warp_wait1(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
-  int ok = 1;
-  if ((threadIdx.x & 31) == 0) ok = wait_or_abort(bar, parity, abort_flag, limit);
-  ok = __shfl_sync(0xffffffffu, ok, 0);
-  __syncwarp();
-  return ok != 0;
 }
 
 // NC: columns per softmax thread: 16 when every unit of the plan has at most 32 rows, 32 up to 64, 64 otherwise
@@ -257,7 +248,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           ask(tile + 8, n2_page, n2_meta);
         }
         if (copied == tile) {
-          if (!warp_wait1(bar + 8 * (L::B_EMPTY + it % F_STAGES), ((it / F_STAGES) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
+          if (!warp_wait_or_abort(bar + 8 * (L::B_EMPTY + it % F_STAGES), ((it / F_STAGES) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
           copies(tile, it);
           ++copied;
           // the first batch: further tiles whose stages are free already, before the scales are waited for
@@ -373,7 +364,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           split4(bf16_lo(val[c].z) * f, bf16_hi(val[c].z) * f, bf16_lo(val[c].w) * f, bf16_hi(val[c].w) * f, h1, l1);
           val[c] = make_uint4(h0, h1, l0, l1);
         }
-        if (r0 == 0 && uc > 0 && !warp_wait1(bar + 8 * L::B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
+        if (r0 == 0 && uc > 0 && !warp_wait_or_abort(bar + 8 * L::B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
         // A row's factor is read by the softmax threads of this unit.  The place of unit uc is written again for unit uc + 4,
         // after Q.K^T of unit uc + 3 and hence P.V of unit uc + 2 has been issued: the softmax of unit uc is long over.
         if (half == 0 && row < rows) factor_s[(uc % F_FACTORS) * 128 + row] = fmaxf(a.scale_log2 * pow2f(-up), 1e-30f);
@@ -423,14 +414,14 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       const int vis0 = plan[vis_at];
       const bool fin = x.final_rows != 0;         // for the epilogue: looked up here, where the wait for it is hidden
       const int qn = active && keeps && fin ? plan[a.off_tq + x.tq_off + (row >> g_shift)] : 0;
-      if (!warp_wait1(bar + 8 * (L::B_FACTORS + uc % F_FACTORS), (uc / F_FACTORS) & 1, abort_flag, limit)) { ok = false; break; }
+      if (!warp_wait_or_abort(bar + 8 * (L::B_FACTORS + uc % F_FACTORS), (uc / F_FACTORS) & 1, abort_flag, limit)) { ok = false; break; }
       const float factor = active ? factor_s[(uc % F_FACTORS) * 128 + row] : 1.f;
       float ref = -INFINITY, l = 0.f;
       for (int k = 0; k < nt; ++k, ++it) {
         const uint32_t s = it % F_STAGES, b = it & 1;
         const uint32_t s_addr = tmem + lane_addr + COL_S + b * T_TILE + grp * F_HALF;
         // (the scores' barrier stands behind the stage's: the MMA thread has seen that one complete)
-        if (!warp_wait1(bar + 8 * (L::B_SFULL + b), (it >> 1) & 1, abort_flag, limit)) { ok = false; break; }
+        if (!warp_wait_or_abort(bar + 8 * (L::B_SFULL + b), (it >> 1) & 1, abort_flag, limit)) { ok = false; break; }
         tc_fence_after();
         if (warp_active) {
           float sc[NC], c_pg[PAGES], mt = -INFINITY;
@@ -512,7 +503,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           if (__any_sync(0xffffffffu, rescale)) {
             // O_g and l are relative to ref: move them to the new reference.  The accumulator is quiet once the P.V of the
             // previous tile has finished, which is what releases that tile's stage.
-            if (!warp_wait1(bar + 8 * (L::B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
+            if (!warp_wait_or_abort(bar + 8 * (L::B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
             tc_fence_after();
             const float f = rescale ? fast_exp2(ref - (mt - 4.f)) : 1.f;
 #pragma unroll 1
@@ -571,7 +562,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       ml_s[((uc & 1) * F_WARPS + warp - 4) * 32 + lane] = make_float2(ref, l);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar + 8 * L::B_MLFULL);
-      if (!warp_wait1(bar + 8 * L::B_MLFULL, uc & 1, abort_flag, limit) || !warp_wait1(bar + 8 * L::B_OFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
+      if (!warp_wait_or_abort(bar + 8 * L::B_MLFULL, uc & 1, abort_flag, limit) || !warp_wait_or_abort(bar + 8 * L::B_OFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
       tc_fence_after();
       if (warp_active) {
         constexpr int COPIES = 64 / NC;
@@ -612,7 +603,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         auto meet = [&](uint32_t n) {             // the group's four warps; n: how many times before this
           __syncwarp();
           if (lane == 0) mbar_arrive(bar + 8 * (L::B_SUM + grp));
-          return warp_wait1(bar + 8 * (L::B_SUM + grp), n & 1, abort_flag, limit);
+          return warp_wait_or_abort(bar + 8 * (L::B_SUM + grp), n & 1, abort_flag, limit);
         };
         if (NC < 64) {
           if (wq >= 2) {
