@@ -94,6 +94,9 @@ def _dev(t) -> C.c_void_p:
 def _stream(stream) -> C.c_void_p:
     if stream is None:
         import torch
+        # the current stream's handle without a Stream object around it (0.3 against 3.5 us, once a call)
+        if torch.cuda.is_initialized():
+            return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream if isinstance(stream, int) else stream.cuda_stream)
 
