@@ -65,7 +65,8 @@ enum {
  * With the rotary appends K is rotated in 64 bits, rounded to fp32 and then quantised (no bf16 rounding in between).
  * An element that is not finite (after rotation) is stored as zero and pasta_pool_status reports
  * PASTA_ERR_DEVICE_CHECK: everything in an 8-bit pool is finite.
- * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16);
+ * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
+ * out have to be 16-byte aligned, else INVALID_ARG);
  * pasta_kv_read returns the numbers held, which bf16 represents exactly.  pasta_kv_bytes is n_layers * (n_pages *
  * n_kv_heads * (32 * head_dim + 2) bytes, the scales' part rounded up to 1024).  Requests of up to 128 stacked rows (threads
  * x group) and 4095 streams run on tensor cores, sums in fp32: with head_dim 128 queries and softmax weights enter as two e4m3
@@ -230,8 +231,9 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *pool, int32_t layer_begin, int32_
  * (No counterpart in the paper: models that bound their attention scores.)  From the next call on, every attention of
  * this pool (pasta_decode_attn, pasta_decode_attn_noalloc, pasta_step_device, pasta_step_host and _begin) caps its
  * scores before masking and softmax:  s = q . k * scale  becomes  cap * tanh(s / cap);  lse is that of the capped scores.
- * The tanh is good to cap * 2^-21.  cap = 0 (the state after pasta_pool_create) switches it off, otherwise 1e-3 <= cap <=
- * 1e6 (INVALID_ARG outside, NaN included).  BAD_STATE on a host-only pool.  Launches already enqueued, or captured in a
+ * The capped score is good to 2^-22 of itself where scores stay within the cap, and to 2^-21 of cap where some do not.
+ * cap = 0 (the state after pasta_pool_create) switches it off, otherwise 1e-3 <= cap <= 1e6 (INVALID_ARG outside, NaN
+ * included).  BAD_STATE on a host-only pool.  Launches already enqueued, or captured in a
  * graph, keep the cap they were made with.
  */
 pasta_status_t pasta_set_softcap(pasta_pool_t *pool, float cap);

@@ -41,6 +41,7 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
   if (c.max_requests < 1 || c.max_threads_per_request < 1 || c.max_segments_per_thread < 1) return PASTA_ERR_INVALID_ARG;
   if (c.max_step_queries < 0 || c.max_partial_rows < 0 || c.max_layers_per_launch < 0) return PASTA_ERR_INVALID_ARG;
   const int grid = 160;   // upper bound on CTAs of the tensor-core kernel, for sizing only
+  const int slots = (c.flags & PASTA_FLAG_KV_FP8) && c.head_dim == 64 ? 6 * grid : grid;      // and on pieces that cutting adds
   d->max_queries = c.max_step_queries ? c.max_step_queries
                                       : static_cast<int32_t>(std::min<int64_t>(int64_t(c.max_requests) * 17, 1 << 20));
   // units of the shared tail, at most: its share of all tiles in pieces of kTailTiles, plus one ragged piece per run
@@ -55,7 +56,7 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                                                  : std::min(c.n_layers, 8);
   const int64_t nq = d->max_queries, nr = c.max_requests;
   d->max_words = PH_WORDS + 2 * nq + PQ_WORDS * nq + PT_WORDS * nr + 2 * nr * c.n_kv_heads +
-                 PU_WORDS * (nr * c.n_kv_heads + grid) + 2 * grid + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
+                 PU_WORDS * (nr * c.n_kv_heads + slots) + 2 * slots + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
                  2 * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
                  PU_WORDS * tail_units + 2 * nr * c.n_kv_heads + 8;
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
@@ -148,6 +149,10 @@ pasta_status_t upload(pasta_pool *p, const int32_t *src, size_t words, int32_t *
   return PASTA_OK;
 }
 
+// 8-bit pools: the kernels read and write rows 16 bytes at a time
+bool misaligned(const pasta_pool *p, const void *a, const void *b) {
+  return p->pv.kv8 && ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15);
+}
 // elements between the layers of a dense [layers, n, n_kv_heads, head_dim] array
 int64_t tokens_stride(const pasta_pool *p, int64_t n) { return n * p->cfg.n_kv_heads * p->cfg.head_dim; }
 
@@ -343,7 +348,7 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
     return PASTA_ERR_INVALID_ARG;
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
-  if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
+  if (!k_new || !v_new || misaligned(p, k_new, v_new)) return PASTA_ERR_INVALID_ARG;
   if (p->pv.kv8)
     PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], n_app,
                                  layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, theta,
@@ -448,7 +453,7 @@ pasta_status_t pasta_kv_append(pasta_pool_t *p, int32_t layer_begin, int32_t lay
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers) return PASTA_ERR_INVALID_ARG;
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
-  if (!k_new || !v_new) return PASTA_ERR_INVALID_ARG;
+  if (!k_new || !v_new || misaligned(p, k_new, v_new)) return PASTA_ERR_INVALID_ARG;
   if (p->pv.kv8)
     PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, n_app, layer_begin, layer_count,
                                  tokens_stride(p, n_app), k_new, v_new, 0.0, static_cast<cudaStream_t>(stream)));
@@ -466,7 +471,7 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers) return PASTA_ERR_INVALID_ARG;
   const int32_t n = p->hdr.w[PH_N_QUERIES];
   if (n == 0 || layer_count == 0) return PASTA_OK;
-  if (!q || !out || !(scale >= 0.f)) return PASTA_ERR_INVALID_ARG;
+  if (!q || !out || !(scale >= 0.f) || misaligned(p, q, out)) return PASTA_ERR_INVALID_ARG;
   const float sc = (scale == 0.f ? 1.0f / std::sqrt(static_cast<float>(p->cfg.head_dim)) : scale) * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t q_layer = size_t(n) * p->cfg.n_q_heads * p->cfg.head_dim;
@@ -510,7 +515,7 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
   if (!p) return PASTA_ERR_INVALID_ARG;
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers) return PASTA_ERR_INVALID_ARG;
   if (layer_count > 0 && p->host_only) return PASTA_ERR_BAD_STATE;
-  if (layer_count > 0 && m > 0 && (!k || !v)) return PASTA_ERR_INVALID_ARG;
+  if (layer_count > 0 && m > 0 && (!k || !v || misaligned(p, k, v))) return PASTA_ERR_INVALID_ARG;
   Slot slot{};
   const Request *rq = p->host.request(req);
   const int32_t pos0 = (rq && thread >= 0 && thread < static_cast<int32_t>(rq->threads.size())) ? rq->threads[thread].pos_next : 0;
@@ -677,7 +682,7 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
   const Stream &sm = r->streams[stream_id];
   if (start < 0 || m < 0 || start > sm.len - m) return PASTA_ERR_INVALID_ARG;
   if (m == 0 || layer_count == 0) return PASTA_OK;
-  if (!k_out || !v_out) return PASTA_ERR_INVALID_ARG;
+  if (!k_out || !v_out || misaligned(p, k_out, v_out)) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;
   if (p->pv.kv8) {

@@ -225,7 +225,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-  const float cap = pv.softcap_log2, cap_k2 = kCap ? 2.f * 1.4426950408889634f / cap : 0.f;
+  const float cap = pv.softcap_log2, cap_inv = kCap ? 1.f / cap : 0.f;
   int cur_stream = -1;
   bool ok = true;
   // this lane's addresses inside a block: K rows of its tokens (tile 1 is two rows further than tile 0), V row of the ldmatrix
@@ -268,7 +268,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float &x = sc[pg][j][2 * h + e];
-            if (kCap) x = softcap(x * c, cap, cap_k2) + fev;
+            if (kCap) x = softcap(x * (c * cap_inv), cap) + fev;
             else x = fmaf(x, c, fev);
             if (kMasked && 4 * tq + 2 * j + e >= thr[pg][h]) x = -INFINITY;
             mx = fmaxf(mx, x);

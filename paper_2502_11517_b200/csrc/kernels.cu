@@ -385,7 +385,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
   // stage never waits for global memory
   const int my_pg0 = lane < n_pg ? pg[lane] : 0;
   const int my_pg1 = lane + 32 < n_pg ? pg[lane + 32] : 0;
-  const float cap = pv.softcap_log2, cap_k2 = kCap ? 2.f * 1.4426950408889634f / cap : 0.f;
+  const float cap = pv.softcap_log2, cap_inv = kCap ? 1.f / cap : 0.f;
   __syncwarp();
   auto issue = [&](int i) {
     int page = i < 32 ? __shfl_sync(0xffffffffu, my_pg0, i) : i < 64 ? __shfl_sync(0xffffffffu, my_pg1, i - 32) : pg[i];
@@ -477,7 +477,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     for (int h = 0; h < G; ++h) {
       float sc = acc[h] + __shfl_xor_sync(0xffffffffu, acc[h], 16);
       if (kKv8) sc *= fk;
-      if (kCap) sc = softcap(sc, cap, cap_k2);
+      if (kCap) sc = softcap(sc * cap_inv, cap);
       if (r >= nv) sc = -INFINITY;
       float mx = sc;
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));

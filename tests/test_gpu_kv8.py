@@ -508,3 +508,36 @@ def test_refusals(lib):
             pool.set_softcap(cap)
     pool.set_softcap(30.0); pool.set_softcap(0.0)
     assert pool.status() == 0 and p
+
+
+def test_tensors_that_are_not_aligned_are_refused(lib):
+    """Rows are read and written 16 bytes at a time; nothing is launched, and a refused append takes no slot."""
+    import torch
+    pool = _pool(lib, 4)
+    flat = torch.zeros(20 * 2 * 128 + 8, dtype=torch.bfloat16, device="cuda")
+    good, odd = flat[:20 * 2 * 128].view(1, 20, 2, 128), flat[1:1 + 20 * 2 * 128].view(1, 20, 2, 128)
+    pool.request_begin()
+    for k, v in ((odd, good), (good, odd)):
+        with pytest.raises(lib.PastaError):
+            pool.kv_append_run(0, 0, 20, k, v)
+        with pytest.raises(lib.PastaError):
+            pool.kv_append_run_rope(0, 0, 20, k, v)
+    pool.kv_append_run(0, 0, 20, good, good)
+    assert pool.dump()["requests"][0]["streams"][0]["len"] == 20
+    pool.step_begin([0], [0], [1])
+    one = flat[:256].view(1, 1, 2, 128)
+    q, out = flat[:1024].view(1, 1, 8, 128), torch.empty(1030, device="cuda")
+    for k, v in ((flat[4:260].view(1, 1, 2, 128), one), (one, flat[4:260].view(1, 1, 2, 128))):
+        with pytest.raises(lib.PastaError):
+            pool.kv_append(k, v)
+        with pytest.raises(lib.PastaError):
+            pool.kv_append_rope(k, v, 10000.0)
+    pool.kv_append(one, one)
+    for a, b in ((flat[1:1025].view(1, 1, 8, 128), out[:1024]), (q, out[1:1025])):
+        with pytest.raises(lib.PastaError):
+            pool.decode_attn(a, b)
+        with pytest.raises(lib.PastaError):
+            pool.decode_attn_noalloc(a, b)
+    assert lib.lib().pasta_kv_read_layers(pool._h, 0, 1, 0, 0, 0, 20, lib._dev(odd), lib._dev(good), None) == lib.INVALID_ARG
+    pool.decode_attn(q, out[:1024])
+    assert pool.status() == 0

@@ -86,6 +86,27 @@ def test_caps_and_gains(lib, hq, hkv, d, flags, cap, gain):
     assert pool.status() == 0
 
 
+@pytest.mark.parametrize("hq,hkv,d,flags", [(8, 2, 128, 0), (8, 2, 128, 2), (4, 4, 64, 0), (8, 2, 64, 8), (8, 2, 128, 8), (16, 2, 128, 8 | 2)])
+def test_a_cap_far_above_the_scores(lib, hq, hkv, d, flags):
+    """The largest cap there is leaves ordinary scores as they are: no error that grows with the cap."""
+    import torch
+    pool, model, store, entries, q = _filled(lib, [1, 17, 130, 700], hq, hkv, d, 4.0, flags)
+    out = torch.full((1, len(entries), hq, d), float("nan"), device="cuda"); lse = torch.empty((1, len(entries), hq), device="cuda")
+    pool.set_softcap(1e6)
+    pool.decode_attn(q.cuda(), out, lse)
+    spread = []
+    want, want_lse = decode_attention_capped(model, store, entries, q[0], cap=1e6, spread=spread)
+    qf = q[0].float().numpy()
+    # the capped score is good to 2^-22 of itself: less than the sums' own rounding, which the bound without a cap holds
+    if flags & lib.FLAG_KV_FP8:
+        compare(out[0], lse[0], want, want_lse, qf, store, spread)
+    else:
+        ds = score_bound(qf, store.k, 1 / np.sqrt(d))
+        assert np.abs(out[0].double().cpu().numpy() - want).max() <= (2.0 ** -7 + 2 * ds) * np.abs(store.v).max()
+        assert np.abs(lse[0].double().cpu().numpy() - want_lse).max() <= 2.0 ** -8 + ds + 2.0 ** -21 * np.abs(want_lse).max()
+    assert pool.status() == 0
+
+
 def test_cap_reaches_every_entry_point(lib):
     import torch
     hq, hkv, d = 8, 2, 128
