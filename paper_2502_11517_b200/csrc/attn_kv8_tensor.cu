@@ -27,8 +27,8 @@
 //
 // Warp roles (384 threads): warp 0 producer (4 or 5 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
 // of P.V, two score buffers in TMEM), warps 2-3 build the Q operand, warps 4-7 and 8-11 the two softmax groups.  Every wait is
-// bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.  (All lanes of a warp poll: one lane that polls and tells
-// the others costs 150 cycles more a wait, 178, 218 and 188 us in the cases above.)
+// bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.  (All lanes of a warp poll: with one
+// lane that polls and tells the others the cases above took 178, 218 and 188 us.)
 #include <cuda_fp16.h>
 
 #include "tensor_common.cuh"
