@@ -2,19 +2,24 @@
 //
 //   S[128 x 128] = (Qhi + Qlo)[128 x 128] . Kcodes^T   tcgen05.mma kind::f8f6f4 (N = 128, K = 32), operands from shared memory
 //   p'           = 2^(S * factor * 2^ek + ev - ref)     factor: scale * log2e / the row's own scale; capped if asked for
-//   O[128 x 128] += (P'hi + P'lo)[128 x 128] . Vcodes   tcgen05.mma, P' read from TMEM as the A operand
+//   O[128 x 128] += (P'0 + P'1 + P'2)[128 x 128] . Vcodes   tcgen05.mma, P' read from TMEM as the A operand
 //   l            += p' 2^-ev                            out = O / l
 //
 // K's and V's codes are MMA operands as they lie in the page (128-byte rows with the 128-byte swizzle: K K-major, V MN-major);
 // the page's scales enter where scores are turned into weights: ek in the factor, ev as an addend of the exponent, so that
-// p' is the size of a token's contribution.  Eight bits are too few for queries and weights, so each is a sum of two e4m3
-// terms, hi and the rest: 8 significant bits, as many as bf16 has.  A query row is first scaled by a power of two that
-// brings its largest magnitude to [2^7, 2^8): the split is exact down to 2^-10 of that and off by at most 2^-17 of it below.
-// The reference of a row is set 2^4 below its largest p' and raised when exceeded by more than 2^8, so a weight is off by at
-// most 2^-8 of itself or 2^-14 of the row's largest contribution; l sums unrounded weights in fp32.
+// p' is the size of a token's contribution.  Eight bits are too few for queries and weights, so each is a sum of terms.
+// A query is two e4m3 terms, hi and the rest: 8 significant bits, as many as bf16 has.  A query row is first scaled by a power
+// of two that brings its largest magnitude to [2^7, 2^8): the split is exact down to 2^-10 of that and off by at most 2^-17 of
+// it below.  A weight is three e5m2 terms.  A row may hold one large weight and thousands of small ones that are most of its
+// result, so a weight needs range as well as bits, and e4m3's steps end at 2^-9 (two e4m3 terms lost up to a third of the output
+// row behind one token of 0.9 of the weight and 32768 others).  An e5m2 code is the upper byte of an fp16 number, so the terms
+// are bytes of the fp16 weight, of what is left of it, and of what is left then, rounded (split4): 9 significant bits, with no
+// conversion but the one to fp16; the last rounding goes up in even columns and down in odd ones where it is a tie.
+// The reference of a row is set 2^8 below its largest p' and raised when exceeded by more than 2^15, so a weight is off by at
+// most 2^-8 of itself or 2^-24 of the row's largest contribution; l sums unrounded weights in fp32.
 //
-// What bounds it.  A tile of 128 tokens is 32 KB, 1408 cycles of the measured copy bandwidth per SM.  The MMAs take 1024
-// (twice 512), during which they read shared memory at 64 to 128 bytes per cycle.  The other half is the softmax, where every
+// What bounds it.  A tile of 128 tokens is 32 KB, 1408 cycles of the measured copy bandwidth per SM.  The MMAs take 1280
+// (512 for two terms of queries, 768 for three of weights), during which they read shared memory at 64 to 128 bytes per cycle.  The other half is the softmax, where every
 // instruction of a warp costs the same for 4 rows as for 32 and a column of scores some 11 cycles of its scheduler, so with few
 // rows they are put to use several times (NC columns per thread of the 64 of its half tile):
 //   up to 32 rows  NC = 16: every TMEM quarter (32 lanes) holds a copy of the rows and answers for a quarter of the columns,
@@ -71,10 +76,11 @@ struct F {
   static_assert(SMEM_BYTES <= 232448, "shared memory budget");
 };
 
-// TMEM columns: S[b] at 128 b (group g's half at 64 g, its P in the first 32 of that: two terms of 16), O_g at 256 + 128 g
+// TMEM columns: S[b] at 128 b (group g's half at 64 g, its P in the first 48 of that: three terms of 16), O_g at 256 + 128 g
 constexpr uint32_t COL_S = 0, COL_O = 256;
-// D fp32, A/B e4m3, N = 128; V is MN-major
-constexpr uint32_t IDESC_QK8 = (1u << 4) | ((128u >> 3) << 17), IDESC_PV8 = IDESC_QK8 | (1u << 16);
+// D fp32, N = 128; A and B e4m3, or A e5m2 and B (= V) MN-major
+constexpr uint32_t IDESC_QK8 = (1u << 4) | ((128u >> 3) << 17), IDESC_PV8 = IDESC_QK8 | (1u << 7) | (1u << 16);
+constexpr float P_TOP = 8.f, P_SLACK = 15.f;                    // log2 of a row's largest p' when its reference is set, and at most
 
 __device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -106,8 +112,8 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r) {
 template <int NC>
 __device__ __forceinline__ bool unit_m64(int rows) { return NC == 16 ? rows <= 16 : NC == 64 ? rows <= 64 : false; }
 
-// Four numbers as the e4m3 terms hi and lo (hi + lo = the number to 8 significant bits, in steps of 2^-9 at the least).
-__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t &hi, uint32_t &lo) {
+// Four query elements as the e4m3 terms hi and lo (hi + lo = the number to 8 significant bits, in steps of 2^-9 at the least).
+__device__ __forceinline__ void split_query4(float a, float b, float c, float d, uint32_t &hi, uint32_t &lo) {
   uint16_t h0, h1, l0, l1;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h0) : "f"(b), "f"(a));
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h1) : "f"(d), "f"(c));
@@ -118,6 +124,23 @@ __device__ __forceinline__ void split4(float a, float b, float c, float d, uint3
   asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l1) : "r"(*reinterpret_cast<const uint32_t *>(&g1)));
   hi = h0 | (static_cast<uint32_t>(h1) << 16);
   lo = l0 | (static_cast<uint32_t>(l1) << 16);
+}
+
+// Four weights, 0 <= p <= 2^15, as three e5m2 terms each: off by at most 2^-8 p, or 1.25 * 2^-17 where that is more.
+__device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t *t) {
+  auto rest = [](uint32_t h) {                    // what the upper bytes of two fp16 leave: exact
+    const uint32_t top = h & 0xff00ff00u;
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&top));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  };
+  uint32_t x, y;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(b), "f"(a));
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(d), "f"(c));
+  t[0] = __byte_perm(x, y, 0x7531);
+  x = rest(x);
+  y = rest(y);
+  t[1] = __byte_perm(x, y, 0x7531);
+  t[2] = __byte_perm(rest(x) + 0x007f0080u, rest(y) + 0x007f0080u, 0x7531);
 }
 
 // NC: columns per softmax thread: 16 when every unit of the plan has at most 32 rows, 32 up to 64, 64 otherwise
@@ -308,7 +331,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
               if (!wait_or_abort(bar + 8 * (L::B_PFULL + 2 * b + g), (j >> 1) & 1, abort_flag, limit)) { ok = false; break; }
               tc_fence_after();
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) {   // steps of 32 tokens (two pages), the two terms of the weights
+              for (int ks = 0; ks < 6; ++ks) {   // steps of 32 tokens (two pages), the three terms of the weights
                 const uint32_t term = ks >> 1, kk = ks & 1;
                 mma8_ts(tmem + COL_O + g * 128, tmem + COL_S + b * T_TILE + g * F_HALF + term * 16 + kk * 8,
                         smem_desc(v_addr + (4 * g + 2 * kk) * F_BLOCK, 1024, 2048), IDESC_PV8 | m_bits, (k > 1) || (ks > 0));
@@ -360,8 +383,8 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
 #pragma unroll
         for (int c = 0; c < 8; ++c) {             // val becomes the half row's 64 + 64 bytes
           uint32_t h0, l0, h1, l1;
-          split4(bf16_lo(val[c].x) * f, bf16_hi(val[c].x) * f, bf16_lo(val[c].y) * f, bf16_hi(val[c].y) * f, h0, l0);
-          split4(bf16_lo(val[c].z) * f, bf16_hi(val[c].z) * f, bf16_lo(val[c].w) * f, bf16_hi(val[c].w) * f, h1, l1);
+          split_query4(bf16_lo(val[c].x) * f, bf16_hi(val[c].x) * f, bf16_lo(val[c].y) * f, bf16_hi(val[c].y) * f, h0, l0);
+          split_query4(bf16_lo(val[c].z) * f, bf16_hi(val[c].z) * f, bf16_lo(val[c].w) * f, bf16_hi(val[c].w) * f, h1, l1);
           val[c] = make_uint4(h0, h1, l0, l1);
         }
         if (r0 == 0 && uc > 0 && !warp_wait_or_abort(bar + 8 * L::B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
@@ -498,14 +521,14 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             }
             mt = fmaxf(mt, fmaf(fmaxf(m0, m1), c_pg[pg], static_cast<float>(static_cast<int8_t>(sc2[pg] >> 8))));
           }
-          const bool need = mt > ref + 8.f;       // also true for the first visible tile (ref = -inf)
+          const bool need = mt > ref + P_SLACK;       // also true for the first visible tile (ref = -inf)
           const bool rescale = active && need && l > 0.f;
           if (__any_sync(0xffffffffu, rescale)) {
             // O_g and l are relative to ref: move them to the new reference.  The accumulator is quiet once the P.V of the
             // previous tile has finished, which is what releases that tile's stage.
             if (!warp_wait_or_abort(bar + 8 * (L::B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
             tc_fence_after();
-            const float f = rescale ? fast_exp2(ref - (mt - 4.f)) : 1.f;
+            const float f = rescale ? fast_exp2(ref - (mt - P_TOP)) : 1.f;
 #pragma unroll 1
             for (int h = 0; h < 128; h += 16) {
               uint32_t ov[16];
@@ -519,16 +542,16 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             tmem_st_wait();
             l *= f;
           }
-          if (need) ref = mt - 4.f;
+          if (need) ref = mt - P_TOP;
           const float rf = ref == -INFINITY ? 0.f : ref;
-          // weights as two e4m3 terms, four to a column, where scores were that are in registers by now; l sums them unrounded
+          // weights as three e5m2 terms, four to a column, where scores were that are in registers by now; l sums them unrounded
           // and without V's scale, page by page
 #pragma unroll
           for (int pg = 0; pg < PAGES; ++pg) {
             const int ev = static_cast<int8_t>(sc2[pg] >> 8);
             const float add = static_cast<float>(ev) - rf;
             float ls[2] = {0.f, 0.f};
-            uint32_t hi[4], lo[4];
+            uint32_t t[4][3];
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
               float x0, x1, x2, x3;
@@ -537,17 +560,16 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
               const float p0 = fast_exp2(x0), p1 = fast_exp2(x1), p2 = fast_exp2(x2), p3 = fast_exp2(x3);
               add2(ls[0], ls[1], p0, p1);
               add2(ls[0], ls[1], p2, p3);
-              split4(p0, p1, p2, p3, hi[j >> 2], lo[j >> 2]);
+              split4(p0, p1, p2, p3, t[j >> 2]);
             }
             l = fmaf(ls[0] + ls[1], pow2f(-ev), l);
-            tmem_st4(s_addr + 4 * (page0 + pg), hi[0], hi[1], hi[2], hi[3]);
-            tmem_st4(s_addr + 16 + 4 * (page0 + pg), lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) tmem_st4(s_addr + 16 * k + 4 * (page0 + pg), t[0][k], t[1][k], t[2][k], t[3][k]);
           }
 #pragma unroll
-          for (int pg = PAGES; pg < 4; ++pg) {    // zeros for the columns that other copies answer for
-            tmem_st4(s_addr + 4 * ((page0 + pg) & 3), 0, 0, 0, 0);
-            tmem_st4(s_addr + 16 + 4 * ((page0 + pg) & 3), 0, 0, 0, 0);
-          }
+          for (int pg = PAGES; pg < 4; ++pg)      // zeros for the columns that other copies answer for
+#pragma unroll
+            for (int k = 0; k < 3; ++k) tmem_st4(s_addr + 16 * k + 4 * ((page0 + pg) & 3), 0, 0, 0, 0);
           tmem_st_wait();
         }
         tc_fence_before();
