@@ -268,7 +268,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float &x = sc[pg][j][2 * h + e];
-            if (kCap) x = softcap(x * (c * cap_inv), cap) + fev;
+            if (kCap) x = softcap(x * capped_factor(c, cap_inv), cap) + fev;
             else x = fmaf(x, c, fev);
             if (kMasked && 4 * tq + 2 * j + e >= thr[pg][h]) x = -INFINITY;
             mx = fmaxf(mx, x);

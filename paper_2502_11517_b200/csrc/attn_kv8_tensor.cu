@@ -501,7 +501,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = fmaxf(code_factor(factor, static_cast<int8_t>(sc2[pg] & 0xff)), 1e-37f);   // never 0: it meets -inf
           if (kCap) {
 #pragma unroll
-            for (int j = 0; j < NC; ++j) sc[j] *= c_pg[j >> 4] * a.cap_inv;
+            for (int j = 0; j < NC; ++j) sc[j] *= capped_factor(c_pg[j >> 4], a.cap_inv);
             softcap_columns<NC>(sc, cap, active);
 #pragma unroll
             for (int pg = 0; pg < PAGES; ++pg) c_pg[pg] = 1.f;    // capped scores are in log2 units from here on

@@ -211,5 +211,7 @@ __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) 
 // What a score over codes is multiplied by: the row's factor and K's scale, kept off infinity so that a score of 0 stays 0
 // (8-bit pools; only reached where the scores of anything but 0 leave fp32's range).
 __device__ __forceinline__ float code_factor(float row, int ek) { return fminf(row * pow2f(ek), 1e38f); }
+// The same over the cap, which may be far below 1.
+__device__ __forceinline__ float capped_factor(float c, float cap_inv) { return fminf(c * cap_inv, 1e38f); }
 
 }  // namespace pasta
