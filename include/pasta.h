@@ -233,7 +233,8 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *pool, int32_t layer_begin, int32_
  * (No counterpart in the paper: models that bound their attention scores.)  From the next call on, every attention of
  * this pool (pasta_decode_attn, pasta_decode_attn_noalloc, pasta_step_device, pasta_step_host and _begin) caps its
  * scores before masking and softmax:  s = q . k * scale  becomes  cap * tanh(s / cap);  lse is that of the capped scores.
- * The capped score is good to 2^-22 of itself where scores stay within the cap, and to 2^-21 of cap where some do not.
+ * The capped score is good to 2^-22 of itself where the score is within the cap, and to 2^-21 of cap where it is not; it depends on
+ * no other score.
  * cap = 0 (the state after pasta_pool_create) switches it off, otherwise 1e-3 <= cap <= 1e6 (INVALID_ARG outside, NaN
  * included).  BAD_STATE on a host-only pool.  Launches already enqueued, or captured in a
  * graph, keep the cap they were made with.

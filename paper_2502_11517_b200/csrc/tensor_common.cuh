@@ -173,11 +173,23 @@ __device__ __forceinline__ void mul2(float &x0, float &x1, float a0, float a1, f
       : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
+// {x0, x1} = C tanh({x0, x1}) by softcap's polynomial, for magnitudes up to 1: 9 packed operations
+__device__ __forceinline__ void softcap_poly2(float &x0, float &x1, float C) {
+  float u0, u1, t0 = kTanhPolyTop, t1 = kTanhPolyTop;
+  mul2(u0, u1, x0, x1, x0, x1);
+#define PASTA_STEP(c) horner2(t0, t1, u0, u1, c);
+  PASTA_TANH_POLY(PASTA_STEP)
+#undef PASTA_STEP
+  mul2(t0, t1, t0, t1, x0, x1);
+  mul2(x0, x1, t0, t1, C, C);
+}
 // x[j] = C tanh(x[j]) for the N scores of every thread of a warp; x = score / C, C in log2 units.
 // The form with ex2 and rcp takes two of the special-function unit's slots, 16 cycles per column and warp, on top of the
 // weight's one; the exponential units are what bounds a capped tile.  Scores that a cap is meant for mostly lie well inside
-// it, so a warp whose scores all have |x| <= 1 takes softcap's polynomial without a branch per score, 9 packed operations for
-// two columns (64 responses over a bf16 cache: 162 -> 144 us).  Rows that are not active do not count.
+// it, so a warp whose scores all have |x| <= 1 takes softcap's polynomial alone (64 responses over a bf16 cache: 162 -> 144 us).
+// Otherwise both are worked out and every score takes the one its own size asks for, so that the vote decides on time only: a
+// row's capped scores do not depend on the rows beside it or on what its masked columns hold.  Rows that are not active do not
+// count.
 template <int N>
 __device__ __forceinline__ void softcap_columns(float *x, float C, bool active) {
   float m0 = 0.f, m1 = 0.f;
@@ -188,18 +200,15 @@ __device__ __forceinline__ void softcap_columns(float *x, float C, bool active) 
   }
   if (__any_sync(0xffffffffu, active && fmaxf(m0, m1) > 1.f)) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = softcap_any(x[j], C);
+    for (int j = 0; j < N; j += 2) {
+      float y0 = x[j], y1 = x[j + 1];
+      softcap_poly2(y0, y1, C);
+      x[j] = fabsf(x[j]) > 1.f ? softcap_any(x[j], C) : y0;
+      x[j + 1] = fabsf(x[j + 1]) > 1.f ? softcap_any(x[j + 1], C) : y1;
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < N; j += 2) {
-      float u0, u1, t0 = kTanhPolyTop, t1 = kTanhPolyTop;
-      mul2(u0, u1, x[j], x[j + 1], x[j], x[j + 1]);
-#define PASTA_STEP(c) horner2(t0, t1, u0, u1, c);
-      PASTA_TANH_POLY(PASTA_STEP)
-#undef PASTA_STEP
-      mul2(t0, t1, t0, t1, x[j], x[j + 1]);
-      mul2(x[j], x[j + 1], t0, t1, C, C);
-    }
+    for (int j = 0; j < N; j += 2) softcap_poly2(x[j], x[j + 1], C);
   }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
