@@ -574,6 +574,12 @@ pasta_status_t pasta_step_device(pasta_pool_t *p, int32_t n, const int32_t *req_
                                  float *lse, float scale, void *stream) {
   if (!p) return PASTA_ERR_INVALID_ARG;
   if (p->host_only) return PASTA_ERR_BAD_STATE;
+  // what the append and the attention would refuse is refused before the step reserves its slots
+  if (n > 0) {
+    if (!q || !out || !(scale >= 0.f) || misaligned(p, q, out)) return PASTA_ERR_INVALID_ARG;
+    if ((!n_new || std::any_of(n_new, n_new + n, [](int32_t m) { return m > 0; })) && (!k_new || !v_new || misaligned(p, k_new, v_new)))
+      return PASTA_ERR_INVALID_ARG;
+  }
   pasta_status_t s = pasta_step_begin(p, n, req_ids, thread_ids, n_new, stream);
   if (s != PASTA_OK) return s;
   s = pasta_kv_append(p, 0, p->cfg.n_layers, k_new, v_new, stream);
@@ -600,6 +606,7 @@ pasta_status_t pasta_step_host_begin(pasta_pool_t *p, int32_t n, const int32_t *
   pasta_status_t s = pasta_step_host_bytes(p, n, &need);
   if (s != PASTA_OK) return s;
   if (staging_bytes < need || (reinterpret_cast<uintptr_t>(staging) & 255)) return PASTA_ERR_INVALID_ARG;
+  if (n > 0 && !(scale >= 0.f)) return PASTA_ERR_INVALID_ARG;
   // A staging area of twice (three times) the size holds two (three) steps: the inputs of this step then travel while
   // the kernels of the steps before still read theirs.  Two steps may be in flight in any case (with one slot the
   // copies wait until the step before has left the area), three when the area holds three.
