@@ -186,6 +186,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
   // exactly, down to 2^-22 of the row's largest (and to within 2^-32 of it below that).
   uint32_t qf[KS][4];
   float c1[2];                                                    // scale * log2e / (the row's factor)
+  bool finite[2];
   int vis_row[2], vis[2] = {0, 0};
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -218,6 +219,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
       qf[2 * k + 1][2 + h] = pack_f16(bf16_lo(w[k].w) * f, bf16_hi(w[k].w) * f);
     }
     c1[h] = a.scale_log2 * pow2f(-up);
+    finite[h] = amax < 0x7f80;
   }
 
   float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[NT][4];
@@ -392,7 +394,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
       float lt = l[h];
       lt += __shfl_xor_sync(0xffffffffu, lt, 1);
       lt += __shfl_xor_sync(0xffffffffu, lt, 2);
-      if (tq == 0) ml_s[warp * 16 + r] = make_float2(ref[h], lt);
+      if (tq == 0) ml_s[warp * 16 + r] = make_float2(ref[h], finite[h] ? lt : NAN);
       // 8-byte pieces: piece x of a row goes to x ^ (4 (r % 4)) so that the rows a warp writes at once spread over the banks
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -406,16 +408,22 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
     const int rr = x / PER, d4 = x % PER, t = rr >> 4, r = rr & 15;
     float m_all = -INFINITY;
     for (int p = 0; p < lanes; ++p) m_all = fmaxf(m_all, ml_s[(p * tiles + t) * 16 + r].x);
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l_all = 0.f;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l_all = 0.f, l_plain = 0.f;
     for (int p = 0; p < lanes; ++p) {
       const int w = p * tiles + t;
       const float2 ml = ml_s[w * 16 + r];
+      l_plain += ml.y;
       if (ml.x == -INFINITY) continue;                            // that warp saw nothing of this row
       const float f = fast_exp2(ml.x - m_all);
       const float4 v = *reinterpret_cast<const float4 *>(smem + w * S::O_BYTES + (r * D + (((d4 * 2) ^ ((r & 3) << 2)) << 1)) * 4);
       l_all = fmaf(f, ml.y, l_all);
       acc[0] = fmaf(f, v.x, acc[0]); acc[1] = fmaf(f, v.y, acc[1]);
       acc[2] = fmaf(f, v.z, acc[2]); acc[3] = fmaf(f, v.w, acc[3]);
+    }
+    if (l_plain != l_plain) {
+      m_all = not_a_row().x;
+      l_all = not_a_row().y;
+      acc[0] = acc[1] = acc[2] = acc[3] = NAN;
     }
     const int row = tile0 * 16 + rr;
     if (fin) {

@@ -390,7 +390,9 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         if (r0 == 0 && uc > 0 && !warp_wait_or_abort(bar + 8 * L::B_QFREE, (uc - 1) & 1, abort_flag, limit)) { ok = false; break; }
         // A row's factor is read by the softmax threads of this unit.  The place of unit uc is written again for unit uc + 4,
         // after Q.K^T of unit uc + 3 and hence P.V of unit uc + 2 has been issued: the softmax of unit uc is long over.
-        if (half == 0 && row < rows) factor_s[(uc % F_FACTORS) * 128 + row] = fmaxf(a.scale_log2 * pow2f(-up), 1e-30f);
+        // A row that is not finite says so by its factor: the codes it became are.
+        if (half == 0 && row < rows)
+          factor_s[(uc % F_FACTORS) * 128 + row] = amax >= 0x7f80 ? NAN : fmaxf(a.scale_log2 * pow2f(-up), 1e-30f);
         if (row < copy_rows)
 #pragma unroll
           for (int copy = 0; copy < COPIES; ++copy) {
@@ -581,24 +583,27 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
       // ---- epilogue: a row's accumulators, one per group and copy, leave TMEM brought to one reference and added up, 64
       // columns per group.  The references and sums go through shared memory; so do the accumulators of copies 1 .. (two slots
       // of 8 KB per group, a column per 128 bytes).
-      ml_s[((uc & 1) * F_WARPS + warp - 4) * 32 + lane] = make_float2(ref, l);
+      ml_s[((uc & 1) * F_WARPS + warp - 4) * 32 + lane] = make_float2(ref, factor == factor ? l : NAN);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar + 8 * L::B_MLFULL);
       if (!warp_wait_or_abort(bar + 8 * L::B_MLFULL, uc & 1, abort_flag, limit) || !warp_wait_or_abort(bar + 8 * L::B_OFULL, uc & 1, abort_flag, limit)) { ok = false; break; }
       tc_fence_after();
       if (warp_active) {
         constexpr int COPIES = 64 / NC;
-        float m_all = -INFINITY, l_all = 0.f;
+        float m_all = -INFINITY, l_all = 0.f, l_plain = 0.f;
         float2 part[2 * COPIES];
 #pragma unroll
         for (int i = 0; i < 2 * COPIES; ++i) {
           const int w = (i & 1) * 4 + (NC == 64 ? wq : NC == 32 ? (wq & 1) + (i >> 1) * 2 : i >> 1);
           part[i] = ml_s[((uc & 1) * F_WARPS + w) * 32 + lane];
           if (part[i].y > 0.f) m_all = fmaxf(m_all, part[i].x);
+          l_plain += part[i].y;
         }
 #pragma unroll
         for (int i = 0; i < 2 * COPIES; ++i)
           if (part[i].y > 0.f) l_all = fmaf(part[i].y, fast_exp2(part[i].x - m_all), l_all);
+        const bool spoilt = l_plain != l_plain;
+        if (spoilt) { m_all = not_a_row().x; l_all = not_a_row().y; }
         // what this lane's two accumulators (one per group) are multiplied by; a factor of 0 means that the accumulator of
         // this row is not looked at
         const int mine = NC == 64 ? 0 : NC == 32 ? wq >> 1 : wq;
@@ -611,6 +616,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             f0 = part[2 * i].y > 0.f ? fast_exp2(part[2 * i].x - m_all) * inv : 0.f;
             f1 = part[2 * i + 1].y > 0.f ? fast_exp2(part[2 * i + 1].x - m_all) * inv : 0.f;
           }
+        if (spoilt) f0 = f1 = NAN;
         const uint32_t o_addr = tmem + lane_addr + COL_O + grp * 64;
         float *slots = reinterpret_cast<float *>(sm + L::OFF_SUM + grp * F_SUM_BYTES) + lane;
         auto folded = [&](int h, float *v) {      // 16 of the group's columns, both accumulators

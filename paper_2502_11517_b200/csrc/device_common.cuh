@@ -208,6 +208,9 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
 }
 // 2^e as fp32 for -126 <= e <= 127
 __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }
+// What takes the place of a row's (reference, sum) on 8-bit pools when its query holds a number that is not finite: the merge
+// gives it all the weight, its accumulator is NaN, and so is the output (lse is infinite).
+__device__ __forceinline__ float2 not_a_row() { return make_float2(3.4e38f, INFINITY); }
 // What a score over codes is multiplied by: the row's factor and K's scale, kept off infinity so that a score of 0 stays 0
 // (8-bit pools; only reached where the scores of anything but 0 leave fp32's range).
 __device__ __forceinline__ float code_factor(float row, int ek) { return fminf(row * pow2f(ek), 1e38f); }

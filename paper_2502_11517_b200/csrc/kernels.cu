@@ -399,6 +399,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     }
   };
   for (int i = 0; i < W_STAGES && i < n_pg; ++i) issue(i);
+  uint32_t spoilt = 0;            // 8-bit pools: bit h set, row h holds a number that is not finite
   // the G query rows of this kv head, pre-multiplied by scale * log2(e) (overlaps the first copies)
   {
     const __nv_bfloat162 *qsrc = reinterpret_cast<const __nv_bfloat162 *>(
@@ -408,7 +409,9 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
       const float2 f = __bfloat1622float2(qsrc[i]);
       q_s[2 * i] = f.x * scale_log2;
       q_s[2 * i + 1] = f.y * scale_log2;
+      if (kKv8 && !(fmaxf(fabsf(f.x), fabsf(f.y)) < INFINITY && f.x == f.x && f.y == f.y)) spoilt |= 1u << (2 * i / D);
     }
+    if (kKv8) spoilt = __reduce_or_sync(0xffffffffu, spoilt);
   }
   __syncwarp();
 
@@ -546,6 +549,12 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     lt += __shfl_xor_sync(0xffffffffu, lt, 4);
     lt += __shfl_xor_sync(0xffffffffu, lt, 2);
     lt += __shfl_xor_sync(0xffffffffu, lt, 1);
+    if (kKv8 && (((spoilt >> h) & 1) || lt != lt)) {
+      m[h] = not_a_row().x;
+      lt = not_a_row().y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[h][e] = NAN;
+    }
     if (lane == 0) pv.part_ml[row0 + h] = make_float2(m[h], lt);
     float *dst = pv.part_o + (row0 + h) * D + lane * E;
     if constexpr (E == 4) *reinterpret_cast<float4 *>(dst) = make_float4(o[h][0], o[h][1], o[h][2], o[h][3]);
