@@ -286,9 +286,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
         store_scales(tile, it);
         prod_it = it + (copied - tile);
       }
-      if (!ok)                                    // so that every stage with copies in flight becomes full for the tear-down
-        for (uint32_t i = it; i < prod_it; ++i)
-          if (lane == 0) mbar_arrive(bar + 8 * (L::B_FULL + i % F_STAGES));
+      // (giving up leaves no stage without its second arrival: only the tile whose copies come next is waited for)
     }
   } else if (warp == 1) {
     // ================================================================ MMA issue (one thread)
