@@ -408,7 +408,8 @@ pasta_status_t pasta_debug_set_wait_limit(pasta_pool_t *pool, int64_t cycles);
  * role_mask (1 page producer, 2 MMA issue, 4 query-operand builder, 8 / 16 the two softmax groups) do not start in
  * the launches that follow, the roles that wait for them give up after the pool's wait limit, every CTA drains what
  * it has in flight, frees its tensor memory and returns, and the status word holds PASTA_ERR_TIMEOUT.  The outputs
- * of such a launch are undefined.  Set a short limit first (pasta_debug_set_wait_limit); 0 switches the hook off.
+ * of such a launch are undefined.  In the kernel of 8-bit pools with head_dim 64, 1 holds the copies back and 2 the warps that
+ * make none.  Set a short limit first (pasta_debug_set_wait_limit); 0 switches the hook off.
  */
 pasta_status_t pasta_debug_hold_roles(pasta_pool_t *pool, int32_t role_mask);
 /*

@@ -177,7 +177,9 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
     if (lane < 2) bulk_g2s(ring + s * S::STAGE + lane * S::BLOCK, kv_head + p * page_stride, S::BLOCK, full + 8 * s);
   };
   int issued = 0;
-  if (producer)
+  // test hook: bit 0 keeps the copies back, bit 1 all warps but the producers; those that wait for them run into their limit
+  const bool held = pv.debug_hold & (producer ? 1 : 2);
+  if (producer && !held)
     for (; issued < stages && issued < n_pairs; ++issued) issue(issued, issued, cur_page);
   int cur_sc = load_scale(cur_page), nxt_sc = 0, nxt_meta = -1;
 
@@ -328,7 +330,7 @@ attn_kv8_kernel(PoolView pv, Kv8Args a, const __nv_bfloat16 *__restrict__ q) {
 
   int s = 0, parity = 0;                                          // stage of pair i, and its phase
   int rs = 0, rparity = 0;                                        // stage refilled next, and the phase of its release
-  for (int i = 0; i < n_pairs; ++i) {
+  for (int i = 0; i < n_pairs && (producer || !held); ++i) {
     if (i > 0 && (i & 15) == 0) {
       cur_page = nxt_page; cur_sc = nxt_sc; cur_meta = nxt_meta;
       nxt_page = load_page(list_index((i >> 4) + 1));
