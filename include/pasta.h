@@ -66,6 +66,7 @@ enum {
  * An element that is not finite (after rotation) is stored as zero and pasta_pool_status reports
  * PASTA_ERR_DEVICE_CHECK: everything in an 8-bit pool is finite.
  * A query row with an element that is not finite comes out as NaN, its lse infinite, capped or not; other rows are untouched.
+ * Without a cap so does a row whose scores leave the range of fp32 (the warp-shuffle kernel: of codes, 448 times as large).
  * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
  * out have to be 16-byte aligned, else INVALID_ARG);
  * pasta_kv_read returns the numbers held, which bf16 represents exactly.  pasta_kv_bytes is n_layers * (n_pages *

@@ -80,6 +80,7 @@ struct F {
 constexpr uint32_t COL_S = 0, COL_O = 256;
 // D fp32, N = 128; A and B e4m3, or A e5m2 and B (= V) MN-major
 constexpr uint32_t IDESC_QK8 = (1u << 4) | ((128u >> 3) << 17), IDESC_PV8 = IDESC_QK8 | (1u << 7) | (1u << 16);
+constexpr float FAR_SCORE = 1048576.f;                          // log2 units: fp32 steps are 2^-3 there
 constexpr float P_TOP = 8.f, P_SLACK = 15.f;                    // log2 of a row's largest p' when its reference is set, and at most
 
 __device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -521,14 +522,27 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             }
             mt = fmaxf(mt, fmaf(fmaxf(m0, m1), c_pg[pg], static_cast<float>(static_cast<int8_t>(sc2[pg] >> 8))));
           }
+          // Far from 0 a rounded maximum and an unrounded score may differ by more than the terms have room for: such a row's scores
+          // are rounded as its maximum was, and taken relative to it, before the reference is subtracted.
+          const bool far = !kCap && fabsf(mt) > FAR_SCORE && fabsf(mt) < INFINITY;      // (a cap keeps scores below 2^21)
+          if (!kCap && __any_sync(0xffffffffu, far)) {
+#pragma unroll
+            for (int pg = 0; pg < PAGES; ++pg) {
+#pragma unroll
+              for (int j = 16 * pg; j < 16 * pg + 16; ++j)
+                sc[j] = far ? fmaf(sc[j], c_pg[pg], static_cast<float>(static_cast<int8_t>(sc2[pg] >> 8))) - mt : sc[j];
+              c_pg[pg] = far ? 1.f : c_pg[pg];
+            }
+          }
           const bool need = mt > ref + P_SLACK;       // also true for the first visible tile (ref = -inf)
           const bool rescale = active && need && l > 0.f;
+          const float set = kCap || fabsf(mt) < 32 * FAR_SCORE ? mt - P_TOP : mt;      // exact: steps beyond are larger than P_TOP / 2
           if (__any_sync(0xffffffffu, rescale)) {
             // O_g and l are relative to ref: move them to the new reference.  The accumulator is quiet once the P.V of the
             // previous tile has finished, which is what releases that tile's stage.
             if (!warp_wait_or_abort(bar + 8 * (L::B_EMPTY + (it - 1) % F_STAGES), ((it - 1) / F_STAGES) & 1, abort_flag, limit)) { ok = false; break; }
             tc_fence_after();
-            const float f = rescale ? fast_exp2(ref - (mt - P_TOP)) : 1.f;
+            const float f = rescale ? fast_exp2(ref - set) : 1.f;
 #pragma unroll 1
             for (int h = 0; h < 128; h += 16) {
               uint32_t ov[16];
@@ -542,14 +556,14 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
             tmem_st_wait();
             l *= f;
           }
-          if (need) ref = mt - P_TOP;
-          const float rf = ref == -INFINITY ? 0.f : ref;
+          if (need) ref = set;
+          const float rf = ref == -INFINITY ? 0.f : ref == INFINITY ? NAN : ref;      // a score beyond fp32 spoils its row
           // weights as three e5m2 terms, four to a column, where scores were that are in registers by now; l sums them unrounded
           // and without V's scale, page by page
 #pragma unroll
           for (int pg = 0; pg < PAGES; ++pg) {
             const int ev = static_cast<int8_t>(sc2[pg] >> 8);
-            const float add = static_cast<float>(ev) - rf;
+            const float add = (far ? mt : static_cast<float>(ev)) - rf;
             float ls[2] = {0.f, 0.f};
             uint32_t t[4][3];
 #pragma unroll
