@@ -11,9 +11,9 @@
 // become fp16 exactly (cvt e4m3x2, 2 cycles per warp and scheduler), Q.K^T and P.V are fp16 mma.sync with fp32 sums (8 cycles
 // per m16n8k16): 32 cycles of matrix pipe per page and 16 rows, and several times that of issue, which is what is left:
 // 32 requests of 8 to 20 rows, 2 layers, 75 MB: 31.9 us, 38 % of the copy bandwidth, against 12.2 us for the bytes.
-// (mma.sync because a row of codes is 64 bytes and the steps have few rows: the e4m3 form of mma.sync is slower, 850
-// instructions per page and 16 rows were counted with it at head_dim 128 against 300 here; tcgen05 at head_dim 128 comes out
-// even with this kernel below 64 rows and ahead above, see attn_kv8_tensor.cu.)
+// (mma.sync because a row of codes is 64 bytes and the steps have few rows; a tcgen05 form was built at head_dim 128 only, where
+// this design took 194, 176 and 449 us for the three cases of attn_kv8_tensor.cu, where that takes 180, 170 and 230.  The e4m3 form of
+// mma.sync is slower: 850 instructions per page and 16 rows were counted with it at head_dim 128 against 300 here.)
 //
 // One CTA of W warps per (unit, layer, group of row tiles).  A row tile is 16 stacked rows; the group's `tiles` row tiles are
 // spread over the warps, warp w = lane_of_pages * tiles + tile, so that W / tiles pairs of pages are worked on at a time and

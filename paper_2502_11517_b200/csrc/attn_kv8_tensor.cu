@@ -19,21 +19,23 @@
 // most 2^-8 of itself or 2^-24 of the row's largest contribution; l sums unrounded weights in fp32.
 //
 // What bounds it.  A tile of 128 tokens is 32 KB, 1408 cycles of the measured copy bandwidth per SM.  The MMAs take 1280
-// (512 for two terms of queries, 768 for three of weights), during which they read shared memory at 64 to 128 bytes per cycle.  The other half is the softmax, where every
-// instruction of a warp costs the same for 4 rows as for 32 and a column of scores some 11 cycles of its scheduler, so with few
-// rows they are put to use several times (NC columns per thread of the 64 of its half tile):
+// (512 for two terms of queries, 768 for three of weights), during which they read shared memory at 64 to 128 bytes per cycle.
+// The other half is the softmax, where every instruction of a warp costs the same for 4 rows as for 32 and a column of scores some
+// 12 cycles of its scheduler, so with few rows they are put to use several times (NC columns per thread of the 64 of its half
+// tile):
 //   up to 32 rows  NC = 16: every TMEM quarter (32 lanes) holds a copy of the rows and answers for a quarter of the columns,
 //   up to 64 rows  NC = 32: every pair of quarters holds a copy and answers for half of them,
 //   more           NC = 64: one copy.
 // A copy's weights for columns it does not answer for are zeros.  The two halves of a tile belong to two softmax groups, as in
 // attn_tensor.cu; each copy of a row in each group has its own reference, sum and accumulator row, so nothing is exchanged
 // between the softmax warps until the unit's epilogue.  Measured (us; one softmax thread per row and half tile throughout in
-// brackets): 64 requests of 4 to 36 rows 165 (197), 68 rows behind long prefixes 211 (219), short capped responses 163 (231).
+// brackets): 64 requests of 4 to 36 rows 180 (200), short capped responses 170 (229); 68 rows behind long prefixes 230.  The bf16
+// pool takes 183, 189 and 234 for the same steps: the codes halve the bytes, and the instructions that replace them take as long.
 //
 // Warp roles (384 threads): warp 0 producer (4 or 5 stages of one tile), warp 1 MMA issue (one thread; Q.K^T runs one tile ahead
 // of P.V, two score buffers in TMEM), warps 2-3 build the Q operand, warps 4-7 and 8-11 the two softmax groups.  Every wait is
 // bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.  (All lanes of a warp poll: with one
-// lane that polls and tells the others the cases above took 178, 218 and 188 us.)
+// lane that polls and tells the others the three cases took 8, 15 and 3 % longer.)
 #include <cuda_fp16.h>
 
 #include "tensor_common.cuh"
@@ -525,7 +527,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           // Far from 0 a rounded maximum and an unrounded score may differ by more than the terms have room for: such a row's scores
           // are rounded as its maximum was, and taken relative to it, before the reference is subtracted.
           const bool far = !kCap && fabsf(mt) > FAR_SCORE && fabsf(mt) < INFINITY;      // (a cap keeps scores below 2^21)
-          if (!kCap && __any_sync(0xffffffffu, far)) {
+          if (!kCap && __any_sync(0xffffffffu, active && far)) {
 #pragma unroll
             for (int pg = 0; pg < PAGES; ++pg) {
 #pragma unroll

@@ -186,7 +186,7 @@ __device__ __forceinline__ void softcap_poly2(float &x0, float &x1, float C) {
 // x[j] = C tanh(x[j]) for the N scores of every thread of a warp; x = score / C, C in log2 units.
 // The form with ex2 and rcp takes two of the special-function unit's slots, 16 cycles per column and warp, on top of the
 // weight's one; the exponential units are what bounds a capped tile.  Scores that a cap is meant for mostly lie well inside
-// it, so a warp whose scores all have |x| <= 1 takes softcap's polynomial alone (64 responses over a bf16 cache: 162 -> 144 us).
+// it, so a warp whose scores all have |x| <= 1 takes softcap's polynomial alone (64 responses over a bf16 cache: 162 -> 148 us).
 // Otherwise both are worked out and every score takes the one its own size asks for, so that the vote decides on time only: a
 // row's capped scores do not depend on the rows beside it or on what its masked columns hold.  Rows that are not active do not
 // count.
