@@ -44,13 +44,13 @@ PROFILE_STEPS = 24
 # DRAM bytes (read + write) of one launch of the tensor-core kernel from the ncu captures summarised under profiles/,
 # as a ratio to the launch's algorithmic bytes (reads grow with the bytes read; the partial-row writes are added as
 # they are).  Valid for the kernel source it was captured from only: its hash is checked at run time.
-NCU_TRAFFIC = {"attn_tensor_sha256_16": "843a495e04b30a5e", "read_ratio": 1.0135, "write_bytes": 4.3e6}
+NCU_TRAFFIC = {"attn_tensor_sha256_16": "96fe8d1ec61dbc92", "read_ratio": 1.0135, "write_bytes": 4.3e6}
 
 
 def kernel_source_hash() -> str:
     import hashlib
     h = hashlib.sha256()
-    for name in ("attn_tensor.cu", "device_common.cuh", "pasta_plan.h"):
+    for name in ("attn_tensor.cu", "tensor_common.cuh", "device_common.cuh", "pasta_plan.h"):
         with open(os.path.join(ROOT, "paper_2502_11517_b200", "csrc", name), "rb") as f:
             h.update(f.read())
     return h.hexdigest()[:16]
