@@ -74,8 +74,9 @@ enum {
  * x group) and 4095 streams run on tensor cores, sums in fp32.  With head_dim 128 a query enters as two e4m3 terms (8 significant
  * bits; an element is off by at most 2^-17 of its row's largest) and a softmax weight as three e5m2 terms, off by at most 2^-8
  * of itself or, where that is more, by 2^-24 of the row's largest contribution (weight times the scale of its page's V, over
- * the scale of its own).  With head_dim 64 queries enter as fp16 of rows scaled by a power of two and weights as fp16: 2^-11 of
- * itself or 2^-24 of the same.  The weights' sum is not rounded, so n small weights behind a large one are off by n * 2^-24 of that
+ * the scale of its own; 2^-16 of it in rows whose scores reach 2^24, where neighbours are whole numbers apart).  With head_dim 64
+ * queries enter as fp16 of rows scaled by a power of two and weights as fp16: 2^-11 of itself or 2^-24 of the same.  The
+ * weights' sum is not rounded, so n small weights behind a large one are off by n * 2^-24 of that
  * one at most.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the warp-shuffle kernel, which rounds no weight.
  */
 

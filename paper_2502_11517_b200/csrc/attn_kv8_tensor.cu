@@ -129,7 +129,8 @@ __device__ __forceinline__ void split_query4(float a, float b, float c, float d,
   lo = l0 | (static_cast<uint32_t>(l1) << 16);
 }
 
-// Four weights, 0 <= p <= 2^15, as three e5m2 terms each: off by at most 2^-8 p, or 1.25 * 2^-17 where that is more.
+// Four weights, 0 <= p <= 2^15, as three e5m2 terms each: off by at most 2^-8 p, or 1.25 * 2^-17 where that is more
+// (over all fp16 numbers; a NaN stays one).
 __device__ __forceinline__ void split4(float a, float b, float c, float d, uint32_t *t) {
   auto rest = [](uint32_t h) {                    // what the upper bytes of two fp16 leave: exact
     const uint32_t top = h & 0xff00ff00u;
@@ -538,7 +539,7 @@ attn_kv8_tensor_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restric
           }
           const bool need = mt > ref + P_SLACK;       // also true for the first visible tile (ref = -inf)
           const bool rescale = active && need && l > 0.f;
-          const float set = kCap || fabsf(mt) < 32 * FAR_SCORE ? mt - P_TOP : mt;      // exact: steps beyond are larger than P_TOP / 2
+          const float set = kCap || fabsf(mt) < 32 * FAR_SCORE ? mt - P_TOP : mt;      // exact: beyond, fp32 steps are 4 and more
           if (__any_sync(0xffffffffu, rescale)) {
             // O_g and l are relative to ref: move them to the new reference.  The accumulator is quiet once the P.V of the
             // previous tile has finished, which is what releases that tile's stage.
