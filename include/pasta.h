@@ -50,7 +50,9 @@ enum {
   PASTA_FLAG_OUT_BF16 = 4,       /* `out` of pasta_decode_attn, pasta_step_device and pasta_step_host is bf16 instead of
                                     fp32 (same shape; the sums stay fp32, one rounding at the end; lse stays fp32).
                                     pasta_decode_attn_noalloc writes fp32 only and returns BAD_STATE on such a pool. */
-  PASTA_FLAG_KV_FP8 = 8          /* the pool holds K and V in 8 bits (see "8-bit pools" below): half the bytes per token */
+  PASTA_FLAG_KV_FP8 = 8,         /* the pool holds K and V in 8 bits (see "8-bit pools" below): half the bytes per token */
+  PASTA_FLAG_KV_INT4 = 16        /* the pool holds K and V in 4 bits (see "4-bit pools" below): 9/32 of the bytes per token.
+                                    INVALID_ARG together with PASTA_FLAG_KV_FP8. */
 };
 
 /*
@@ -79,6 +81,51 @@ enum {
  * weights' sum is not rounded, so n small weights behind a large one are off by n * 2^-24 of that
  * one at most.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the warp-shuffle kernel, which rounds no weight.
  */
+
+/*
+ * 4-bit pools (no counterpart in the paper; PASTA_FLAG_KV_INT4).  32 neighbouring elements of one token's K, or V, of one kv head
+ * are held as whole numbers n = -7 ... 7 times one scale s:
+ *   s = the smallest number of five significant bits with amax <= 7 s over the 32 elements, kept within [2^-110, 31 * 2^106],
+ *   n = the whole number nearest to x / s (ties to the even one, at most 7 in magnitude).
+ * So an element within that range is off by at most s / 2, which is less than 1/13 of the largest of the 32.  A token's codes
+ * depend on that token alone: what the pool holds does not depend on how tokens were grouped into calls, nothing is rounded
+ * again when later tokens arrive, and what pasta_kv_read returns (n s, which bf16 represents exactly) is held unchanged when it
+ * is appended again.  With the rotary appends K is rotated in 64 bits, rounded to fp32 and then quantised.
+ * An element that is not finite is stored as zero (with a rotary append both elements of a rotated pair), and pasta_pool_status reports
+ * PASTA_ERR_DEVICE_CHECK: everything in a 4-bit pool is finite.
+ * A query row with an element that is not finite, or whose scores leave the range of fp32, comes out as NaN, its lse not finite,
+ * capped or not; other rows are untouched.
+ * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
+ * out have to be 16-byte aligned, else INVALID_ARG).  pasta_kv_bytes is n_layers * n_pages * n_kv_heads * 18 * head_dim.
+ * Requests of up to 128 stacked rows (threads x group) and 4095 streams run on tensor cores, with either head_dim: queries,
+ * and K and V as held, enter unrounded, a softmax weight as bf16 (2^-8 of itself; the weights' sum is that of the rounded ones), sums
+ * are fp32.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the warp-shuffle kernel, which rounds no weight.
+ */
+
+/*
+ * Forms of the rotary embedding (no counterpart in the paper beyond its position ids): which elements of a head form the pairs that
+ * are turned, and by what angle.  Pair i of the first rotary_dim elements turns by position * f_i, f_i = theta^(-2i/rotary_dim)
+ * before scaling; the other elements stay as they are.
+ *   layout       HALF: element i with element i + rotary_dim/2;  INTERLEAVED: element 2i with element 2i + 1
+ *   scaling      NONE; LINEAR: f_i / factor;  BASE: theta becomes theta * factor^(rotary_dim / (rotary_dim - 2));
+ *                WAVELENGTH: with turns = original_length * f_i / 2 pi, f_i is kept where turns > high, divided by factor where
+ *                turns < low, and in between  f_i (t + (1 - t) / factor), t = (turns - low) / (high - low);
+ *                RAMP: with p(turns) = rotary_dim ln(original_length / (2 pi turns)) / (2 ln theta), the pairs up to
+ *                first = max(0, floor p(high)) keep f_i, those from last = min(rotary_dim - 1, ceil p(low)) on take f_i / factor,
+ *                and in between it goes linearly from one to the other (last = first + 0.001 when last <= first)
+ *   magnitude    what rotated elements are also multiplied by; 0 means 0.1 ln(factor) + 1 with RAMP and 1 otherwise
+ * Limits: rotary_dim a multiple of 16 up to head_dim (0 = head_dim); factor in [1, 1e6]; magnitude 0 or in [1e-3, 1e3]; with WAVELENGTH
+ * and RAMP original_length in [1, 1e9] and 0 < low < high <= 1e6.  What a scaling does not use is not looked at.
+ */
+enum { PASTA_ROPE_HALF = 0, PASTA_ROPE_INTERLEAVED = 1 };
+enum {
+  PASTA_ROPE_SCALE_NONE = 0, PASTA_ROPE_SCALE_LINEAR = 1, PASTA_ROPE_SCALE_BASE = 2, PASTA_ROPE_SCALE_WAVELENGTH = 3,
+  PASTA_ROPE_SCALE_RAMP = 4
+};
+typedef struct {
+  int32_t layout, rotary_dim, scaling, reserved;      /* reserved: 0 */
+  double factor, original_length, low, high, magnitude;
+} pasta_rope_form_t;
 
 /* thread states reported by pasta_pool_dump */
 enum { PASTA_THREAD_ACTIVE = 0, PASTA_THREAD_FINISHED = 1, PASTA_THREAD_MERGED = 2 };
@@ -205,6 +252,21 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *pool, int32_t layer_begin, int
                                     const void *k_new, const void *v_new, float theta, void *stream);
 /* Rotates the step's queries in place by the same rule: q device bf16 [layer_count, n, n_q_heads, head_dim]. */
 pasta_status_t pasta_rope_queries(pasta_pool_t *pool, int32_t layer_count, void *q, float theta, void *stream);
+/* The same into another array of that shape (q_out == q rotates in place; arrays that overlap otherwise are not supported).  q and
+ * q_out 16-byte aligned (INVALID_ARG). */
+pasta_status_t pasta_rope_queries_to(pasta_pool_t *pool, int32_t layer_count, const void *q, void *q_out, float theta, void *stream);
+
+/*
+ * From the next call on the rotary calls of this pool (pasta_kv_append_rope, pasta_kv_append_run_rope, pasta_rope_queries, _to) rotate in
+ * the given form, on every kind of pool; NULL restores the form above (HALF, whole head, no scaling), which is the state after
+ * pasta_pool_create.  With another form k, v and q have to be 16-byte aligned on a bf16 pool too (INVALID_ARG).  Angles are 64-bit
+ * products of the position and f_i; sines, cosines and the rotation are evaluated in 64 bits.  Launches already enqueued, or
+ * captured in a graph, keep their form.  Host state only, so it works on a host-only pool.
+ */
+pasta_status_t pasta_set_rope(pasta_pool_t *pool, const pasta_rope_form_t *form);
+/* The frequencies f_i that the rotary calls use with this theta, one per pair (rotary_dim / 2 of them, *count), and the magnitude.
+ * Host arrays; CAPACITY when f is too short (f may be NULL with capacity 0 and count then receives the number: PASTA_OK). */
+pasta_status_t pasta_rope_frequencies(pasta_pool_t *pool, float theta, double *f, int32_t capacity, int32_t *count, double *magnitude);
 
 /*
  * Copies the new tokens' K and V into their reserved slots for layers

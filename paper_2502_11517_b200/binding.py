@@ -15,7 +15,9 @@ import numpy as np
 from .build import LIB
 
 OK, INVALID_ARG, OUT_OF_PAGES, BAD_STATE, CAPACITY, CUDA, DEVICE_CHECK, TIMEOUT = range(8)
-FLAG_HOST_ONLY, FLAG_NO_TENSOR_PATH, FLAG_OUT_BF16, FLAG_KV_FP8 = 1, 2, 4, 8
+FLAG_HOST_ONLY, FLAG_NO_TENSOR_PATH, FLAG_OUT_BF16, FLAG_KV_FP8, FLAG_KV_INT4 = 1, 2, 4, 8, 16
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "wavelength": 3, "ramp": 4}
 _NAMES = ["OK", "INVALID_ARG", "OUT_OF_PAGES", "BAD_STATE", "CAPACITY", "CUDA", "DEVICE_CHECK", "TIMEOUT"]
 
 EXPORTS = [
@@ -31,6 +33,7 @@ EXPORTS = [
     "pasta_debug_stream_read", "pasta_step_host_begin", "pasta_step_host_wait",
     "pasta_dense_mask_scratch_bytes", "pasta_dense_append", "pasta_dense_mask_attn", "pasta_debug_set_tail",
     "pasta_debug_set_launch_overlap", "pasta_set_softcap", "pasta_kv_read_layers",
+    "pasta_set_rope", "pasta_rope_frequencies", "pasta_rope_queries_to",
 ]
 
 
@@ -53,6 +56,12 @@ class Config(C.Structure):
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("free_order", C.POINTER(C.c_int32)),
     ]
+
+
+class RopeForm(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rotary_dim", C.c_int32), ("scaling", C.c_int32), ("reserved", C.c_int32),
+                ("factor", C.c_double), ("original_length", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("magnitude", C.c_double)]
 
 
 _lib = None
@@ -212,9 +221,29 @@ class Pool:
         _check(lib().pasta_kv_append_rope(self._h, layer_begin, cnt, _dev(k_new), _dev(v_new), C.c_float(theta),
                                           _stream(stream)), "pasta_kv_append_rope")
 
-    def rope_queries(self, q, theta: float = 10000.0, layer_count: Optional[int] = None, stream=None) -> None:
+    def rope_queries(self, q, theta: float = 10000.0, layer_count: Optional[int] = None, stream=None, out=None) -> None:
+        """Rotates the step's queries by their positions, in place or into `out`."""
         cnt = self.n_layers if layer_count is None else layer_count
-        _check(lib().pasta_rope_queries(self._h, cnt, _dev(q), C.c_float(theta), _stream(stream)), "pasta_rope_queries")
+        if out is None:
+            _check(lib().pasta_rope_queries(self._h, cnt, _dev(q), C.c_float(theta), _stream(stream)), "pasta_rope_queries")
+        else:
+            _check(lib().pasta_rope_queries_to(self._h, cnt, _dev(q), _dev(out), C.c_float(theta), _stream(stream)),
+                   "pasta_rope_queries_to")
+
+    def set_rope(self, layout: str = "half", rotary_dim: int = 0, scaling: str = "none", factor: float = 1.0,
+                 original_length: float = 0.0, low: float = 1.0, high: float = 4.0, magnitude: float = 0.0) -> None:
+        """The form of this pool's rotary calls from the next one on (see pasta_rope_form_t); no argument: the usual one."""
+        form = RopeForm(ROPE_LAYOUTS.get(layout, -1), rotary_dim, ROPE_SCALINGS.get(scaling, -1), 0, factor, original_length, low,
+                        high, magnitude)
+        _check(lib().pasta_set_rope(self._h, C.byref(form)), "pasta_set_rope")
+
+    def rope_frequencies(self, theta: float = 10000.0):
+        """(frequency of every rotated pair, what rotated elements are multiplied by) in the pool's form."""
+        f = np.empty(self.head_dim // 2, dtype=np.float64)
+        n, size = C.c_int32(), C.c_double()
+        _check(lib().pasta_rope_frequencies(self._h, C.c_float(theta), _ptr(f), len(f), C.byref(n), C.byref(size)),
+               "pasta_rope_frequencies")
+        return f[:n.value].copy(), size.value
 
     def kv_append_run_rope(self, req: int, thread: int, m: int, k, v, theta: float = 10000.0, layer_begin: int = 0,
                            layer_count: Optional[int] = None, stream=None) -> None:

@@ -10,8 +10,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpasta.so")
-SOURCES = ["pool.cpp", "plan.cpp", "kernels.cu", "attn_tensor.cu", "kv8.cu", "attn_kv8.cu", "attn_kv8_tensor.cu", "api.cu", "noalloc.cu", "dense_mask.cu"]
-HEADERS = ["pool.hpp", "plan.hpp", "pasta_plan.h", "device_common.cuh", "tensor_common.cuh", "kernels.hpp",
+SOURCES = ["pool.cpp", "plan.cpp", "kernels.cu", "attn_tensor.cu", "kv8.cu", "attn_kv8.cu", "attn_kv8_tensor.cu", "kv4.cu", "rope.cu", "api.cu", "noalloc.cu", "dense_mask.cu"]
+HEADERS = ["pool.hpp", "plan.hpp", "pasta_plan.h", "device_common.cuh", "tensor_common.cuh", "page_run.cuh", "rope_form.cuh", "kernels.hpp",
            os.path.join("..", "..", "include", "pasta.h")]
 
 
@@ -49,7 +49,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     stamp = source_hash()
-    cmd = [_nvcc()] + FLAGS + ["-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
+    cmd = [_nvcc(), "--threads", "0"] + FLAGS + ["-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     if os.path.exists(STAMP):

@@ -9,6 +9,7 @@
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "pool.hpp"
+#include "rope_form.cuh"
 
 using namespace pasta;
 
@@ -60,8 +61,10 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                  2 * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
                  PU_WORDS * tail_units + 2 * nr * c.n_kv_heads + 8;
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
-  const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0;
-  d->scale_off = size_t(c.n_pages) * c.n_kv_heads * (kv8 ? kv8_block_bytes(c.head_dim) : kv_block_bytes(c.head_dim));
+  const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0, kv4 = (c.flags & PASTA_FLAG_KV_INT4) != 0;
+  if (kv8 && kv4) return PASTA_ERR_INVALID_ARG;
+  d->scale_off = size_t(c.n_pages) * c.n_kv_heads *
+                 (kv8 ? kv8_block_bytes(c.head_dim) : kv4 ? kv4_block_bytes(c.head_dim) : kv_block_bytes(c.head_dim));
   d->layer_stride = d->scale_off + (kv8 ? align_up(size_t(c.n_pages) * c.n_kv_heads * 2, 1024) : 0);
   d->kv_bytes = d->layer_stride * c.n_layers;
   size_t off = 0;
@@ -103,6 +106,9 @@ struct pasta_pool {
   cudaEvent_t work_mark[2] = {nullptr, nullptr};    // recorded on the caller's stream at the start of step i (slot i % 2)
   int64_t step_index = 0;
   int32_t tail_percent = kTailPercent, tail_tiles = kTailTiles;
+  pasta_rope_form_t rope_form{};      // all zero: the form of a new pool
+  RopeForm rope_table{};              // of rope_form and rope_theta
+  double rope_theta = 0;              // 0: no table yet
   // pasta_step_host_begin / _wait: at most two steps in flight; their copies run on streams of the pool
   cudaStream_t d2h_stream = nullptr;
   // pasta_step_host_begin / _wait: up to kHostInflight steps between begin and wait; step i uses event set i % kHostInflight
@@ -149,9 +155,54 @@ pasta_status_t upload(pasta_pool *p, const int32_t *src, size_t words, int32_t *
   return PASTA_OK;
 }
 
-// 8-bit pools: the kernels read and write rows 16 bytes at a time
-bool misaligned(const pasta_pool *p, const void *a, const void *b) {
-  return p->pv.kv8 && ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15);
+bool odd_address(const void *a, const void *b) { return (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15; }
+// 8-bit and 4-bit pools: the kernels read and write rows 16 bytes at a time
+bool misaligned(const pasta_pool *p, const void *a, const void *b) { return (p->pv.kv8 || p->pv.kv4) && odd_address(a, b); }
+
+bool usual_rope(const pasta_pool *p) {
+  const pasta_rope_form_t &f = p->rope_form;
+  return f.layout == PASTA_ROPE_HALF && f.rotary_dim == 0 && f.scaling == PASTA_ROPE_SCALE_NONE && f.magnitude == 0;
+}
+
+// The pool's form as a table for this theta, worked out again only when either changes.
+const RopeForm *rope_table(pasta_pool *p, double theta) {
+  RopeForm &t = p->rope_table;
+  if (p->rope_theta == theta) return &t;
+  const pasta_rope_form_t &f = p->rope_form;
+  const int R = f.rotary_dim ? f.rotary_dim : p->cfg.head_dim;
+  const double turn = 6.283185307179586;
+  const double log2_theta = std::log2(theta) + (f.scaling == PASTA_ROPE_SCALE_BASE ? std::log2(f.factor) * R / (R - 2) : 0.0);
+  t = RopeForm{};
+  t.slots = R / 16;
+  t.interleaved = f.layout == PASTA_ROPE_INTERLEAVED ? 1 : 0;
+  t.size = f.magnitude > 0 ? f.magnitude : f.scaling == PASTA_ROPE_SCALE_RAMP ? 0.1 * std::log(f.factor) + 1.0 : 1.0;
+  double first = 0, last = 0;
+  if (f.scaling == PASTA_ROPE_SCALE_RAMP) {
+    auto pair = [&](double turns) { return R * std::log(f.original_length / (turn * turns)) / (2 * std::log(theta)); };
+    first = std::max(0.0, std::floor(pair(f.high)));
+    last = std::min(R - 1.0, std::ceil(pair(f.low)));
+    if (last <= first) last = first + 0.001;
+  }
+  for (int i = 0; i < R / 2; ++i) {
+    double x = std::exp2(-2.0 * i / R * log2_theta), keep = 1.0;      // keep: the share of the unstretched frequency
+    if (f.scaling == PASTA_ROPE_SCALE_LINEAR) keep = 0.0;
+    if (f.scaling == PASTA_ROPE_SCALE_WAVELENGTH) keep = (f.original_length * x / turn - f.low) / (f.high - f.low);
+    if (f.scaling == PASTA_ROPE_SCALE_RAMP) keep = 1.0 - (i - first) / (last - first);
+    keep = std::min(1.0, std::max(0.0, keep));
+    if (keep < 1.0) x = x * keep + x / f.factor * (1.0 - keep);
+    t.f[i] = x;
+    t.c1[i] = std::cos(x);
+    t.s1[i] = std::sin(x);
+  }
+  p->rope_theta = theta;
+  return &t;
+}
+
+// the layers' new tokens into their slots on an 8-bit or a 4-bit pool (form null: no rotation)
+cudaError_t append_codes(pasta_pool *p, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin, int32_t layer_count,
+                         int64_t in_layer_stride, const void *k, const void *v, const RopeForm *form, cudaStream_t st) {
+  const auto launch = p->pv.kv8 ? launch_kv8_append : launch_kv4_append;
+  return launch(p->pv, slots, pos, n_tok, layer_begin, layer_count, in_layer_stride, k, v, form, st);
 }
 // elements between the layers of a dense [layers, n, n_kv_heads, head_dim] array
 int64_t tokens_stride(const pasta_pool *p, int64_t n) { return n * p->cfg.n_kv_heads * p->cfg.head_dim; }
@@ -165,7 +216,7 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.max_rows = p->d.max_rows;
   l.max_words = p->d.max_words;
   l.grid = p->sm_count;
-  l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & PASTA_FLAG_KV_FP8)) &&
+  l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & PASTA_FLAG_KV_FP8)) && !(p->cfg.flags & PASTA_FLAG_KV_INT4) &&
                   !(p->cfg.flags & PASTA_FLAG_NO_TENSOR_PATH) && tensor_path_available();
   l.tail_percent = p->tail_percent;
   if ((p->cfg.flags & PASTA_FLAG_KV_FP8) && p->cfg.head_dim == 64) {      // that kernel runs one CTA per unit, six to an SM
@@ -280,6 +331,7 @@ pasta_status_t pasta_pool_create(const pasta_pool_config_t *cfg, pasta_pool_t **
     p->pv.softcap_log2 = 0.f;
     p->pv.kv8 = (cfg->flags & PASTA_FLAG_KV_FP8) ? 1 : 0;
     p->pv.scale_off = static_cast<int64_t>(d.scale_off);
+    p->pv.kv4 = (cfg->flags & PASTA_FLAG_KV_INT4) ? 1 : 0;
   }
   *out = p;
   return PASTA_OK;
@@ -349,27 +401,77 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new || misaligned(p, k_new, v_new)) return PASTA_ERR_INVALID_ARG;
-  if (p->pv.kv8)
-    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], n_app,
-                                 layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, theta,
-                                 static_cast<cudaStream_t>(stream)));
+  if (!usual_rope(p) && odd_address(k_new, v_new)) return PASTA_ERR_INVALID_ARG;
+  const int32_t *slots = p->pv.plan + p->hdr.w[PH_OFF_APPEND], *pos = p->pv.plan + p->hdr.w[PH_OFF_APOS];
+  if (p->pv.kv8 || p->pv.kv4)
+    PASTA_CUDA(append_codes(p, slots, pos, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, rope_table(p, theta),
+                            static_cast<cudaStream_t>(stream)));
+  else if (!usual_rope(p))
+    PASTA_CUDA(launch_kv_append_form(p->pv, slots, pos, 0, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new,
+                                     *rope_table(p, theta), static_cast<cudaStream_t>(stream)));
   else
-    PASTA_CUDA(launch_kv_append_rope(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], p->pv.plan + p->hdr.w[PH_OFF_APOS], 0, n_app,
-                                     layer_begin, layer_count, k_new, v_new, theta, static_cast<cudaStream_t>(stream)));
+    PASTA_CUDA(launch_kv_append_rope(p->pv, slots, pos, 0, n_app, layer_begin, layer_count, k_new, v_new, theta,
+                                     static_cast<cudaStream_t>(stream)));
+  p->launches += 1;
+  return PASTA_OK;
+}
+
+static pasta_status_t rope_queries_impl(pasta_pool_t *p, int32_t layer_count, const void *q, void *q_out, float theta, void *stream) {
+  if (!p) return PASTA_ERR_INVALID_ARG;
+  if (p->host_only || !p->plan_valid) return PASTA_ERR_BAD_STATE;
+  if (layer_count < 0 || layer_count > p->cfg.n_layers || !(theta > 1.f && theta < INFINITY)) return PASTA_ERR_INVALID_ARG;
+  const int32_t n = p->hdr.w[PH_N_QUERIES];
+  if (n == 0 || layer_count == 0) return PASTA_OK;
+  if (!q || !q_out) return PASTA_ERR_INVALID_ARG;
+  const int32_t *pos = p->pv.plan + p->hdr.w[PH_OFF_QPOS];
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (q == q_out && usual_rope(p)) {
+    PASTA_CUDA(launch_rope_queries(p->pv, pos, n, layer_count, q_out, theta, st));
+  } else {
+    if (odd_address(q, q_out)) return PASTA_ERR_INVALID_ARG;
+    PASTA_CUDA(launch_rope_queries_form(p->pv, pos, n, layer_count, q, q_out, *rope_table(p, theta), st));
+  }
   p->launches += 1;
   return PASTA_OK;
 }
 
 pasta_status_t pasta_rope_queries(pasta_pool_t *p, int32_t layer_count, void *q, float theta, void *stream) {
+  return rope_queries_impl(p, layer_count, q, q, theta, stream);
+}
+
+pasta_status_t pasta_rope_queries_to(pasta_pool_t *p, int32_t layer_count, const void *q, void *q_out, float theta, void *stream) {
+  return rope_queries_impl(p, layer_count, q, q_out, theta, stream);
+}
+
+pasta_status_t pasta_set_rope(pasta_pool_t *p, const pasta_rope_form_t *form) {
   if (!p) return PASTA_ERR_INVALID_ARG;
-  if (p->host_only || !p->plan_valid) return PASTA_ERR_BAD_STATE;
-  if (layer_count < 0 || layer_count > p->cfg.n_layers || !(theta > 1.f)) return PASTA_ERR_INVALID_ARG;
-  const int32_t n = p->hdr.w[PH_N_QUERIES];
-  if (n == 0 || layer_count == 0) return PASTA_OK;
-  if (!q) return PASTA_ERR_INVALID_ARG;
-  PASTA_CUDA(launch_rope_queries(p->pv, p->pv.plan + p->hdr.w[PH_OFF_QPOS], n, layer_count, q, theta,
-                                 static_cast<cudaStream_t>(stream)));
-  p->launches += 1;
+  pasta_rope_form_t f{};
+  if (form) {
+    f = *form;
+    if ((f.layout != PASTA_ROPE_HALF && f.layout != PASTA_ROPE_INTERLEAVED) || f.reserved != 0) return PASTA_ERR_INVALID_ARG;
+    if (f.rotary_dim < 0 || f.rotary_dim % 16 || f.rotary_dim > p->cfg.head_dim) return PASTA_ERR_INVALID_ARG;
+    if (f.scaling < PASTA_ROPE_SCALE_NONE || f.scaling > PASTA_ROPE_SCALE_RAMP) return PASTA_ERR_INVALID_ARG;
+    if (!(f.magnitude == 0 || (f.magnitude >= 1e-3 && f.magnitude <= 1e3))) return PASTA_ERR_INVALID_ARG;
+    if (f.scaling != PASTA_ROPE_SCALE_NONE && !(f.factor >= 1 && f.factor <= 1e6)) return PASTA_ERR_INVALID_ARG;
+    if (f.scaling == PASTA_ROPE_SCALE_WAVELENGTH || f.scaling == PASTA_ROPE_SCALE_RAMP) {
+      if (!(f.original_length >= 1 && f.original_length <= 1e9)) return PASTA_ERR_INVALID_ARG;
+      if (!(f.low > 0 && f.low < f.high && f.high <= 1e6)) return PASTA_ERR_INVALID_ARG;
+    }
+    if (f.rotary_dim == p->cfg.head_dim) f.rotary_dim = 0;
+  }
+  p->rope_form = f;
+  p->rope_theta = 0;
+  return PASTA_OK;
+}
+
+pasta_status_t pasta_rope_frequencies(pasta_pool_t *p, float theta, double *f, int32_t capacity, int32_t *count, double *magnitude) {
+  if (!p || !count || capacity < 0 || (capacity > 0 && !f) || !(theta > 1.f && theta < INFINITY)) return PASTA_ERR_INVALID_ARG;
+  const RopeForm *t = rope_table(p, theta);
+  const int32_t n = 8 * t->slots;
+  if (capacity > 0 && capacity < n) return PASTA_ERR_CAPACITY;
+  if (capacity > 0) std::memcpy(f, t->f, size_t(n) * sizeof(double));
+  if (magnitude) *magnitude = t->size;
+  *count = n;
   return PASTA_OK;
 }
 
@@ -454,9 +556,9 @@ pasta_status_t pasta_kv_append(pasta_pool_t *p, int32_t layer_begin, int32_t lay
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
   if (!k_new || !v_new || misaligned(p, k_new, v_new)) return PASTA_ERR_INVALID_ARG;
-  if (p->pv.kv8)
-    PASTA_CUDA(launch_kv8_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, n_app, layer_begin, layer_count,
-                                 tokens_stride(p, n_app), k_new, v_new, 0.0, static_cast<cudaStream_t>(stream)));
+  if (p->pv.kv8 || p->pv.kv4)
+    PASTA_CUDA(append_codes(p, p->pv.plan + p->hdr.w[PH_OFF_APPEND], nullptr, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new,
+                            v_new, nullptr, static_cast<cudaStream_t>(stream)));
   else
     PASTA_CUDA(launch_kv_append(p->pv, p->pv.plan + p->hdr.w[PH_OFF_APPEND], n_app, layer_begin, layer_count, k_new, v_new,
                                 static_cast<cudaStream_t>(stream)));
@@ -516,6 +618,8 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
   if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers) return PASTA_ERR_INVALID_ARG;
   if (layer_count > 0 && p->host_only) return PASTA_ERR_BAD_STATE;
   if (layer_count > 0 && m > 0 && (!k || !v || misaligned(p, k, v))) return PASTA_ERR_INVALID_ARG;
+  const bool form = theta > 0.f && !usual_rope(p);
+  if (layer_count > 0 && m > 0 && form && odd_address(k, v)) return PASTA_ERR_INVALID_ARG;
   Slot slot{};
   const Request *rq = p->host.request(req);
   const int32_t pos0 = (rq && thread >= 0 && thread < static_cast<int32_t>(rq->threads.size())) ? rq->threads[thread].pos_next : 0;
@@ -529,9 +633,10 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;      // elements per token
   const std::vector<int32_t> &pages = rq->streams[thread].pages;
   const int32_t at0 = rq->streams[thread].len - m;      // the run's first token within its stream
-  if (p->pv.kv8) {         // all layers in one launch, page by page
-    PASTA_CUDA(launch_kv8_append_run(p->pv, pages.data() + at0 / PASTA_PAGE, slot.offset, pos0, m, layer_begin, layer_count,
-                                     tokens_stride(p, m), k, v, theta, st, &p->launches));
+  if (p->pv.kv8 || p->pv.kv4) {         // all layers in one launch, page by page
+    const auto launch = p->pv.kv8 ? launch_kv8_append_run : launch_kv4_append_run;
+    PASTA_CUDA(launch(p->pv, pages.data() + at0 / PASTA_PAGE, slot.offset, pos0, m, layer_begin, layer_count, tokens_stride(p, m), k, v,
+                      theta > 0.f ? rope_table(p, theta) : nullptr, st, &p->launches));
     return PASTA_OK;
   }
   std::vector<int32_t> words;
@@ -545,6 +650,13 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
     }
     s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
+    if (form) {                                      // all layers in one launch
+      PASTA_CUDA(launch_kv_append_form(p->pv, p->run_slots_dev, nullptr, pos0 + begin, cnt, layer_begin, layer_count, tokens_stride(p, m),
+                                       static_cast<const uint16_t *>(k) + begin * tok, static_cast<const uint16_t *>(v) + begin * tok,
+                                       *rope_table(p, theta), st));
+      p->launches += 1;
+      continue;
+    }
     for (int32_t l = 0; l < layer_count; ++l) {     // the run's layers are [layer_count, m, …]: one launch per layer and chunk
       const uint16_t *kl = static_cast<const uint16_t *>(k) + (size_t(l) * m + begin) * tok;
       const uint16_t *vl = static_cast<const uint16_t *>(v) + (size_t(l) * m + begin) * tok;
@@ -692,9 +804,10 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
   if (!k_out || !v_out || misaligned(p, k_out, v_out)) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;
-  if (p->pv.kv8) {
-    PASTA_CUDA(launch_kv8_read_run(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count,
-                                   tokens_stride(p, m), k_out, v_out, st, &p->launches));
+  if (p->pv.kv8 || p->pv.kv4) {
+    const auto launch = p->pv.kv8 ? launch_kv8_read_run : launch_kv4_read_run;
+    PASTA_CUDA(launch(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count, tokens_stride(p, m),
+                      k_out, v_out, st, &p->launches));
     return PASTA_OK;
   }
   std::vector<int32_t> words;

@@ -53,6 +53,41 @@ __device__ __forceinline__ int kv8_chunk_offset(int kv, int r, int c) {
   return (j * 2 + kv) * (8 * D) + r8 * D + ((c ^ (D == 128 ? r8 : (r8 >> 1))) << 4);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Layout of one (page, kv head) block of a 4-bit pool (PASTA_FLAG_KV_INT4), 18 D bytes: K and V of 16 tokens, a code of 4 bits
+// per element and one scale of 16 bits for every 32 neighbouring elements of a token:
+//
+//   block = [K codes: D/32 groups of 32 elements][16 tokens][16 bytes]    [K scales: 16 tokens][D/32]
+//           [V codes: D channels][16 tokens, 8 bytes]                     [V scales: D/32 groups][16 tokens]
+//
+// K lies by token and V by channel, the way the attention kernel's threads need them as rows of an MMA operand: a thread per
+// token reads 16 bytes of K next to its neighbours', a thread per channel 8 bytes of V.  A code is u = n + 8 for the whole
+// number n = -7 ... 7 that the element is held as; a scale is the bf16 number t = 16 s.  Eight codes (elements 0 .. 7 of K's
+// row, tokens 0 .. 7 of V's) make a word: codes 2 i and 2 i + 1 lie at bits 4 i and 16 + 4 i, and the word is rotated left by
+// 3, so that (w rotated right by 4 i) & 0x00780078 | 0x3f803f80 is the pair of bf16 numbers 1 + u / 16 and one fused
+// multiply-add makes them the numbers held: (1 + u / 16) t - 1.5 t = n s, exact, since s has five significant bits.
+// Whatever bits a word or a scale of zero holds is finite, so bytes beyond a stream's end vanish against zero weights.
+// ---------------------------------------------------------------------------------------------
+__host__ __device__ constexpr int kv4_block_bytes(int head_dim) { return head_dim * 18; }
+__host__ __device__ constexpr int kv4_k_scales(int head_dim) { return head_dim * 8; }
+__host__ __device__ constexpr int kv4_v_codes(int head_dim) { return head_dim * 9; }
+__host__ __device__ constexpr int kv4_v_scales(int head_dim) { return head_dim * 17; }
+constexpr int kKv4Group = 32;                        // elements that share a scale
+// pair i of a word as 1 + u / 16, and the pair of numbers held for the scale pair t2 and c2 = -1.5 t2
+__device__ __forceinline__ uint32_t kv4_pair(uint32_t w, int i) {
+  return (__funnelshift_r(w, w, 4 * i) & 0x00780078u) | 0x3f803f80u;
+}
+__device__ __forceinline__ uint32_t kv4_offset_of(uint32_t t2) {
+  uint32_t c2;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(c2) : "r"(t2), "r"(0xbfc0bfc0u));
+  return c2;
+}
+__device__ __forceinline__ uint32_t kv4_value(uint32_t pair, uint32_t t2, uint32_t c2) {
+  uint32_t v;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(pair), "r"(t2), "r"(c2));
+  return v;
+}
+
 struct PoolView {
   uint8_t *kv_base;
   int64_t layer_stride;      // bytes between layers
@@ -66,6 +101,7 @@ struct PoolView {
   float softcap_log2;        // 0, or C = cap * log2(e): a score s (in log2 units) becomes C tanh(s / C)
   int32_t kv8;               // 1: the pool holds 8-bit codes and scales (kv8_block_bytes, kv8_chunk_offset)
   int64_t scale_off;         // bytes from a layer's start to its scales (8-bit pools)
+  int32_t kv4;               // 1: the pool holds 4-bit codes and scales (kv4_block_bytes)
   int32_t debug_hold;        // test hook, 0 in normal use: bit r set = role r of the tensor-core kernel never starts
 };
 

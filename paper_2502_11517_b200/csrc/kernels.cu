@@ -335,9 +335,9 @@ cudaError_t launch_kv_read(const PoolView &pv, const int32_t *slots, int32_t n_t
 constexpr int W_WARPS = 1;            // one warp per block: the block scheduler balances the units
 constexpr int W_STAGES = 2;
 
-template <int D, int G, bool kKv8>
+template <int D, int G, int kBits>
 struct WarpSmem {
-  static constexpr int BLOCK = kKv8 ? kv8_block_bytes(D) : kv_block_bytes(D);
+  static constexpr int BLOCK = kBits == 4 ? kv4_block_bytes(D) : kBits == 8 ? kv8_block_bytes(D) : kv_block_bytes(D);
   static constexpr int Q_BYTES = G * D * 4;
   static constexpr int P_BYTES = 16 * G * 4;
   static constexpr int BAR_BYTES = 64;
@@ -345,16 +345,18 @@ struct WarpSmem {
   static constexpr int TOTAL = PER_WARP * W_WARPS;
 };
 
-// kKv8: the pool's 8-bit blocks; ek joins the score's scale, 2^ev the weights on their way to P.V.  kCap: capped scores.
-template <int D, int G, bool kKv8, bool kCap>
+// kBits: of the pool's elements.  8: ek joins the score's scale, 2^ev the weights on their way to P.V.  4: codes become the
+// numbers held as they are read.  kCap: capped scores.
+template <int D, int G, int kBits, bool kCap>
 __global__ void __launch_bounds__(W_WARPS * 32)
 attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wunits, int32_t t_rows,
                  int32_t n_queries, int32_t layer_begin, int32_t layer_count,
                  const __nv_bfloat16 *__restrict__ q, float scale_log2) {
-  using S = WarpSmem<D, G, kKv8>;
+  using S = WarpSmem<D, G, kBits>;
+  constexpr bool kKv8 = kBits == 8, kKv4 = kBits == 4;
   constexpr int NH = D / 64;
   constexpr int E = D / 32;            // output elements per lane
-  constexpr int CH = kKv8 ? D / 32 : D / 16;           // 16-byte chunks of a K row handled by one lane
+  constexpr int CH = kKv4 ? D / 64 : kKv8 ? D / 32 : D / 16;           // 16-byte chunks of a K row handled by one lane
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   grid_dependency_wait();         // the kernel ahead in the stream (append or tensor-core pass) has completed
   grid_launch_dependents();
@@ -399,7 +401,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     }
   };
   for (int i = 0; i < W_STAGES && i < n_pg; ++i) issue(i);
-  uint32_t spoilt = 0;            // 8-bit pools: bit h set, row h holds a number that is not finite
+  uint32_t spoilt = 0;            // 8-bit and 4-bit pools: bit h set, row h holds a number that is not finite
   // the G query rows of this kv head, pre-multiplied by scale * log2(e) (overlaps the first copies)
   {
     const __nv_bfloat162 *qsrc = reinterpret_cast<const __nv_bfloat162 *>(
@@ -409,9 +411,9 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
       const float2 f = __bfloat1622float2(qsrc[i]);
       q_s[2 * i] = f.x * scale_log2;
       q_s[2 * i + 1] = f.y * scale_log2;
-      if (kKv8 && !(fmaxf(fabsf(f.x), fabsf(f.y)) < INFINITY && f.x == f.x && f.y == f.y)) spoilt |= 1u << (2 * i / D);
+      if (kBits < 16 && !(fmaxf(fabsf(f.x), fabsf(f.y)) < INFINITY && f.x == f.x && f.y == f.y)) spoilt |= 1u << (2 * i / D);
     }
-    if (kKv8) spoilt = __reduce_or_sync(0xffffffffu, spoilt);
+    if (kBits < 16) spoilt = __reduce_or_sync(0xffffffffu, spoilt);
   }
   __syncwarp();
 
@@ -461,6 +463,23 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
             acc[h] = fmaf(k23.x, qa.z, acc[h]); acc[h] = fmaf(k23.y, qa.w, acc[h]);
           }
         }
+      } else if constexpr (kKv4) {
+        const uint4 kk = *reinterpret_cast<const uint4 *>(sp + c * 256 + r * 16);
+        const uint32_t t = *reinterpret_cast<const uint16_t *>(sp + kv4_k_scales(D) + (r * (D / kKv4Group) + c) * 2);
+        const uint32_t t2 = t | (t << 16), c2 = kv4_offset_of(t2);
+        const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v = kv4_value(kv4_pair(kw[w], i), t2, c2);
+            const float k0 = bf16_lo(v), k1 = bf16_hi(v);
+#pragma unroll
+            for (int h = 0; h < G; ++h) {
+              const float2 qa = *reinterpret_cast<const float2 *>(q_s + h * D + c * 32 + w * 8 + i * 2);
+              acc[h] = fmaf(k0, qa.x, acc[h]); acc[h] = fmaf(k1, qa.y, acc[h]);
+            }
+          }
       } else {
         const uint4 kk = *reinterpret_cast<const uint4 *>(sp + kv_chunk_offset(NH, 0, r, c));
         const float k0 = bf16_lo(kk.x), k1 = bf16_hi(kk.x), k2 = bf16_lo(kk.y), k3 = bf16_hi(kk.y);
@@ -497,7 +516,29 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
       if (sub == 0) p_s[r * G + h] = kKv8 ? pj * fv : pj;
     }
     __syncwarp();
-    {
+    if constexpr (kKv4) {
+      // a lane's channels lie side by side, 16 tokens of a channel in 8 bytes; tokens beyond the unit's last have weight 0
+      constexpr int LPG = kKv4Group / E;
+      uint32_t w[E][2];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(sp + kv4_v_codes(D) + (lane * E + e) * 8);
+        w[e][0] = v.x; w[e][1] = v.y;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t t2 = *reinterpret_cast<const uint32_t *>(sp + kv4_v_scales(D) + (lane / LPG) * 32 + j * 4), c2 = kv4_offset_of(t2);
+        uint32_t v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = kv4_value(kv4_pair(w[e][j >> 2], j & 3), t2, c2);
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+          const float p0 = p_s[2 * j * G + h], p1 = p_s[(2 * j + 1) * G + h];
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[h][e] = fmaf(p1, bf16_hi(v[e]), fmaf(p0, bf16_lo(v[e]), o[h][e]));
+        }
+      }
+    } else {
       constexpr int EC = kKv8 ? 16 : 8;             // elements of a 16-byte chunk
       const int c = (lane * E) / EC;                // chunk that holds this lane's elements
       const int within = ((lane * E) % EC) * (16 / EC);      // byte offset inside the chunk
@@ -549,7 +590,7 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
     lt += __shfl_xor_sync(0xffffffffu, lt, 4);
     lt += __shfl_xor_sync(0xffffffffu, lt, 2);
     lt += __shfl_xor_sync(0xffffffffu, lt, 1);
-    if (kKv8 && (((spoilt >> h) & 1) || lt != lt)) {
+    if (kBits < 16 && (((spoilt >> h) & 1) || lt != lt)) {
       m[h] = not_a_row().x;
       lt = not_a_row().y;
 #pragma unroll
@@ -562,29 +603,29 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
   }
 }
 
-template <int D, int G, bool kKv8, bool kCap>
+template <int D, int G, int kBits, bool kCap>
 static cudaError_t launch_warp_t(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                                  const void *q, float scale_log2, cudaStream_t st) {
-  using S = WarpSmem<D, G, kKv8>;
+  using S = WarpSmem<D, G, kBits>;
   static uint64_t prepared = 0;
   {
-    cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_warp_kernel<D, G, kKv8, kCap>), S::TOTAL, &prepared);
+    cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(attn_warp_kernel<D, G, kBits, kCap>), S::TOTAL, &prepared);
     if (e != cudaSuccess) return e;
   }
   const int64_t warps = static_cast<int64_t>(h.w[PH_N_WUNITS]) * layer_count;
   if (warps == 0) return cudaSuccess;
   const int64_t blocks = (warps + W_WARPS - 1) / W_WARPS;
-  return launch_overlapped(attn_warp_kernel<D, G, kKv8, kCap>, dim3(static_cast<unsigned>(blocks)), dim3(W_WARPS * 32), S::TOTAL, st, pv,
+  return launch_overlapped(attn_warp_kernel<D, G, kBits, kCap>, dim3(static_cast<unsigned>(blocks)), dim3(W_WARPS * 32), S::TOTAL, st, pv,
                            h.w[PH_OFF_WUNIT], h.w[PH_OFF_PAGES], h.w[PH_N_WUNITS], h.w[PH_T_ROWS], h.w[PH_N_QUERIES],
                            layer_begin, layer_count, static_cast<const __nv_bfloat16 *>(q), scale_log2);
 }
 
-template <bool kKv8, bool kCap>
+template <int kBits, bool kCap>
 static cudaError_t launch_warp_k(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                                  const void *q, float scale_log2, cudaStream_t st) {
   const int G = pv.n_q_heads / pv.n_kv_heads;
 #define PASTA_W(DD, GG) \
-  if (pv.head_dim == DD && G == GG) return launch_warp_t<DD, GG, kKv8, kCap>(pv, h, layer_begin, layer_count, q, scale_log2, st);
+  if (pv.head_dim == DD && G == GG) return launch_warp_t<DD, GG, kBits, kCap>(pv, h, layer_begin, layer_count, q, scale_log2, st);
   PASTA_W(128, 1) PASTA_W(128, 2) PASTA_W(128, 4) PASTA_W(128, 8)
   PASTA_W(64, 1) PASTA_W(64, 2) PASTA_W(64, 4) PASTA_W(64, 8)
 #undef PASTA_W
@@ -594,10 +635,10 @@ static cudaError_t launch_warp_k(const PoolView &pv, const PlanHeader &h, int32_
 cudaError_t launch_attn_warp(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                              const void *q, float scale_log2, cudaStream_t st) {
   const bool cap = pv.softcap_log2 > 0.f;
-  if (pv.kv8) return cap ? launch_warp_k<true, true>(pv, h, layer_begin, layer_count, q, scale_log2, st)
-                         : launch_warp_k<true, false>(pv, h, layer_begin, layer_count, q, scale_log2, st);
-  return cap ? launch_warp_k<false, true>(pv, h, layer_begin, layer_count, q, scale_log2, st)
-             : launch_warp_k<false, false>(pv, h, layer_begin, layer_count, q, scale_log2, st);
+  const auto launch = pv.kv4 ? (cap ? launch_warp_k<4, true> : launch_warp_k<4, false>)
+                    : pv.kv8 ? (cap ? launch_warp_k<8, true> : launch_warp_k<8, false>)
+                             : (cap ? launch_warp_k<16, true> : launch_warp_k<16, false>);
+  return launch(pv, h, layer_begin, layer_count, q, scale_log2, st);
 }
 
 // =============================================================================================

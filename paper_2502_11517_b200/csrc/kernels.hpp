@@ -7,6 +7,7 @@
 namespace pasta {
 
 struct PoolView;   // device_common.cuh
+struct RopeForm;   // rope_form.cuh
 
 struct PlanHeader {            // host copy of the plan's header words
   int32_t w[32];
@@ -73,21 +74,38 @@ cudaError_t launch_attn_kv8(const PoolView &pv, const PlanHeader &h, int32_t lay
 // the kernel that serves this pool's t-units and d-units
 cudaError_t launch_attn_units(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count, const void *q,
                               float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
-// K1 of an 8-bit pool: quantises the new tokens' K and V page by page.  slots: device, 2 words per token.  theta = 0: no
+// K1 of an 8-bit pool: quantises the new tokens' K and V page by page.  slots: device, 2 words per token.  form NULL: no
 // rotation; else K is rotated by pos (device).  k_new, v_new: [layer_count, n_tok, Hkv, D], layers in_layer_stride elements
 // apart.
 cudaError_t launch_kv8_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
-                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new, double theta,
-                              cudaStream_t st);
+                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                              const RopeForm *form, cudaStream_t st);
 // The same for a run of tokens of one stream at consecutive positions, and a run read back as dense bf16 [n_tok, Hkv, D] arrays,
 // layers out_layer_stride elements apart (exact: a code times its power-of-two scale is a bf16 number).  `pages` is host memory:
 // the run's pages, first_offset the first token's row; they travel as kernel arguments.  `launches` is counted up.
 cudaError_t launch_kv8_append_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
                                   int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
-                                  const void *v_new, double theta, cudaStream_t st, int64_t *launches);
+                                  const void *v_new, const RopeForm *form, cudaStream_t st, int64_t *launches);
 cudaError_t launch_kv8_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
                                 int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st,
                                 int64_t *launches);
+// The same three for a 4-bit pool.
+cudaError_t launch_kv4_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
+                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                              const RopeForm *form, cudaStream_t st);
+cudaError_t launch_kv4_append_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                  const void *v_new, const RopeForm *form, cudaStream_t st, int64_t *launches);
+cudaError_t launch_kv4_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
+                                int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st,
+                                int64_t *launches);
+// K1 of a bf16 pool with K rotated in any form; pos: device, or null for pos0, pos0 + 1, ...
+cudaError_t launch_kv_append_form(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t pos0, int32_t n_tok,
+                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                  const void *v_new, const RopeForm &form, cudaStream_t st);
+// the step's queries rotated in any form, q -> q_out (which may be q)
+cudaError_t launch_rope_queries_form(const PoolView &pv, const int32_t *pos, int32_t n, int32_t layer_count, const void *q, void *q_out,
+                                     const RopeForm &form, cudaStream_t st);
 bool tensor_path_available();       // false while the tensor-core kernel is compiled out
 // test kernel: a bounded wait that runs out (one warp, PoolView::wait_limit cycles), reported as PASTA_ERR_TIMEOUT
 cudaError_t launch_wait_expiry(const PoolView &pv, cudaStream_t st);

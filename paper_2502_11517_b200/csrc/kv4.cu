@@ -1,0 +1,487 @@
+// The 4-bit cache: quantising append (K1 of a 4-bit pool) and read-back.  Layout of a block: device_common.cuh.
+//
+// 32 neighbouring elements of one token's K (or V) of one kv head are a group with a scale of its own:
+//   s = the smallest number of five significant bits with amax <= 7 s over the group, kept within [2^-110, 31 * 2^106],
+//   n = the whole number nearest to x / s, ties to the even one, kept within -7 ... 7; the element is held as n s.
+// A token's codes depend on that token alone, so what the cache holds does not depend on how tokens were grouped into calls,
+// and nothing stored is ever rounded again.  The largest element of a group comes out as n = +-7 (7 s is less than 17/16 of
+// amax), so what is read back has the same scale and quantises to itself.  Five bits: n s then has at most eight significant
+// bits and is a bf16 number, and s is less than 1/16 above what the group would need.
+//
+// An exact x / s decides a code wherever 2 x is an odd multiple of s, which for bf16 numbers is often.  Two ways, neither with
+// a division per element:
+//   bf16 numbers   x / s is at least 2^-10 away from k + 1/2 unless it is k + 1/2, so x (1/s) is rounded to a multiple of 2^-13
+//                  first (a tie comes out as the tie it is) and to a whole number then;
+//   rotated keys   (fp32) n0 = nearest to x (1/s), then x - n0 s, which is exact, is compared with s / 2.
+// An element that is not finite is stored as zero and reported (PASTA_ERR_DEVICE_CHECK), as in an 8-bit pool.
+//
+// What bounds it: memory.  2 bytes of bf16 in and 9/16 of a byte out per element, one pass.
+#include <cmath>
+
+#include "device_common.cuh"
+#include "kernels.hpp"
+#include "page_run.cuh"
+#include "rope_form.cuh"
+
+namespace pasta {
+
+namespace {
+
+constexpr float kScaleMin = 0x1p-110f, kScaleMax = 31 * 0x1p106f;
+
+// The scale of a group whose largest magnitude is amax (finite).  amax / 7 rounded to fp32 is never below a number of five
+// bits that the quotient exceeds (its distance is at least 1/7 of a step of amax, more than half a step of the quotient).
+__device__ __forceinline__ float group_scale(float amax) {
+  const float s = __uint_as_float((__float_as_uint(__fdiv_rn(amax, 7.f)) + 0x7ffffu) & 0xfff80000u);
+  return fminf(fmaxf(s, kScaleMin), kScaleMax);
+}
+__device__ __forceinline__ uint32_t scale_bits(float s) { return __float_as_uint(16.f * s) >> 16; }      // t, a bf16 number
+
+// whole number of scales nearest to a bf16 number x, as fp32 (|x| <= 7 s); r = 1 / s
+__device__ __forceinline__ float code_of_bf16(float x, float r) {
+  // 1536 = 1.5 * 2^10: the sum is a multiple of 2^-13; 12582912 = 1.5 * 2^23
+  return ((fmaf(x, r, 1536.f) - 1536.f) + 12582912.f) - 12582912.f;
+}
+// the same of any fp32 number
+__device__ __forceinline__ float code_of_fp32(float x, float s, float r) {
+  float n = fmaf(x, r, 12582912.f) - 12582912.f;
+  const float e = fmaf(-n, s, x), half = 0.5f * s;
+  if (fabsf(e) >= half) {
+    const bool odd = static_cast<int>(n) & 1;
+    if (fabsf(e) > half || odd) n += copysignf(1.f, e);
+  }
+  return n;
+}
+// Word of eight codes n[0..7].  The sums are whole numbers below 2^24, hence exact.
+__device__ __forceinline__ uint32_t code_word(const float *n) {
+  const float lo = fmaf(n[6], 4096.f, fmaf(n[4], 256.f, fmaf(n[2], 16.f, n[0]))) + (8388608.f + 34952.f);      // 34952: 8 in each code
+  const float hi = fmaf(n[7], 4096.f, fmaf(n[5], 256.f, fmaf(n[3], 16.f, n[1]))) + (8388608.f + 34952.f);
+  const uint32_t w = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
+  return __funnelshift_l(w, w, 3);
+}
+
+// 16 elements of a K row (16-element chunk c of token row r), as fp32 numbers of a bf16 row or of a rotated one; two lanes
+// share a group.
+template <int D, bool kRotated>
+__device__ __forceinline__ void store_k16(uint8_t *block, int r, int c, bool valid, float *x) {
+  float amax = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[e]));
+  amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+  const float s = group_scale(amax), inv = __frcp_rn(s);
+  if (s >= kScaleMax) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = fminf(fmaxf(x[e], -7.f * s), 7.f * s);
+  }
+  float n[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) n[e] = kRotated ? code_of_fp32(x[e], s, inv) : code_of_bf16(x[e], inv);
+  if (!valid) return;
+  *reinterpret_cast<uint2 *>(block + (c >> 1) * 256 + r * 16 + (c & 1) * 8) = make_uint2(code_word(n), code_word(n + 8));
+  if ((c & 1) == 0)
+    *reinterpret_cast<uint16_t *>(block + kv4_k_scales(D) + (r * (D / kKv4Group) + (c >> 1)) * 2) = static_cast<uint16_t>(scale_bits(s));
+}
+
+// zeros in place of numbers that are not finite; returns whether there were any
+__device__ __forceinline__ bool clean_word(uint32_t &w) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  if (lo) w &= 0xffff0000u;
+  if (hi) w &= 0xffffu;
+  return lo || hi;
+}
+
+// K of tokens in rows off0 .. off0 + cnt - 1 of a page, one kv head, by a warp.  rows: the tokens' K, `stride` elements apart.
+// stage: this warp's room for the rotated rows of one pass (32 x 16 floats).
+template <int D, bool kRope>
+__device__ __forceinline__ bool append_k(uint8_t *block, const __nv_bfloat16 *rows, int64_t stride, int off0, int cnt,
+                                         const RopeForm &form, const double2 *turn, float *stage) {
+  constexpr int LPT = D / 16, TPI = 32 / LPT;
+  const int lane = threadIdx.x & 31, c = lane % LPT;
+  bool bad = false;
+  for (int r0 = 0; r0 < cnt; r0 += TPI) {
+    const int r = r0 + lane / LPT;
+    const bool valid = r < cnt;
+    const uint4 *row = reinterpret_cast<const uint4 *>(rows + r * stride);
+    float x[16];
+    if constexpr (kRope) {
+      const int c_a = rope_chunk_a(form, c), c_b = rope_chunk_b(form, c);
+      const bool turns = c < form.slots, alternate = form.interleaved && turns;
+      uint4 lo4 = make_uint4(0, 0, 0, 0), hi4 = lo4;
+      if (valid) { lo4 = __ldg(row + c_a); hi4 = __ldg(row + c_b); }
+      if (chunk_not_finite(lo4) || chunk_not_finite(hi4)) { bad = true; rope_clean(lo4, hi4, alternate, turns); }
+      float y[16], lo[8], hi[8];
+      rope_slot<D>(lo4, hi4, alternate, turn + (valid ? r : 0) * (D / 2), c, y);
+      rope_unslot(y, alternate, lo, hi);
+      // the rotated row's chunks change hands through shared memory, so that a lane holds 16 neighbouring elements
+      float *mine = stage + (lane / LPT) * D;
+      auto put = [&](int chunk, const float *v) {
+        float4 *dst = reinterpret_cast<float4 *>(mine + chunk * 8);
+        dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+        dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+      };
+      put(c_a, lo);
+      put(c_b, hi);
+      __syncwarp();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = reinterpret_cast<const float4 *>(mine + c * 16)[e];
+        x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+      }
+      __syncwarp();
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+      if (top == INFINITY) {                      // a rotation that left fp32 (no NaN: its operands are finite)
+        bad = true;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = fabsf(x[e]) == INFINITY ? 0.f : x[e];
+      }
+    } else {
+      uint4 a = make_uint4(0, 0, 0, 0), b = a;
+      if (valid) { a = __ldg(row + 2 * c); b = __ldg(row + 2 * c + 1); }
+      uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      if (chunk_not_finite(a) || chunk_not_finite(b)) {
+        bad = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) clean_word(w[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    }
+    store_k16<D, kRope>(block, off0 + r, c, valid, x);
+  }
+  return bad;
+}
+
+// V of the same tokens, by a warp: a lane holds D / 32 channels of all 16 rows of the page.  Words (8 tokens of a channel) that
+// the call does not fill are read, changed and written back; a page is worked on by one warp per call and kv head.
+template <int D>
+__device__ __forceinline__ bool append_v(uint8_t *block, const __nv_bfloat16 *rows, int64_t stride, int off0, int cnt) {
+  constexpr int CH = D / 32, LPG = kKv4Group / CH;      // channels per lane, lanes per group
+  const int lane = threadIdx.x & 31;
+  bool bad = false;
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {                         // rows 8 h .. 8 h + 7: one word of every channel
+    const int lo = max(off0, 8 * h), hi = min(off0 + cnt, 8 * h + 8);
+    if (lo >= hi) continue;
+    uint32_t x[8][CH / 2];
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 8 * h + i;
+#pragma unroll
+      for (int w = 0; w < CH / 2; ++w) x[i][w] = 0;
+      if (r >= lo && r < hi) {
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(rows + (r - off0) * stride) + lane * (CH / 2);
+        if constexpr (CH == 4) {
+          const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
+          x[i][0] = v.x;
+          x[i][1] = v.y;
+        } else {
+          x[i][0] = __ldg(src);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int w = 0; w < CH / 2; ++w) any = __vmaxu2(any, x[i][w] & 0x7fff7fffu);
+    if ((any & 0xffffu) >= 0x7f80u || any >= 0x7f800000u) {
+      bad = true;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < CH / 2; ++w) clean_word(x[i][w]);
+    }
+    // largest magnitudes of two tokens at a time (bf16 bits compare as integers), over the lanes of a group
+    uint32_t m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t a = x[2 * j][0] & 0x7fff7fffu, b = x[2 * j + 1][0] & 0x7fff7fffu;
+      if constexpr (CH == 4) {
+        a = __vmaxu2(a, x[2 * j][1] & 0x7fff7fffu);
+        b = __vmaxu2(b, x[2 * j + 1][1] & 0x7fff7fffu);
+      }
+      m[j] = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+      for (int o = 1; o < LPG; o <<= 1) m[j] = __vmaxu2(m[j], __shfl_xor_sync(0xffffffffu, m[j], o));
+    }
+    // lane i of a group works out the scale of token i, and keeps it; the others ask for 1 / s
+    const int who = lane & 7;
+    const uint32_t pair = (who & 4) ? ((who & 2) ? m[3] : m[2]) : ((who & 2) ? m[1] : m[0]);
+    const float s = group_scale((who & 1) ? bf16_hi(pair) : bf16_lo(pair)), inv = __frcp_rn(s);
+    if ((lane & (LPG - 1)) < 8 && 8 * h + who >= lo && 8 * h + who < hi)
+      *reinterpret_cast<uint16_t *>(block + kv4_v_scales(D) + (lane / LPG) * 32 + (8 * h + who) * 2) = static_cast<uint16_t>(scale_bits(s));
+    const bool clamp = __any_sync(0xffffffffu, s >= kScaleMax);
+    float n[CH][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float r = __shfl_sync(0xffffffffu, inv, (lane & ~7) | i);
+      float v[CH];
+#pragma unroll
+      for (int w = 0; w < CH / 2; ++w) { v[2 * w] = bf16_lo(x[i][w]); v[2 * w + 1] = bf16_hi(x[i][w]); }
+#pragma unroll
+      for (int ch = 0; ch < CH; ++ch) {
+        if (clamp) v[ch] = fminf(fmaxf(v[ch], -7.f / r), 7.f / r);
+        n[ch][i] = code_of_bf16(v[ch], r);
+        if (clamp) n[ch][i] = fminf(fmaxf(n[ch][i], -7.f), 7.f);
+      }
+    }
+    uint32_t *dst = reinterpret_cast<uint32_t *>(block + kv4_v_codes(D)) + lane * CH * 2 + h;
+    uint32_t keep = 0;                                  // bits of the word that hold other tokens
+    if (hi - lo < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (8 * h + i < lo || 8 * h + i >= hi) keep |= 0xfu << ((i & 1) * 16 + (i >> 1) * 4);
+      keep = __funnelshift_l(keep, keep, 3);
+    }
+#pragma unroll
+    for (int ch = 0; ch < CH; ++ch) {
+      uint32_t w = code_word(n[ch]);
+      if (keep) w = (w & ~keep) | (dst[2 * ch] & keep);
+      dst[2 * ch] = w;
+    }
+  }
+  return bad;
+}
+
+template <int D, bool kRope>
+struct AppendSmem {
+  double2 turn[kRope ? PASTA_PAGE * (D / 2) : 1];
+  float stage[kRope ? A_WARPS : 1][kRope ? 512 : 4];
+};
+
+// The new tokens that fall into one page, layers ll .. ll_end - 1, by one CTA: a warp takes one (kv head, K or V) at a time.
+template <int D, bool kRope>
+__device__ __forceinline__ void append_page4(const PoolView &pv, int page, int off0, int first, int cnt, int layer_begin, int ll, int ll_end,
+                                             int64_t in_layer_stride, const __nv_bfloat16 *__restrict__ k_new,
+                                             const __nv_bfloat16 *__restrict__ v_new, const RopeForm &form, AppendSmem<D, kRope> &sm) {
+  const int warp = threadIdx.x >> 5;
+  const int H = pv.n_kv_heads;
+  const int64_t stride = static_cast<int64_t>(H) * D;
+  for (; ll < ll_end; ++ll) {
+    if (ll + 1 < ll_end) prefetch_rows(k_new, v_new, (ll + 1) * in_layer_stride + first * stride, cnt * H * D * 2);
+    uint8_t *layer = pv.kv_base + (layer_begin + ll) * pv.layer_stride;
+    for (int item = warp; item < 2 * H; item += A_WARPS) {
+      const int g = item >> 1, kv = (item ^ (item / A_WARPS)) & 1;      // a warp's items are K and V in turn
+      uint8_t *block = layer + (static_cast<int64_t>(page) * H + g) * kv4_block_bytes(D);
+      const int64_t at = ll * in_layer_stride + first * stride + g * D;
+      const bool bad = kv ? append_v<D>(block, v_new + at, stride, off0, cnt)
+                          : append_k<D, kRope>(block, k_new + at, stride, off0, cnt, form, sm.turn, sm.stage[kRope ? warp : 0]);
+      if (bad) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    }
+  }
+}
+
+// Tokens of a step: slots[2 i], slots[2 i + 1] are token i's page and row.  One CTA per group of tokens that are neighbours in
+// one page (the CTA of a group's first token takes it) and slice of the layers.
+template <int D, bool kRope>
+__global__ void __launch_bounds__(A_THREADS, 2)
+kv4_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t n_tok,
+                  int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
+                  const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm form) {
+  __shared__ AppendSmem<D, kRope> sm;
+  grid_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int first = blockIdx.x;
+  const int page = slots[2 * first], off0 = slots[2 * first + 1];
+  if (first > 0 && slots[2 * first - 2] == page && slots[2 * first - 1] == off0 - 1) return;
+  const int a = first + lane;
+  const bool mine = lane < PASTA_PAGE && a < n_tok && slots[2 * a] == page && slots[2 * a + 1] == off0 + lane;
+  const int cnt = __ffs(~__ballot_sync(0xffffffffu, mine)) - 1;
+  if (page < 0 || page >= pv.n_pages || off0 < 0 || off0 + cnt > PASTA_PAGE || cnt < 1) {
+    if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    return;
+  }
+  if constexpr (kRope) {
+    for (int x = tid; x < cnt * (D / 2); x += A_THREADS)
+      sm.turn[x / (D / 2) * (D / 2) + turn_at<D>(x % (D / 2))] = turn_of(form, x % (D / 2), pos[first + x / (D / 2)]);
+    __syncthreads();
+  }
+  const int ll = blockIdx.y * layers_per_cta;
+  append_page4<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, form, sm);
+}
+
+// A run: n_tok tokens of one stream at consecutive positions, the first at row first_offset of the first page.  One CTA per
+// page and slice of the layers.
+template <int D, bool kRope, int N>
+__global__ void __launch_bounds__(A_THREADS, 2)
+kv4_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
+                      int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
+                      const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm form) {
+  __shared__ AppendSmem<D, kRope> sm;
+  grid_launch_dependents();
+  const int first = max(0, static_cast<int>(blockIdx.x) * PASTA_PAGE - first_offset);
+  const int cnt = min(n_tok, (static_cast<int>(blockIdx.x) + 1) * PASTA_PAGE - first_offset) - first;
+  const int page = pages.page[blockIdx.x], off0 = blockIdx.x == 0 ? first_offset : 0;
+  if (page < 0 || page >= pv.n_pages || cnt < 1) {
+    if (threadIdx.x == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    return;
+  }
+  const int ll = blockIdx.y * layers_per_cta;
+  prefetch_rows(k_new, v_new, ll * in_layer_stride + static_cast<int64_t>(first) * pv.n_kv_heads * D, cnt * pv.n_kv_heads * D * 2);
+  if constexpr (kRope) {
+    turns_of_run<D, A_THREADS>(form, pos0 + first, cnt, sm.turn);
+    __syncthreads();
+  }
+  append_page4<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, form, sm);
+}
+
+// A run read back: one CTA per page and layer (blockIdx.y), a warp per (kv head, K or V).
+template <int D, int N>
+__global__ void __launch_bounds__(A_THREADS, 4)
+kv4_read_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t n_tok, int32_t first_offset, int32_t layer_begin,
+                int64_t out_layer_stride, __nv_bfloat16 *__restrict__ k_out, __nv_bfloat16 *__restrict__ v_out) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int first = static_cast<int>(blockIdx.x) * PASTA_PAGE - first_offset;       // token of the page's first row
+  const int page = pages.page[blockIdx.x];
+  if (page < 0 || page >= pv.n_pages) {
+    if (threadIdx.x == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
+    return;
+  }
+  const int H = pv.n_kv_heads;
+  const uint8_t *layer = pv.kv_base + (layer_begin + static_cast<int64_t>(blockIdx.y)) * pv.layer_stride;
+  for (int item = warp; item < 2 * H; item += A_WARPS) {
+    const int g = item >> 1;
+    const uint8_t *block = layer + (static_cast<int64_t>(page) * H + g) * kv4_block_bytes(D);
+    if ((item & 1) == 0) {                            // K: a lane turns 16 codes of a row into 32 bytes
+      constexpr int LPT = D / 16, TPI = 32 / LPT, NI = PASTA_PAGE / TPI;
+      const int c = lane % LPT;
+      uint2 q[NI];
+      uint32_t t[NI];
+#pragma unroll
+      for (int it = 0; it < NI; ++it) {
+        const int r = it * TPI + lane / LPT;
+        q[it] = *reinterpret_cast<const uint2 *>(block + (c >> 1) * 256 + r * 16 + (c & 1) * 8);
+        t[it] = *reinterpret_cast<const uint16_t *>(block + kv4_k_scales(D) + (r * (D / kKv4Group) + (c >> 1)) * 2);
+      }
+#pragma unroll
+      for (int it = 0; it < NI; ++it) {
+        const int tok = first + it * TPI + lane / LPT;
+        if (tok < 0 || tok >= n_tok) continue;
+        const uint32_t t2 = t[it] | (t[it] << 16), c2 = kv4_offset_of(t2);
+        uint32_t o[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          o[i] = kv4_value(kv4_pair(q[it].x, i), t2, c2);
+          o[4 + i] = kv4_value(kv4_pair(q[it].y, i), t2, c2);
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(k_out + blockIdx.y * out_layer_stride + (static_cast<int64_t>(tok) * H + g) * D + c * 16);
+        dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      }
+    } else {                                          // V: a lane turns D / 32 channels of 16 tokens
+      constexpr int CH = D / 32, LPG = kKv4Group / CH;
+      uint32_t w[CH][2], t[8];
+#pragma unroll
+      for (int ch = 0; ch < CH; ch += 2) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(block + kv4_v_codes(D) + (lane * CH + ch) * 8);
+        w[ch][0] = v.x; w[ch][1] = v.y; w[ch + 1][0] = v.z; w[ch + 1][1] = v.w;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(block + kv4_v_scales(D) + (lane / LPG) * 32 + j * 16);
+        t[4 * j] = v.x; t[4 * j + 1] = v.y; t[4 * j + 2] = v.z; t[4 * j + 3] = v.w;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {                   // tokens 2 j and 2 j + 1
+        const uint32_t c2 = kv4_offset_of(t[j]);
+        uint32_t v[CH];
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) v[ch] = kv4_value(kv4_pair(w[ch][j >> 2], j & 3), t[j], c2);
+#pragma unroll
+        for (int up = 0; up < 2; ++up) {
+          const int tok = first + 2 * j + up;
+          if (tok < 0 || tok >= n_tok) continue;
+          uint32_t *dst = reinterpret_cast<uint32_t *>(v_out + blockIdx.y * out_layer_stride + (static_cast<int64_t>(tok) * H + g) * D) + lane * (CH / 2);
+          if constexpr (CH == 4)
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(__byte_perm(v[0], v[1], up ? 0x7632 : 0x5410), __byte_perm(v[2], v[3], up ? 0x7632 : 0x5410));
+          else
+            *dst = __byte_perm(v[0], v[1], up ? 0x7632 : 0x5410);
+        }
+      }
+    }
+  }
+}
+
+template <int N>
+cudaError_t launch_append_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
+                                int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const __nv_bfloat16 *k,
+                                const __nv_bfloat16 *v, const RopeForm *form, cudaStream_t st) {
+  static const RopeForm none{};
+  const PageList<N> list = list_of<N>(pages, n_pages);
+  const int per = layers_per_cta(n_pages, layer_count);
+  const dim3 grid(n_pages, (layer_count + per - 1) / per);
+  const auto kernel = pv.head_dim == 128 ? (form ? kv4_append_run_kernel<128, true, N> : kv4_append_run_kernel<128, false, N>)
+                                         : (form ? kv4_append_run_kernel<64, true, N> : kv4_append_run_kernel<64, false, N>);
+  kernel<<<grid, A_THREADS, 0, st>>>(pv, list, pos0, n_tok, first_offset, layer_begin, layer_count, per, in_layer_stride, k, v,
+                                     form ? *form : none);
+  return cudaGetLastError();
+}
+
+template <int N>
+cudaError_t launch_read_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t n_tok, int32_t first_offset,
+                              int32_t layer_begin, int32_t layer_count, int64_t out_layer_stride, __nv_bfloat16 *k, __nv_bfloat16 *v,
+                              cudaStream_t st) {
+  const PageList<N> list = list_of<N>(pages, n_pages);
+  const auto kernel = pv.head_dim == 128 ? kv4_read_kernel<128, N> : kv4_read_kernel<64, N>;
+  kernel<<<dim3(n_pages, layer_count), A_THREADS, 0, st>>>(pv, list, n_tok, first_offset, layer_begin, out_layer_stride, k, v);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
+                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                              const RopeForm *form, cudaStream_t st) {
+  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
+  static const RopeForm none{};
+  const int per = layers_per_cta(n_tok, layer_count);
+  const dim3 grid(n_tok, (layer_count + per - 1) / per);
+  const auto kernel = pv.head_dim == 128 ? (form ? kv4_append_kernel<128, true> : kv4_append_kernel<128, false>)
+                                         : (form ? kv4_append_kernel<64, true> : kv4_append_kernel<64, false>);
+  kernel<<<grid, A_THREADS, 0, st>>>(pv, slots, pos, n_tok, layer_begin, layer_count, per, in_layer_stride,
+                                     static_cast<const __nv_bfloat16 *>(k_new), static_cast<const __nv_bfloat16 *>(v_new), form ? *form : none);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv4_append_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                  const void *v_new, const RopeForm *form, cudaStream_t st, int64_t *launches) {
+  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const auto launch = n <= kPagesSmall ? launch_append_pages<kPagesSmall> : launch_append_pages<kPagesLarge>;
+    const cudaError_t e = launch(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok,
+                                 v + done * tok, form, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_kv4_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
+                                int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st,
+                                int64_t *launches) {
+  __nv_bfloat16 *k = static_cast<__nv_bfloat16 *>(k_out), *v = static_cast<__nv_bfloat16 *>(v_out);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const auto launch = n <= kPagesSmall ? launch_read_pages<kPagesSmall> : launch_read_pages<kPagesLarge>;
+    const cudaError_t e = launch(pv, pages, n, cnt, first_offset, layer_begin, layer_count, out_layer_stride, k + done * tok, v + done * tok, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace pasta

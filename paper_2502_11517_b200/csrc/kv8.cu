@@ -17,27 +17,13 @@
 
 #include "device_common.cuh"
 #include "kernels.hpp"
+#include "page_run.cuh"
+#include "rope_form.cuh"
 
 namespace pasta {
 
 namespace {
 
-constexpr int A_THREADS = 256, A_WARPS = A_THREADS / 32;
-
-// Rotation by angle i = f[i] times the position, f[i] = theta^(-2i/D); (c1[i], s1[i]) is the rotation by one position.
-struct Freqs { double f[64], c1[64], s1[64]; };
-// The pages of a run, as kernel arguments (a run needs no copy to the device before it); two sizes, since every launch
-// carries the whole array.
-template <int N> struct PageList { int32_t page[N]; };
-constexpr int kPagesSmall = 64, kPagesLarge = 2048;
-
-// Sines and cosines are kept times 2^896, and a bf16 number becomes the 64-bit number whose exponent field is its own: that
-// is the number times 2^-896, subnormal or not, for two integer instructions in place of a conversion (measured: 17 cycles
-// per warp for a conversion there and back, 2 for a multiplication).  Infinities and NaN are sorted out before.
-constexpr double kTurnScale = 0x1p896;
-__device__ __forceinline__ double scaled_down(uint32_t bits) {       // bits: fp32 bits of a bf16 number
-  return __hiloint2double((static_cast<int>(bits) >> 3) & 0x8fffffff, 0);
-}
 
 // exponent of the scale for a largest magnitude given by its fp32 bits (finite)
 __device__ __forceinline__ int scale_exp(uint32_t amax_bits) {
@@ -71,19 +57,14 @@ __device__ __forceinline__ int grow_scale(uint8_t *block, int8_t *scale, int kv,
   return e;
 }
 
-// Rows of one layer on their way into L2 while the CTA works on something else (16-byte aligned, as the loads require).
-__device__ __forceinline__ void prefetch_rows(const __nv_bfloat16 *k_new, const __nv_bfloat16 *v_new, int64_t at, int bytes) {
-  if (threadIdx.x < 2)
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((threadIdx.x ? v_new : k_new) + at), "r"(bytes) : "memory");
-}
-
 // The new tokens that fall into one page (rows off0 .. off0 + cnt - 1 of it), layers ll .. ll_end - 1, by one CTA: a warp takes
 // one (kv head, K or V) at a time, holds the group's elements in registers, finds their largest magnitude, and writes the
 // codes, so every element is read once.  turn: (cos, sin) of token r, angle i = 8 c + e at r * H + e * (H / 8) + c.
-template <int D, bool kRope>
+// kRope: 0 no rotation, 1 the first half of a row paired with the second, 2 any form.
+template <int D, int kRope>
 __device__ __forceinline__ void append_page(const PoolView &pv, int page, int off0, int first, int cnt, int layer_begin, int ll, int ll_end,
                                             int64_t in_layer_stride, const __nv_bfloat16 *__restrict__ k_new,
-                                            const __nv_bfloat16 *__restrict__ v_new, const double2 *turn) {
+                                            const __nv_bfloat16 *__restrict__ v_new, const RopeForm &form, const double2 *turn) {
   constexpr int H = D / 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int Hkv = pv.n_kv_heads;
@@ -101,13 +82,21 @@ __device__ __forceinline__ void append_page(const PoolView &pv, int page, int of
         // a lane holds the 8 elements of chunk c of the low half and the 8 they pair with in the high half
         constexpr int LPT = D / 16, TPI = 32 / LPT, NI = PASTA_PAGE / TPI;
         const int c = lane % LPT;
+        const int c_lo = kRope == 2 ? rope_chunk_a(form, c) : c, c_hi = kRope == 2 ? rope_chunk_b(form, c) : c + LPT;
+        const bool alternate = kRope == 2 && form.interleaved && c < form.slots;
         float y[NI][16], top = 0.f;
 #pragma unroll
         for (int it = 0; it < NI; ++it) {
           const int r = it * TPI + lane / LPT;
           if (r < cnt) {
             const uint4 *row = reinterpret_cast<const uint4 *>(src + static_cast<int64_t>(r) * Hkv * D);
-            const uint4 lo4 = __ldg(row + c), hi4 = __ldg(row + c + LPT);
+            uint4 lo4 = __ldg(row + c_lo), hi4 = __ldg(row + c_hi);
+            if constexpr (kRope == 2) {
+              if (chunk_not_finite(lo4) || chunk_not_finite(hi4)) { bad = true; rope_clean(lo4, hi4, alternate, c < form.slots); }
+              float z[16];
+              rope_slot<D>(lo4, hi4, alternate, turn + r * H, c, z);
+              rope_unslot(z, alternate, y[it], y[it] + 8);
+            } else {
             uint32_t lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
             uint32_t m2 = 0;
 #pragma unroll
@@ -129,6 +118,7 @@ __device__ __forceinline__ void append_page(const PoolView &pv, int page, int of
               const double b = scaled_down((e & 1) ? hi[e >> 1] & 0xffff0000u : hi[e >> 1] << 16);
               y[it][e] = static_cast<float>(a * t.x - b * t.y);
               y[it][8 + e] = static_cast<float>(b * t.x + a * t.y);
+            }
             }
           } else {
 #pragma unroll
@@ -156,7 +146,7 @@ __device__ __forceinline__ void append_page(const PoolView &pv, int page, int of
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const float *z = y[it] + 8 * half;
-              const int c8 = c + half * LPT;            // 8-element chunk of the row
+              const int c8 = half ? c_hi : c_lo;        // 8-element chunk of the row
               *reinterpret_cast<uint2 *>(block + kv8_chunk_offset<D>(0, off0 + r, c8 >> 1) + (c8 & 1) * 8) =
                   make_uint2(e4m3x4(z[0] * inv, z[1] * inv, z[2] * inv, z[3] * inv),
                              e4m3x4(z[4] * inv, z[5] * inv, z[6] * inv, z[7] * inv));
@@ -209,11 +199,11 @@ __device__ __forceinline__ void append_page(const PoolView &pv, int page, int of
 // Tokens of a step: slots[2 i], slots[2 i + 1] are token i's page and row.  One CTA per group of tokens that are neighbours in
 // one page (the CTA of a group's first token takes it) and slice of the layers; the sines and cosines (64 bits) are worked
 // out once per CTA for all heads and layers.
-template <int D, bool kRope>
+template <int D, int kRope>
 __global__ void __launch_bounds__(A_THREADS, kRope ? 2 : 3)
 kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t n_tok,
                   int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
-                  const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ Freqs freqs) {
+                  const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm freqs) {
   constexpr int H = D / 2;
   __shared__ double2 turn[kRope ? PASTA_PAGE * H : 1];
   grid_launch_dependents();
@@ -228,7 +218,11 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
     if (tid == 0) report(pv.status, PASTA_ERR_DEVICE_CHECK);
     return;
   }
-  if (kRope) {
+  if (kRope == 2) {
+    for (int x = tid; x < cnt * H; x += A_THREADS)
+      turn[x / H * H + turn_at<D>(x % H)] = turn_of(freqs, x % H, pos[first + x / H]);
+    __syncthreads();
+  } else if (kRope) {
     for (int x = tid; x < cnt * H; x += A_THREADS) {
       const int r = x / H, i = x % H;
       double sn, cs;
@@ -238,17 +232,17 @@ kv8_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
     __syncthreads();
   }
   const int ll = blockIdx.y * layers_per_cta;
-  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, turn);
+  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, freqs, turn);
 }
 
 // A run: n_tok tokens of one stream at consecutive positions, the first at row first_offset of the first page.  One CTA per
 // page and slice of the layers.  A thread works out the sine and cosine of one angle at every fourth token and turns it on by
 // one position at a time for the three behind it: three products, each good to a few times 2^-53.
-template <int D, bool kRope, int N>
+template <int D, int kRope, int N>
 __global__ void __launch_bounds__(A_THREADS, kRope ? 2 : 3)
 kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
                       int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
-                      const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ Freqs freqs) {
+                      const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm freqs) {
   constexpr int H = D / 2;
   __shared__ double2 turn[kRope ? PASTA_PAGE * H : 1];
   grid_launch_dependents();
@@ -262,7 +256,10 @@ kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, in
   }
   const int ll = blockIdx.y * layers_per_cta;
   prefetch_rows(k_new, v_new, ll * in_layer_stride + static_cast<int64_t>(first) * pv.n_kv_heads * D, cnt * pv.n_kv_heads * D * 2);
-  if (kRope) {
+  if (kRope == 2) {
+    turns_of_run<D, A_THREADS>(freqs, pos0 + first, cnt, turn);
+    __syncthreads();
+  } else if (kRope) {
     for (int x = tid; x < PASTA_PAGE / 4 * H; x += A_THREADS) {
       const int r = x / H * 4, i = x % H;
       double2 *at = turn + r * H + (i & 7) * (H / 8) + (i >> 3);
@@ -281,7 +278,7 @@ kv8_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, in
     }
     __syncthreads();
   }
-  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, turn);
+  append_page<D, kRope>(pv, page, off0, first, cnt, layer_begin, ll, min(layer_count, ll + layers_per_cta), in_layer_stride, k_new, v_new, freqs, turn);
 }
 
 // A run read back: one CTA per page and layer (blockIdx.y), a warp per (kv head, K or V); a lane turns 16 codes into 32 bytes.
@@ -334,50 +331,21 @@ kv8_read_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t 
   }
 }
 
-// the frequencies of a theta, worked out again only when it changes (one table per host thread)
-const Freqs &freqs_of(double theta, int head_dim) {
-  static thread_local Freqs fr;
-  static thread_local double of = 0;
-  static thread_local int dim = 0;
-  if (of != theta || dim != head_dim) {
-    for (int i = 0; i < head_dim / 2; ++i) {
-      fr.f[i] = std::exp2(-2.0 * i / head_dim * std::log2(theta));
-      fr.c1[i] = std::cos(fr.f[i]);
-      fr.s1[i] = std::sin(fr.f[i]);
-    }
-    of = theta;
-    dim = head_dim;
-  }
-  return fr;
-}
-
-// layers per CTA: all layers of a page in one CTA share its sines and cosines; split only as far as the GPU has to be filled
-int layers_per_cta(int groups, int layer_count) {
-  const int want = 148 * 2;          // (twice as many: 35.4 against 33.3 us for 64 pages of 8 layers with rotation)
-  const int slices = std::min(layer_count, std::max(1, (want + groups - 1) / groups));
-  return (layer_count + slices - 1) / slices;
-}
-
-template <int N>
-PageList<N> list_of(const int32_t *pages, int n) {
-  PageList<N> list;
-  std::copy(pages, pages + n, list.page);
-  return list;
-}
-
 template <int N>
 cudaError_t launch_append_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
                                 int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const __nv_bfloat16 *k,
-                                const __nv_bfloat16 *v, double theta, cudaStream_t st) {
+                                const __nv_bfloat16 *v, const RopeForm *form, cudaStream_t st) {
   const PageList<N> list = list_of<N>(pages, n_pages);
   const int per = layers_per_cta(n_pages, layer_count);
   const dim3 grid(n_pages, (layer_count + per - 1) / per);
-  const Freqs &fr = freqs_of(theta > 0 ? theta : 2.0, pv.head_dim);
+  static const RopeForm none{};
+  const RopeForm &fr = form ? *form : none;
+  const int rope = !form ? 0 : rope_form_is_plain(fr, pv.head_dim) ? 1 : 2;
 #define PASTA_A8(DD, RR)                                                                                                \
   kv8_append_run_kernel<DD, RR, N><<<grid, A_THREADS, 0, st>>>(pv, list, pos0, n_tok, first_offset, layer_begin, layer_count, per, \
                                                                in_layer_stride, k, v, fr)
-  if (pv.head_dim == 128) { if (theta > 0) PASTA_A8(128, true); else PASTA_A8(128, false); }
-  else { if (theta > 0) PASTA_A8(64, true); else PASTA_A8(64, false); }
+  if (pv.head_dim == 128) { if (rope == 2) PASTA_A8(128, 2); else if (rope) PASTA_A8(128, 1); else PASTA_A8(128, 0); }
+  else { if (rope == 2) PASTA_A8(64, 2); else if (rope) PASTA_A8(64, 1); else PASTA_A8(64, 0); }
 #undef PASTA_A8
   return cudaGetLastError();
 }
@@ -396,32 +364,34 @@ cudaError_t launch_read_pages(const PoolView &pv, const int32_t *pages, int n_pa
 }  // namespace
 
 cudaError_t launch_kv8_append(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
-                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new, double theta,
+                              int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new, const RopeForm *form,
                               cudaStream_t st) {
   if (n_tok == 0 || layer_count == 0) return cudaSuccess;
   const int per = layers_per_cta(n_tok, layer_count);
   const dim3 grid(n_tok, (layer_count + per - 1) / per);
-  const Freqs &fr = freqs_of(theta > 0 ? theta : 2.0, pv.head_dim);
+  static const RopeForm none{};
+  const RopeForm &fr = form ? *form : none;
+  const int rope = !form ? 0 : rope_form_is_plain(fr, pv.head_dim) ? 1 : 2;
   const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
 #define PASTA_A8(DD, RR) \
   kv8_append_kernel<DD, RR><<<grid, A_THREADS, 0, st>>>(pv, slots, pos, n_tok, layer_begin, layer_count, per, in_layer_stride, k, v, fr)
-  if (pv.head_dim == 128) { if (theta > 0) PASTA_A8(128, true); else PASTA_A8(128, false); }
-  else { if (theta > 0) PASTA_A8(64, true); else PASTA_A8(64, false); }
+  if (pv.head_dim == 128) { if (rope == 2) PASTA_A8(128, 2); else if (rope) PASTA_A8(128, 1); else PASTA_A8(128, 0); }
+  else { if (rope == 2) PASTA_A8(64, 2); else if (rope) PASTA_A8(64, 1); else PASTA_A8(64, 0); }
 #undef PASTA_A8
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv8_append_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
                                   int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
-                                  const void *v_new, double theta, cudaStream_t st, int64_t *launches) {
+                                  const void *v_new, const RopeForm *form, cudaStream_t st, int64_t *launches) {
   const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
   const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
   for (int32_t done = 0; done < n_tok;) {
     const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
     const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
     const cudaError_t e = n <= kPagesSmall
-        ? launch_append_pages<kPagesSmall>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, theta, st)
-        : launch_append_pages<kPagesLarge>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, theta, st);
+        ? launch_append_pages<kPagesSmall>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, form, st)
+        : launch_append_pages<kPagesLarge>(pv, pages, n, pos0 + done, cnt, first_offset, layer_begin, layer_count, in_layer_stride, k + done * tok, v + done * tok, form, st);
     if (e != cudaSuccess) return e;
     *launches += 1;
     pages += n;

@@ -44,7 +44,7 @@ extern "C" pasta_status_t pasta_decode_attn_noalloc(pasta_pool_t *pool, int32_t 
   if (layer < 0 || layer >= n_layers) return PASTA_ERR_INVALID_ARG;
   if (hdr.w[PH_N_QUERIES] == 0) return PASTA_OK;                   // an empty step needs no buffers, as in pasta_decode_attn
   if (!q || !out || !(scale >= 0.f)) return PASTA_ERR_INVALID_ARG;
-  if (pv.kv8 && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)) return PASTA_ERR_INVALID_ARG;
+  if ((pv.kv8 || pv.kv4) && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)) return PASTA_ERR_INVALID_ARG;
   if (hdr.w[PH_ROWS] > kMaxRows) return PASTA_ERR_CAPACITY;       // this step needs more partial rows than the array holds
   int current = -1;
   if (cudaGetDevice(&current) != cudaSuccess || current != device || device < 0 || device >= kMaxDevices)
