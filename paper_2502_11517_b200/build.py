@@ -10,7 +10,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpasta.so")
-SOURCES = ["pool.cpp", "plan.cpp", "kernels.cu", "attn_tensor.cu", "kv8.cu", "attn_kv8.cu", "attn_kv8_tensor.cu", "kv4.cu", "rope.cu", "api.cu", "noalloc.cu", "dense_mask.cu"]
+SOURCES = ["pool.cpp", "plan.cpp", "kernels.cu", "attn_tensor.cu", "kv8.cu", "attn_kv8.cu", "attn_kv8_tensor.cu", "kv4.cu", "attn_kv4.cu", "rope.cu", "api.cu", "noalloc.cu", "dense_mask.cu"]
 HEADERS = ["pool.hpp", "plan.hpp", "pasta_plan.h", "device_common.cuh", "tensor_common.cuh", "page_run.cuh", "rope_form.cuh", "kernels.hpp",
            os.path.join("..", "..", "include", "pasta.h")]
 

@@ -216,7 +216,7 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.max_rows = p->d.max_rows;
   l.max_words = p->d.max_words;
   l.grid = p->sm_count;
-  l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & PASTA_FLAG_KV_FP8)) && !(p->cfg.flags & PASTA_FLAG_KV_INT4) &&
+  l.tensor_path = (p->cfg.head_dim == 128 || (p->cfg.flags & (PASTA_FLAG_KV_FP8 | PASTA_FLAG_KV_INT4))) &&
                   !(p->cfg.flags & PASTA_FLAG_NO_TENSOR_PATH) && tensor_path_available();
   l.tail_percent = p->tail_percent;
   if ((p->cfg.flags & PASTA_FLAG_KV_FP8) && p->cfg.head_dim == 64) {      // that kernel runs one CTA per unit, six to an SM

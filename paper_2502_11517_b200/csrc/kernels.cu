@@ -756,7 +756,7 @@ merge_kernel(PoolView pv, int32_t n_queries, int32_t layer_count, int32_t off_qu
 
 cudaError_t launch_attn_units(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count, const void *q,
                               float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st) {
-  const auto launch = !pv.kv8 ? launch_attn_tensor : pv.head_dim == 128 ? launch_attn_kv8_tensor : launch_attn_kv8;
+  const auto launch = pv.kv4 ? launch_attn_kv4 : !pv.kv8 ? launch_attn_tensor : pv.head_dim == 128 ? launch_attn_kv8_tensor : launch_attn_kv8;
   return launch(pv, h, layer_begin, layer_count, q, scale_log2, out, lse, out_bf16, st);
 }
 

@@ -71,6 +71,9 @@ cudaError_t launch_attn_kv8_tensor(const PoolView &pv, const PlanHeader &h, int3
 // K2 of an 8-bit pool, head_dim 64: every unit of the plan's t-requests, one CTA each
 cudaError_t launch_attn_kv8(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
                             const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
+// K2 of a 4-bit pool: tensor-core kernel, persistent CTAs like launch_attn_tensor's
+cudaError_t launch_attn_kv4(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count,
+                            const void *q, float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
 // the kernel that serves this pool's t-units and d-units
 cudaError_t launch_attn_units(const PoolView &pv, const PlanHeader &h, int32_t layer_begin, int32_t layer_count, const void *q,
                               float scale_log2, void *out, float *lse, bool out_bf16, cudaStream_t st);
