@@ -42,7 +42,8 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
   if (c.max_requests < 1 || c.max_threads_per_request < 1 || c.max_segments_per_thread < 1) return PASTA_ERR_INVALID_ARG;
   if (c.max_step_queries < 0 || c.max_partial_rows < 0 || c.max_layers_per_launch < 0) return PASTA_ERR_INVALID_ARG;
   const int grid = 160;   // upper bound on CTAs of the tensor-core kernel, for sizing only
-  const int slots = (c.flags & PASTA_FLAG_KV_FP8) && c.head_dim == 64 ? 6 * grid : grid;      // and on pieces that cutting adds
+  // and on pieces that cutting adds
+  const int slots = (c.flags & PASTA_FLAG_KV_INT4) ? 4 * grid : (c.flags & PASTA_FLAG_KV_FP8) && c.head_dim == 64 ? 6 * grid : grid;
   d->max_queries = c.max_step_queries ? c.max_step_queries
                                       : static_cast<int32_t>(std::min<int64_t>(int64_t(c.max_requests) * 17, 1 << 20));
   // units of the shared tail, at most: its share of all tiles in pieces of kTailTiles, plus one ragged piece per run
@@ -51,7 +52,7 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
   const int64_t unit_rows = std::min<int64_t>(PASTA_MAX_ROWS, int64_t(c.max_threads_per_request) * d->group);
   d->max_rows = c.max_partial_rows ? c.max_partial_rows
                                    : static_cast<int32_t>(std::min<int64_t>(
-                                         int64_t(d->max_queries) * c.n_q_heads * 8 + int64_t(grid) * PASTA_MAX_ROWS +
+                                         int64_t(d->max_queries) * c.n_q_heads * 8 + int64_t((c.flags & PASTA_FLAG_KV_INT4) ? 2 * grid : grid) * PASTA_MAX_ROWS +
                                              tail_units * unit_rows, 1 << 28));
   d->layers_per_launch = c.max_layers_per_launch ? std::min(c.max_layers_per_launch, c.n_layers)
                                                  : std::min(c.n_layers, 8);
@@ -225,6 +226,7 @@ PlanLimits limits_of(const pasta_pool *p) {
     l.even_cuts = true;
   }
   l.tail_tiles = p->tail_tiles;
+  l.kv4 = (p->cfg.flags & PASTA_FLAG_KV_INT4) != 0;
   return l;
 }
 

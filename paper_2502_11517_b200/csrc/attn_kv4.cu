@@ -14,77 +14,77 @@
 // of the tensor pipe is spent on N columns instead of 128.
 //
 // head_dim 64 has 64 channels for the 128 rows of O^T's MMA, so V^T's upper 64 rows are the channels of the tile's second 64
-// tokens, and the weights of those tokens are N further columns: [V_0; V_1] [P_0 | P_1], K = 64.  The two diagonal blocks are
-// what is wanted and are added up at a unit's end; the other two cost nothing that matters at these N.
+// tokens, and the weights of those tokens are N further columns: [V_0; V_1] [P_0 | P_1], K = 64 (the columns of P_0 and P_1 eight
+// at a time in turn).  The two diagonal blocks are what is wanted and are added up at a unit's end; the other two cost nothing
+// that matters at these N.
 //
-// The reference of a row is shared by the tokens of a tile, that is by the four warps of a softmax group, so raising it takes
-// an agreement: every tile the group votes whether some score lies more than 2^R_SLACK above its row's reference (also: whether a
-// row sees its first token), and only then are the rows' maxima worked out, and O and l brought to the new reference.
+// What bounds it: instructions (some 250 per warp and tile of 128 tokens for K's codes, 330 for V's, 35 for every 8 rows of the
+// softmax, on each of the four schedulers) against the 785 cycles that the tile's 18 KB take at the measured copy bandwidth.  A warp
+// alone issues one every four or five cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so several CTAs share an SM and
+// fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows,
+// two of 256 threads and 256 columns for up to 80 (64 at head_dim 64), one above.
+// Every warp does everything in turn.  (Measured, with the roles on warps of their own and one CTA to an SM, in three forms:
+// 290 to 390 us for the batched case and 310 to 410 for the long prefix; hand-overs and the four programs' instruction fetches took
+// more than the work.)
 //
-// Warp roles (640 threads): warp 0 producer (bulk copies), warp 1 MMA issue (one thread, Q.K^T one tile ahead of P.V), warps 2-3
-// build the Q operand, warps 4-7 turn K's codes into the A operand, warps 8-11 V's, warps 12-15 and 16-19 are two softmax
-// groups, which take the rows in turn, eight at a time.  Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains
-// and leaves.
+// A CTA walks its units as those of attn_tensor.cu do.  TMEM holds one operand (K, then V in its place), the scores and O^T.
+// The reference of a row is shared by the CTA's warps and raised only when a score exceeds it by more than 2^R_SLACK: the CTA
+// votes on that with the barrier that publishes the weights, and only then the rows' maxima are worked out and O and l brought to them.
+// With 256 threads the two halves of the CTA share the work on every token, channel and eight rows.
+// Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
+#include <type_traits>
+
 #include "tensor_common.cuh"
 
 namespace pasta {
 
 namespace {
 
-constexpr int U_THREADS = 640;
-constexpr int U_RING = 32;                       // unit records and tiles' page metas kept published: more than the pipeline is deep
-constexpr int U_INIT = 4;                        // units whose rows' first references are kept
 constexpr float R_SLACK = 10.f;                  // weights are at most 2^10 (bf16 and fp32 keep their precision at any size)
 constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing
 
 // Sizes of one build: head_dim D, at most NMAX stacked rows.
 template <int D, int NMAX>
 struct U {
-  static constexpr int CHUNKS = NMAX / 16;                        // groups of 8 rows per softmax group
+  static constexpr int H = NMAX <= 32 ? 1 : 2, THREADS = 128 * H; // threads that share a token
+  static constexpr int CHUNKS = NMAX / 8 / H;                     // groups of 8 rows per thread: chunk H i + h for half h
   static constexpr int OW = D == 128 ? 1 : 2;                     // blocks of N columns of an accumulator
   static constexpr int KSTEPS = D / 16, VSTEPS = D == 128 ? 8 : 4;
-  static constexpr int KW = D / 2, VW = VSTEPS * 8;               // TMEM columns of a K and a V operand
-  // how many of each fit 512 columns
-  static constexpr int SB = D == 64 && NMAX > 96 ? 1 : 2, OB = NMAX > 64 ? 1 : 2;
-  static constexpr int KB = D == 128 && NMAX > 96 ? 1 : 2, VB = D == 128 && NMAX > 64 ? 1 : 2;
-  static constexpr int QB = NMAX > 64 ? 1 : 2;
-  static constexpr uint32_t COL_S = 0, COL_O = COL_S + SB * NMAX, COL_K = COL_O + OB * OW * NMAX, COL_V = COL_K + KB * KW;
-  static_assert(COL_V + VB * VW <= TMEM_COLS, "tensor memory budget");
+  static constexpr uint32_t COL_A = 0, COL_S = D / 2, COL_O = COL_S + NMAX;      // (V's operand is D / 2 columns wide, too)
+  static constexpr uint32_t COLS_USED = COL_O + OW * NMAX, COLS = COLS_USED <= 128 ? 128 : COLS_USED <= 256 ? 256 : 512;
+  static_assert(COLS_USED <= 512, "tensor memory budget");
+  static constexpr int RESIDENT = 512 / COLS;                     // CTAs on an SM
   static constexpr int BLOCK = kv4_block_bytes(D), STAGE_BYTES = PASTA_TILE_PAGES * BLOCK;
-  static constexpr int ATOMS = (OW * NMAX + 63) / 64;             // 64-column atoms of a weight row
-  static constexpr int P_BYTES = (D == 128 ? 16 : 8) * ATOMS * 1024;
+  static constexpr int STAGES = D == 128 && NMAX <= 32 ? 2 : RESIDENT > 1 ? 3 : 6;
+  // a row of weights: 128 bytes per 64 columns, or 64 bytes where they are at most 32 (so that four CTAs fit)
+  static constexpr bool NARROW = OW * NMAX <= 32;
+  static constexpr int ATOMS = (OW * NMAX + 63) / 64, P_GROUP = NARROW ? 512 : ATOMS * 1024;      // bytes of 8 rows
+  static constexpr int P_BYTES = (D == 128 ? 16 : 8) * P_GROUP;
   static constexpr int Q_BYTES = NMAX * D * 2;
-  static constexpr int SUM_BYTES = D == 64 ? NMAX * 64 * 4 : 0;   // where the halves of accumulators are added up
-  static constexpr int STAGES = D == 64 ? 10 : NMAX > 64 ? 6 : 7;
+  // (head_dim 64: the halves of accumulators are added up where the weights were)
+  static_assert(D == 128 || NMAX * 64 * 4 <= P_BYTES, "room for 64 channels of every row");
   static constexpr int OFF_Q = 0;
-  static constexpr int OFF_P = OFF_Q + QB * Q_BYTES;
-  static constexpr int OFF_STAGE = OFF_P + 2 * P_BYTES;
-  static constexpr int OFF_SUM = OFF_STAGE + STAGES * STAGE_BYTES;
-  static constexpr int OFF_BAR = OFF_SUM + SUM_BYTES;
-  // barriers (8 bytes each)
-  static constexpr int B_FULL = 0, B_EMPTY = B_FULL + STAGES, B_KFULL = B_EMPTY + STAGES, B_KFREE = B_KFULL + KB,
-                       B_VFULL = B_KFREE + KB, B_VFREE = B_VFULL + VB, B_SFULL = B_VFREE + VB, B_SFREE = B_SFULL + SB,
-                       B_PFULL = B_SFREE + SB, B_PFREE = B_PFULL + 2, B_QFULL = B_PFREE + 2, B_QFREE = B_QFULL + QB,
-                       B_OFULL = B_QFREE + QB, B_OFREE = B_OFULL + OB,
-                       B_SYNC = B_OFREE + OB,                       // [group] where a softmax group meets
-                       B_DRAIN = B_SYNC + 2,                        // only used when a role gave up
-                       B_COUNT = B_DRAIN + 1;
-  static constexpr int OFF_META = OFF_BAR + 8 * ((B_COUNT + 1) & ~1);        // [U_RING] 8 page metas
-  static constexpr int OFF_MISC = OFF_META + U_RING * 32;                  // tmem base, abort flag, shared units taken, their records
-  static constexpr int OFF_INIT = OFF_MISC + 16 + 64 * U_RING;             // [U_INIT][NMAX] rows' first references (negated)
-  static constexpr int OFF_REF = OFF_INIT + U_INIT * NMAX * 4;             // [NMAX] references (negated)
-  static constexpr int OFF_FACT = OFF_REF + NMAX * 4;                      // [NMAX] what a raised reference multiplies O and l by; 1 / l
-  static constexpr int OFF_WARP = OFF_FACT + NMAX * 4;                     // [4][NMAX] a warp's maxima, or sums
-  static constexpr int OFF_VOTE = OFF_WARP + 4 * NMAX * 4;                 // [group][4] votes of the latest tiles
-  static constexpr int SMEM_BYTES = OFF_VOTE + 32 + 1024;                  // slack to align the base to 1024
-  static_assert(SMEM_BYTES <= 232448, "shared memory budget");
-  static_assert(OFF_META % 16 == 0 && OFF_MISC % 16 == 0 && OFF_REF % 16 == 0, "read as vectors");
-  static_assert(STAGES + KB + SB + 4 <= U_RING, "records are overwritten only after their last reader");
+  static constexpr int OFF_P = OFF_Q + Q_BYTES;
+  static constexpr int OFF_STAGE = OFF_P + P_BYTES;
+  static constexpr int OFF_BAR = OFF_STAGE + STAGES * STAGE_BYTES;       // FULL[STAGES], QK, PV, DRAIN
+  static constexpr int B_FULL = 0, B_QK = STAGES, B_PV = B_QK + 1, B_DRAIN = B_PV + 1, B_COUNT = B_DRAIN + 1;
+  static constexpr int OFF_META = OFF_BAR + 8 * ((B_COUNT + 1) & ~1);    // [STAGES] 8 page metas
+  static constexpr int OFF_MISC = OFF_META + STAGES * 32;                // tmem base, abort flag, -, -, the unit's record
+  static constexpr int OFF_REF = OFF_MISC + 16 + 64;                     // [NMAX] references (negated)
+  static constexpr int OFF_FACT = OFF_REF + NMAX * 4;                    // [NMAX] what a raised reference multiplies O and l by; 1 / l
+  static constexpr int OFF_WARP = OFF_FACT + NMAX * 4;                   // [4][NMAX] a warp's maxima, or sums
+  static constexpr int SMEM_BYTES = OFF_WARP + 4 * NMAX * 4 + 1024;      // slack to align the base to 1024
+  static_assert((SMEM_BYTES + 1024) * RESIDENT <= 233472, "shared memory budget");
+  static_assert(OFF_P % 1024 == 0 && OFF_STAGE % 16 == 0 && OFF_META % 16 == 0 && OFF_MISC % 16 == 0, "alignment");
 };
 
 constexpr uint32_t IDESC4 = (1u << 4) | (1u << 7) | (1u << 10) | IDESC_M128;      // D fp32, A and B bf16, M = 128
 constexpr uint32_t IDESC4_PV = IDESC4 | (1u << 16);                                // B (= P^T) MN-major
 
+// descriptor of the weights where their rows are 64 bytes: the 64-byte swizzle
+__device__ __forceinline__ uint64_t smem_desc64(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+  return (smem_desc(addr, lbo_bytes, sbo_bytes) & ~(7ull << 61)) | (4ull << 61);
+}
 __device__ __forceinline__ void tmem_ld8_issue(uint32_t taddr, uint32_t *r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
@@ -97,6 +97,20 @@ __device__ __forceinline__ void tmem_ld_order8(uint32_t *r) { asm volatile("" : 
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+// {l0, l1} += the two bf16 numbers of w
+__device__ __forceinline__ void add_bf16x2(float &l0, float &l1, uint32_t w) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}" : "+f"(l0), "+f"(l1) : "r"(w));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
 }
 __device__ __forceinline__ float warp_max(float x) {
   float y;
@@ -124,10 +138,22 @@ __device__ __forceinline__ float warp_sum8(const float *v, int lane) {
   return t + __shfl_xor_sync(0xffffffffu, t, 1);
 }
 
+// Waits for a phase, or for some thread of the CTA to have given up; sets the flag when the time is up.  Whole warps.
+__device__ __forceinline__ void cta_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+  const long long t0 = clock64();
+#pragma unroll 1
+  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+    if (clock64() - t0 > limit) *abort_flag = 1;
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return;
+  }
+}
+
 template <int D, int NMAX, bool kCap>
-__global__ void __launch_bounds__(U_THREADS, 1)
+__global__ void __launch_bounds__(U<D, NMAX>::THREADS, U<D, NMAX>::RESIDENT)
 attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) {
   using L = U<D, NMAX>;
+  constexpr int H = L::H;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -138,31 +164,26 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   const uint32_t bar = base + L::OFF_BAR;
   int32_t *meta_s = reinterpret_cast<int32_t *>(sm + L::OFF_META);
   uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);
+  int32_t *unit_s = reinterpret_cast<int32_t *>(misc + 4);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(misc + 1);
-  float *init_s = reinterpret_cast<float *>(sm + L::OFF_INIT);
+  float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
+  float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
   const int32_t *plan = pv.plan;
 
   if (tid == 0) {
-    for (int s = 0; s < L::STAGES; ++s) { mbar_init(bar + 8 * (L::B_FULL + s), 1); mbar_init(bar + 8 * (L::B_EMPTY + s), 8); }
-    for (int b = 0; b < L::KB; ++b) { mbar_init(bar + 8 * (L::B_KFULL + b), 4); mbar_init(bar + 8 * (L::B_KFREE + b), 1); }
-    for (int b = 0; b < L::VB; ++b) { mbar_init(bar + 8 * (L::B_VFULL + b), 4); mbar_init(bar + 8 * (L::B_VFREE + b), 1); }
-    for (int b = 0; b < L::SB; ++b) { mbar_init(bar + 8 * (L::B_SFULL + b), 1); mbar_init(bar + 8 * (L::B_SFREE + b), 8); }
-    for (int b = 0; b < 2; ++b) { mbar_init(bar + 8 * (L::B_PFULL + b), 8); mbar_init(bar + 8 * (L::B_PFREE + b), 1); }
-    for (int b = 0; b < L::QB; ++b) { mbar_init(bar + 8 * (L::B_QFULL + b), 2); mbar_init(bar + 8 * (L::B_QFREE + b), 1); }
-    for (int b = 0; b < L::OB; ++b) { mbar_init(bar + 8 * (L::B_OFULL + b), 1); mbar_init(bar + 8 * (L::B_OFREE + b), 8); }
-    for (int b = 0; b < 2; ++b) mbar_init(bar + 8 * (L::B_SYNC + b), 4);
-    mbar_init(bar + 8 * L::B_DRAIN, 1);
+    for (int b = 0; b < L::B_COUNT; ++b) mbar_init(bar + 8 * b, b == L::B_DRAIN ? 4 : 1);
     misc[1] = 0;
-    misc[2] = 0;
-    for (int i = 0; i < 8; ++i) reinterpret_cast<int *>(sm + L::OFF_VOTE)[i] = 0;
     mbar_init_fence();
   }
   fence_proxy_async();
-  if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::OFF_MISC), "r"(TMEM_COLS)
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::OFF_MISC), "r"(L::COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // operand bytes that no copy fills meet zero weights, so they only have to be finite: page slots that a partial tile leaves empty
+  for (int i = tid; i < L::STAGES * L::STAGE_BYTES / 16; i += L::THREADS) reinterpret_cast<uint4 *>(sm + L::OFF_STAGE)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -171,136 +192,83 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   grid_launch_dependents();
   const int u0 = plan[a.off_tcta + 2 * blockIdx.x], u1 = plan[a.off_tcta + 2 * blockIdx.x + 1];
   const long long limit = pv.wait_limit;
-  uint32_t prod_it = 0;       // warp 0: tiles whose copies have been issued
-  volatile int *ring = reinterpret_cast<volatile int *>(misc + 2);
   int32_t *counter = pv.status + PASTA_STATUS_TAIL_COUNTER;
-  auto next = [&](Walk &w, bool whole_warp, bool &ok, UnitInfo &x, int &ll) {
-    return next_unit<false, true, U_RING>(w, a, plan, u0, u1, ring, counter, lane, whole_warp, abort_flag, limit, ok, x, ll);
-  };
-  auto rows16 = [&](const UnitInfo &x) { return ((x.n_threads << g_shift) + 15) & ~15; };
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  const int wq = warp & 3, half = warp >> 2;          // the quarter of TMEM this warp reaches, its half of the work
+  const int token = wq * 32 + lane;                   // as a thread of the scores; as one of V and O: channel `token` (head_dim 64: % 64)
+  const uint32_t lane_addr = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+  // test hook: held copies or MMAs, so that what waits for them runs into its limit
+  const bool no_copies = pv.debug_hold & 1, no_mma = pv.debug_hold & 2;
+  uint32_t it = 0, issued = 0;                        // tiles worked on and copied; MMA phases follow `it`
+  int ll = 0, u = u0;
 
-  // test hook: a held role goes straight to the tear-down, so that the roles waiting for it run into their limits
-  const int role = warp == 0 ? 0 : warp < 12 ? (warp == 1 || warp >= 4 ? 1 : 2) : 3 + ((warp - 12) >> 2);
-  if ((pv.debug_hold >> role) & 1) {
-  } else if (warp == 0) {
-    // ================================================================ producer
-    uint32_t it = 0;
-    bool ok = true;
-    uint64_t policy;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    Walk wk{0, u0, 0};
+  for (;;) {
+    // ---- the next unit: those assigned to the CTA, layer by layer, then those handed out at run time
     UnitInfo x;
-    int ll = 0;
-    while (ok && next_unit<true, true, U_RING>(wk, a, plan, u0, u1, ring, counter, lane, true, abort_flag, limit, ok, x, ll)) {
-      const uint8_t *kv_layer = pv.kv_base + (a.layer_begin + ll) * pv.layer_stride;
-      // page ids and metas of a batch of 4 tiles live in registers, a page per lane; the next batch's are asked for ahead
-      auto ask = [&](int tile, int &page, int &meta) {
-        page = 0;
-        meta = -1;
-        const int at = tile * PASTA_TILE_PAGES + lane;
-        if (at < x.n_pages && at < x.tile_end * PASTA_TILE_PAGES) {
-          page = plan[a.off_pages + x.page_off + at];
-          meta = plan[a.off_pmeta + x.page_off + at];
-        }
-      };
-      int page, meta, next_page, next_meta;
-      ask(x.tile_begin, page, meta);
-      ask(x.tile_begin + 4, next_page, next_meta);
-      for (int tile = x.tile_begin; tile < x.tile_end; ++tile, ++it) {
-        const int first = ((tile - x.tile_begin) & 3) * PASTA_TILE_PAGES, r = lane - first;
-        if (first == 0 && tile > x.tile_begin) {
-          page = next_page;
-          meta = next_meta;
-          ask(tile + 4, next_page, next_meta);
-        }
-        const int s = it % L::STAGES;
-        if (!warp_wait_or_abort(bar + 8 * (L::B_EMPTY + s), ((it / L::STAGES) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-        const int n_valid = min(PASTA_TILE_PAGES, x.n_pages - tile * PASTA_TILE_PAGES);
-        if (page < 0 || page >= pv.n_pages) { report(pv.status, PASTA_ERR_DEVICE_CHECK); page = 0; meta = -1; }
-        if (r >= 0 && r < PASTA_TILE_PAGES) meta_s[(it % U_RING) * PASTA_TILE_PAGES + r] = meta;
-        uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
-        if (it < L::STAGES && n_valid < PASTA_TILE_PAGES) {       // first use of this stage and some slots stay empty
-          uint4 *slot = reinterpret_cast<uint4 *>(stage + n_valid * L::BLOCK);
-          for (int i = lane; i < (PASTA_TILE_PAGES - n_valid) * (L::BLOCK / 16); i += 32) slot[i] = make_uint4(0, 0, 0, 0);
-          fence_proxy_async();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_expect_tx(bar + 8 * (L::B_FULL + s), n_valid * L::BLOCK);
-        __syncwarp();
-        if (r >= 0 && r < n_valid)
-          bulk_g2s_stream(base + L::OFF_STAGE + s * L::STAGE_BYTES + r * L::BLOCK,
-                          kv_layer + (static_cast<int64_t>(page) * pv.n_kv_heads + x.g) * L::BLOCK, L::BLOCK,
-                          bar + 8 * (L::B_FULL + s), policy);
-      }
+    int layer;
+    if (u0 < u1 && ll < a.layer_count) {
+      x = load_unit(plan, a.off_tunit, 0, u);
+      layer = ll;
+      if (++u == u1) { u = u0; ++ll; }
+    } else {
+      if (a.n_dunits == 0) break;
+      if (tid == 0) unit_s[0] = atomicAdd(counter, 1);
+      __syncthreads();
+      const int id = unit_s[0];
+      if (id >= a.n_dunits * a.layer_count) break;
+      layer = id / a.n_dunits;
+      x = load_unit(plan, a.off_dunit, 0, id - layer * a.n_dunits);
+      // (the word is written again behind the unit's barriers)
     }
-    prod_it = it;
-  } else if (warp == 1) {
-    // ================================================================ MMA issue (one thread)
-    if (lane == 0) {
-      uint32_t it = 0, uc = 0;
-      bool ok = true;
-      Walk wk{0, u0, 0};
-      UnitInfo x;
-      int ll = 0;
-      for (; ok && next(wk, false, ok, x, ll); ++uc) {
-        const int nt = x.tile_end - x.tile_begin;
-        const uint32_t n = rows16(x), qb = uc % L::QB, ob = uc % L::OB;
-        const uint32_t i_qk = IDESC4 | ((n >> 3) << 17), i_pv = IDESC4_PV | (((L::OW * n) >> 3) << 17);
-        if (!wait_or_abort(bar + 8 * (L::B_QFULL + qb), (uc / L::QB) & 1, abort_flag, limit)) { ok = false; break; }
-        for (int k = 0; k <= nt && ok; ++k) {
-          if (k < nt) {
-            // ---- S^T = K . Q^T for tile `it`
-            const uint32_t kb = it % L::KB, sb = it % L::SB;
-            if (!wait_or_abort(bar + 8 * (L::B_SFREE + sb), ((it / L::SB) & 1) ^ 1, abort_flag, limit) ||
-                !wait_or_abort(bar + 8 * (L::B_KFULL + kb), (it / L::KB) & 1, abort_flag, limit)) { ok = false; break; }
-            tc_fence_after();
-#pragma unroll
-            for (int ks = 0; ks < L::KSTEPS; ++ks)
-              mma_ts(tmem + L::COL_S + sb * NMAX, tmem + L::COL_K + kb * L::KW + ks * 8,
-                     smem_desc(base + L::OFF_Q + qb * L::Q_BYTES + (ks >> 2) * (NMAX * 128) + (ks & 3) * 32, 16, 1024), i_qk, ks > 0);
-            mma_commit(bar + 8 * (L::B_SFULL + sb));
-            mma_commit(bar + 8 * (L::B_KFREE + kb));
-            if (k == nt - 1) mma_commit(bar + 8 * (L::B_QFREE + qb));   // the Q operand may be replaced once these finish
-          }
-          if (k > 0) {
-            // ---- O^T += V^T . P^T for tile `it - 1` (when k == nt, `it` already points past it)
-            const uint32_t j = it - 1, vb = j % L::VB, pb = j & 1;
-            if (k == 1 && !wait_or_abort(bar + 8 * (L::B_OFREE + ob), ((uc / L::OB) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-            if (!wait_or_abort(bar + 8 * (L::B_VFULL + vb), (j / L::VB) & 1, abort_flag, limit) ||
-                !wait_or_abort(bar + 8 * (L::B_PFULL + pb), (j >> 1) & 1, abort_flag, limit)) { ok = false; break; }
-            tc_fence_after();
-#pragma unroll
-            for (int ks = 0; ks < L::VSTEPS; ++ks)
-              mma_ts(tmem + L::COL_O + ob * L::OW * NMAX, tmem + L::COL_V + vb * L::VW + ks * 8,
-                     smem_desc(base + L::OFF_P + pb * L::P_BYTES + ks * 2 * L::ATOMS * 1024, 1024, L::ATOMS * 1024), i_pv, (k > 1) || (ks > 0));
-            mma_commit(bar + 8 * (L::B_VFREE + vb));
-            mma_commit(bar + 8 * (L::B_PFREE + pb));
-            if (k == nt) mma_commit(bar + 8 * (L::B_OFULL + ob));
-          }
-          if (k < nt) ++it;
-        }
+    const int nt = x.tile_end - x.tile_begin;
+    const int rows = x.n_threads << g_shift, n = (rows + 15) & ~15;
+    const uint8_t *kv_head = pv.kv_base + (a.layer_begin + layer) * pv.layer_stride + static_cast<int64_t>(x.g) * L::BLOCK;
+    const bool fin = x.final_rows != 0;
+    // one tile's copies, by the first warp: a lane per page.  Its page id and meta were asked for a tile ahead.
+    int next_page = 0, next_meta = -1, asked = 0;
+    auto ask = [&]() {
+      next_page = 0;
+      next_meta = -1;
+      const int at = (x.tile_begin + asked) * PASTA_TILE_PAGES + lane;
+      if (lane < PASTA_TILE_PAGES && asked < nt && at < x.n_pages) {
+        next_page = plan[a.off_pages + x.page_off + at];
+        next_meta = plan[a.off_pmeta + x.page_off + at];
       }
+      ++asked;
+    };
+    auto copy = [&]() {
+      const int s = issued % L::STAGES;
+      const int n_valid = min(PASTA_TILE_PAGES, x.n_pages - (x.tile_begin + asked - 1) * PASTA_TILE_PAGES);
+      if (next_page < 0 || next_page >= pv.n_pages) { report(pv.status, PASTA_ERR_DEVICE_CHECK); next_page = 0; next_meta = -1; }
+      if (lane < PASTA_TILE_PAGES) meta_s[s * PASTA_TILE_PAGES + lane] = next_meta;
+      __syncwarp();
+      if (lane == 0) mbar_expect_tx(bar + 8 * (L::B_FULL + s), n_valid * L::BLOCK);
+      __syncwarp();
+      if (lane < n_valid)
+        bulk_g2s_stream(base + L::OFF_STAGE + s * L::STAGE_BYTES + lane * L::BLOCK,
+                        kv_head + static_cast<int64_t>(next_page) * pv.n_kv_heads * L::BLOCK, L::BLOCK, bar + 8 * (L::B_FULL + s), policy);
+      ++issued;
+      ask();
+    };
+    if (warp == 0 && !no_copies) {
+      ask();
+      for (int k = 0; k < L::STAGES && k < nt; ++k) copy();
     }
-  } else if (warp < 4) {
-    // ================================================================ stacked Q operand (64 threads, four to a row)
-    constexpr int PER = D / 32;                  // 16-byte chunks of a thread
-    const int t64 = tid - 64, part = t64 & 3;
-    uint32_t uc = 0;
-    bool ok = true;
-    Walk wk{0, u0, 0};
-    UnitInfo x;
-    int ll = 0;
-    for (; ok && next(wk, true, ok, x, ll); ++uc) {
-      const int rows = x.n_threads << g_shift, n = rows16(x), qb = uc % L::QB;
-      for (int r0 = 0; r0 < n; r0 += 16) {
-        const int row = r0 + (t64 >> 2);
+
+    // ---- stacked queries, four threads to a row; a row's first reference: NaN spoils a row whose query is not finite
+    {
+      constexpr int PER = D / 32;
+      const int part = tid & 3;
+#pragma unroll 1
+      for (int row = tid >> 2; row < n; row += L::THREADS / 4) {
         uint4 val[PER];
 #pragma unroll
         for (int c = 0; c < PER; ++c) val[c] = make_uint4(0, 0, 0, 0);
         if (row < rows) {
           const int qn = plan[a.off_tq + x.tq_off + (row >> g_shift)];
           const uint4 *src = reinterpret_cast<const uint4 *>(
-              q + ((static_cast<int64_t>(ll) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (row & (G - 1))) * D) + part * PER;
+              q + ((static_cast<int64_t>(layer) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (row & (G - 1))) * D) + part * PER;
 #pragma unroll
           for (int c = 0; c < PER; ++c) val[c] = __ldg(src + c);
         }
@@ -309,432 +277,356 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         for (int c = 0; c < PER; ++c)
           m2 = __vmaxu2(__vmaxu2(m2, val[c].x & 0x7fff7fffu),
                         __vmaxu2(__vmaxu2(val[c].y & 0x7fff7fffu, val[c].z & 0x7fff7fffu), val[c].w & 0x7fff7fffu));
-        m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
-        m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
-        if (r0 == 0 && !warp_wait_or_abort(bar + 8 * (L::B_QFREE + qb), ((uc / L::QB) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-        // A row's first reference; NaN spoils a row whose query is not finite.  The softmax reads it with the unit's first tile.
-        // The place of unit uc is written again for unit uc + 4, after the last Q.K^T of unit uc + 4 - QB, whose first tile is at least
-        // two behind unit uc's, so that its scores' buffer has been given back by the softmax of unit uc's first tile.
-        if (part == 0)
-          init_s[(uc % U_INIT) * NMAX + row] = row >= rows ? 0.f : (m2 & 0xffffu) >= 0x7f80u || m2 >= 0x7f800000u ? NAN : R_UNSET;
-        uint8_t *dst = sm + L::OFF_Q + qb * L::Q_BYTES + (row >> 3) * 1024 + (row & 7) * 128;
+        m2 = __vmaxu2(m2, __shfl_xor_sync(0xfu << (lane & 28), m2, 1));
+        m2 = __vmaxu2(m2, __shfl_xor_sync(0xfu << (lane & 28), m2, 2));
+        if (part == 0) ref_s[row] = row >= rows ? 0.f : (m2 & 0xffffu) >= 0x7f80u || m2 >= 0x7f800000u ? NAN : R_UNSET;
+        uint8_t *dst = sm + L::OFF_Q + (row >> 3) * 1024 + (row & 7) * 128;
 #pragma unroll
         for (int c = 0; c < PER; ++c) {
           const int chunk = part * PER + c;
           *reinterpret_cast<uint4 *>(dst + (chunk >> 3) * (NMAX * 128) + (((chunk & 7) ^ (row & 7)) << 4)) = val[c];
         }
       }
-      if (!ok) break;
       fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar + 8 * (L::B_QFULL + qb));
     }
-  } else if (warp < 8) {
-    // ================================================================ K's codes to the A operand: a thread per token
-    const int wq = warp & 3;
-    const uint32_t lane_addr = static_cast<uint32_t>(wq * 32) << 16;
-    const int at = (2 * wq + (lane >> 4)) * L::BLOCK + (lane & 15) * 16;             // this token's 16 bytes of the first group
-    const int at_scale = (2 * wq + (lane >> 4)) * L::BLOCK + kv4_k_scales(D) + (lane & 15) * (D / 16);
-    uint32_t it = 0;
-    bool ok = true;
-    Walk wk{0, u0, 0};
-    UnitInfo x;
-    int ll = 0;
-    while (ok && next(wk, true, ok, x, ll)) {
-      for (int k = x.tile_begin; k < x.tile_end; ++k, ++it) {
-        const uint32_t s = it % L::STAGES, kb = it % L::KB;
-        if (!warp_wait_or_abort(bar + 8 * (L::B_FULL + s), (it / L::STAGES) & 1, abort_flag, limit)) { ok = false; break; }
-        const uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
-        uint4 c[D / 32];
-        uint32_t t[D / 64];
+    float l[L::CHUNKS][8];
 #pragma unroll
-        for (int g = 0; g < D / 32; ++g) c[g] = *reinterpret_cast<const uint4 *>(stage + at + g * 256);
-        if constexpr (D == 128) {
-          const uint2 v = *reinterpret_cast<const uint2 *>(stage + at_scale);
-          t[0] = v.x; t[1] = v.y;
+    for (int c = 0; c < L::CHUNKS; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) l[c][j] = 0.f;
+
+    for (int k = 0; k < nt; ++k, ++it) {
+      const int s = it % L::STAGES;
+      const uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
+      // ---- K's codes to the A operand, a thread per token (half the channels); the P.V before has read what it replaces
+      cta_wait(bar + 8 * (L::B_FULL + s), (it / L::STAGES) & 1, abort_flag, limit);
+      if (k > 0) cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
+      tc_fence_after();
+      const int meta = meta_s[s * PASTA_TILE_PAGES + (token >> 4)];
+      {
+        const uint8_t *block = stage + (token >> 4) * L::BLOCK;
+        const uint8_t *at = block + (token & 15) * 16, *at_scale = block + kv4_k_scales(D) + (token & 15) * (D / 16);
+        constexpr int GROUPS = D / 32 / H;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+          const int g = half * GROUPS + i;
+          const uint4 c = *reinterpret_cast<const uint4 *>(at + g * 256);
+          const uint32_t t = *reinterpret_cast<const uint16_t *>(at_scale + 2 * g), t2 = t | (t << 16), c2 = kv4_offset_of(t2);
+          const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+          uint32_t o[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = kv4_value(kv4_pair(w[e >> 2], e & 3), t2, c2);
+          tmem_st16(lane_addr + L::COL_A + g * 16, o);
+        }
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncthreads();
+      if (warp == (it & 3) && lane == 0 && !no_mma) {
+        // ---- S^T = K . Q^T
+        tc_fence_after();
+        const uint32_t idesc = IDESC4 | ((static_cast<uint32_t>(n) >> 3) << 17);
+#pragma unroll
+        for (int ks = 0; ks < L::KSTEPS; ++ks)
+          mma_ts(tmem + L::COL_S, tmem + L::COL_A + ks * 8, smem_desc(base + L::OFF_Q + (ks >> 2) * (NMAX * 128) + (ks & 3) * 32, 16, 1024), idesc, ks > 0);
+        mma_commit(bar + 8 * L::B_QK);
+      }
+      __syncwarp();
+      // ---- which rows see this token (a bit each); pages that every thread of the request sees in full need no look
+      const bool masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
+      uint32_t seen[(NMAX + 31) / 32];
+      if (masked) {
+        const int pos = PASTA_PMETA_PAGE(meta) * PASTA_PAGE + (token & 15);
+        const int32_t *vis = plan + a.off_vis + x.vis_off + (meta < 0 ? 0 : PASTA_PMETA_STREAM(meta));
+        int thread = 0;
+#pragma unroll
+        for (int w = 0; w < (NMAX + 31) / 32; ++w) {
+          seen[w] = 0;
+#pragma unroll 4
+          for (int j = 0; j < 32 && thread < x.n_threads; j += G, ++thread)
+            if (pos < vis[thread * x.n_streams]) seen[w] |= ((1u << G) - 1) << j;
+          if (meta < 0) seen[w] = 0;
+        }
+      }
+      cta_wait(bar + 8 * L::B_QK, it & 1, abort_flag, limit);
+      tc_fence_after();
+      // ---- V's codes to the A operand, in K's place, a thread per channel (half the pages)
+      {
+        const int channel = token % D;
+        constexpr int PAGES = L::VSTEPS / H;
+        const int page0 = (D == 128 ? 0 : 4 * (wq >> 1)) + half * PAGES;
+        const uint8_t *at = stage + page0 * L::BLOCK + kv4_v_codes(D) + channel * 8;
+        const uint8_t *at_scale = stage + page0 * L::BLOCK + kv4_v_scales(D) + (channel / kKv4Group) * 32;
+#pragma unroll
+        for (int p = 0; p < PAGES; ++p) {
+          const uint2 c = *reinterpret_cast<const uint2 *>(at + p * L::BLOCK);
+          const uint4 ta = *reinterpret_cast<const uint4 *>(at_scale + p * L::BLOCK), tb = *reinterpret_cast<const uint4 *>(at_scale + p * L::BLOCK + 16);
+          const uint32_t t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
+          uint32_t o[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = kv4_value(kv4_pair(i < 4 ? c.x : c.y, i & 3), t[i], kv4_offset_of(t[i]));
+          tmem_st8(lane_addr + L::COL_A + (half * PAGES + p) * 8, o);
+        }
+      }
+      // ---- the tile's weights
+      auto hide = [&](int c, float *v) {            // c: chunk of rows
+        uint32_t w = seen[0];
+#pragma unroll
+        for (int i = 1; i < (NMAX + 31) / 32; ++i) w = (c >> 2) == i ? seen[i] : w;
+        w >>= 8 * (c & 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (!((w >> j) & 1)) v[j] = -INFINITY;
+      };
+      // scores of chunk c as they come from the MMA; scaled (log2 units), capped and masked; and relative to the references
+      auto scores = [&](int c, float *v) { tmem_ld8_issue(lane_addr + L::COL_S + c * 8, reinterpret_cast<uint32_t *>(v)); };
+      auto finish = [&](int c, float *v, auto hidden) {
+        if (kCap) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= a.scale_log2 * a.cap_inv;
+          softcap_columns<8>(v, pv.softcap_log2, true);
         } else {
-          t[0] = *reinterpret_cast<const uint32_t *>(stage + at_scale);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= a.scale_log2;
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar + 8 * (L::B_EMPTY + s));
-        if (!warp_wait_or_abort(bar + 8 * (L::B_KFREE + kb), ((it / L::KB) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-        tc_fence_after();
-#pragma unroll
-        for (int h = 0; h < D / 64; ++h) {
-          uint32_t o[32];
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const uint32_t t2 = __byte_perm(t[h], t[h], g ? 0x3232 : 0x1010), c2 = kv4_offset_of(t2);
-            const uint32_t w[4] = {c[2 * h + g].x, c[2 * h + g].y, c[2 * h + g].z, c[2 * h + g].w};
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[16 * g + i] = kv4_value(kv4_pair(w[i >> 2], i & 3), t2, c2);
-          }
-          tmem_st32_u32(tmem + lane_addr + L::COL_K + kb * L::KW + h * 32, o);
+        if (decltype(hidden)::value) hide(c, v);
+      };
+      auto relative = [&](int c, float *v, auto hidden) {
+        const float4 r0 = *reinterpret_cast<const float4 *>(ref_s + c * 8), r1 = *reinterpret_cast<const float4 *>(ref_s + c * 8 + 4);
+        if (kCap) {
+          finish(c, v, hidden);
+          v[0] += r0.x; v[1] += r0.y; v[2] += r0.z; v[3] += r0.w; v[4] += r1.x; v[5] += r1.y; v[6] += r1.z; v[7] += r1.w;
+        } else {
+          fma2v(v[0], v[1], v[0], v[1], a.scale_log2, r0.x, r0.y);
+          fma2v(v[2], v[3], v[2], v[3], a.scale_log2, r0.z, r0.w);
+          fma2v(v[4], v[5], v[4], v[5], a.scale_log2, r1.x, r1.y);
+          fma2v(v[6], v[7], v[6], v[7], a.scale_log2, r1.z, r1.w);
+          if (decltype(hidden)::value) hide(c, v);
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar + 8 * (L::B_KFULL + kb));
-      }
-    }
-  } else if (warp < 12) {
-    // ================================================================ V's codes to the A operand: a thread per channel
-    const int wq = warp & 3;
-    const uint32_t lane_addr = static_cast<uint32_t>(wq * 32) << 16;
-    const int channel = (wq * 32 + lane) % D, page0 = D == 128 ? 0 : 4 * (wq >> 1);        // first page of this thread's
-    const int at = page0 * L::BLOCK + kv4_v_codes(D) + channel * 8, at_scale = page0 * L::BLOCK + kv4_v_scales(D) + (channel / kKv4Group) * 32;
-    uint32_t it = 0;
-    bool ok = true;
-    Walk wk{0, u0, 0};
-    UnitInfo x;
-    int ll = 0;
-    while (ok && next(wk, true, ok, x, ll)) {
-      for (int k = x.tile_begin; k < x.tile_end; ++k, ++it) {
-        const uint32_t s = it % L::STAGES, vb = it % L::VB;
-        if (!warp_wait_or_abort(bar + 8 * (L::B_FULL + s), (it / L::STAGES) & 1, abort_flag, limit)) { ok = false; break; }
-        if (!warp_wait_or_abort(bar + 8 * (L::B_VFREE + vb), ((it / L::VB) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-        tc_fence_after();
-        const uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
-#pragma unroll
-        for (int h = 0; h < L::VW / 32; ++h) {        // four pages at a time
-          uint32_t o[32];
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            const uint8_t *block = stage + (4 * h + p) * L::BLOCK;
-            const uint2 c = *reinterpret_cast<const uint2 *>(block + at);
-            const uint4 ta = *reinterpret_cast<const uint4 *>(block + at_scale), tb = *reinterpret_cast<const uint4 *>(block + at_scale + 16);
-            const uint32_t t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              o[8 * p + i] = kv4_value(kv4_pair(i < 4 ? c.x : c.y, i & 3), t[i], kv4_offset_of(t[i]));
-          }
-          if (h == L::VW / 32 - 1) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar + 8 * (L::B_EMPTY + s));
-          }
-          tmem_st32_u32(tmem + lane_addr + L::COL_V + vb * L::VW + h * 32, o);
-        }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar + 8 * (L::B_VFULL + vb));
-      }
-    }
-  } else {
-    // ================================================================ softmax + epilogue (2 groups of 128 threads)
-    const int grp = (warp - 12) >> 2;             // this group's rows: 8 (2 c + grp) .. + 7 for c = 0, 1, ...
-    const int wq = warp & 3, token = wq * 32 + lane;
-    const int gt = token;                         // thread of the group
-    const uint32_t lane_addr = static_cast<uint32_t>(wq * 32) << 16;
-    float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
-    float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
-    volatile int *vote_s = reinterpret_cast<volatile int *>(sm + L::OFF_VOTE) + 4 * grp;
-    const float cap = pv.softcap_log2;
-    constexpr bool kKeep = L::CHUNKS <= 4;        // a tile's scores stay in registers from the vote to the weights
-    constexpr int SC = kKeep ? L::CHUNKS : 1;
-    uint32_t it = 0, uc = 0, meets = 0;
-    bool ok = true;
-    // the group's four warps meet
-    auto meet = [&]() {
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar + 8 * (L::B_SYNC + grp));
-      return warp_wait_or_abort(bar + 8 * (L::B_SYNC + grp), meets++ & 1, abort_flag, limit);
-    };
-    Walk wk{0, u0, 0};
-    UnitInfo x;
-    int ll = 0;
-    for (; ok && next(wk, true, ok, x, ll); ++uc) {
-      const int nt = x.tile_end - x.tile_begin;
-      const int rows = x.n_threads << g_shift, n = rows16(x);
-      const uint32_t ob = uc % L::OB;
-      const bool fin = x.final_rows != 0;
-      const int n_chunks = max(0, (((rows + 7) >> 3) - grp + 1) >> 1);      // of this group
-      const int my_row = ((gt >> 3) * 2 + grp) * 8 + (gt & 7);               // the row this thread looks after between tiles
-      const bool keeper = my_row < n && gt < NMAX / 2;
-      float l[L::CHUNKS][8];
-#pragma unroll
-      for (int c = 0; c < L::CHUNKS; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) l[c][j] = 0.f;
-      for (int k = 0; k < nt; ++k, ++it) {
-        const uint32_t sb = it % L::SB, pb = it & 1;
-        const uint32_t s_addr = tmem + lane_addr + L::COL_S + sb * NMAX + grp * 8;
-        if (!warp_wait_or_abort(bar + 8 * (L::B_SFULL + sb), (it / L::SB) & 1, abort_flag, limit)) { ok = false; break; }
-        tc_fence_after();
-        if (k == 0) {
-          if (keeper) ref_s[my_row] = init_s[(uc % U_INIT) * NMAX + my_row];
-          if (!meet()) { ok = false; break; }
-        }
-        // which rows see this token: bit j of seen[c] for row j of chunk c; pages that every thread sees in full need no look
-        const int meta = meta_s[(it % U_RING) * PASTA_TILE_PAGES + (token >> 4)];
-        const bool masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
-        uint32_t seen[(L::CHUNKS + 3) / 4];
-        if (masked) {
-#pragma unroll
-          for (int i = 0; i < (L::CHUNKS + 3) / 4; ++i) seen[i] = 0;
-          const int pos = PASTA_PMETA_PAGE(meta) * PASTA_PAGE + (token & 15);
-          const int32_t *vis = plan + a.off_vis + x.vis_off + (meta < 0 ? 0 : PASTA_PMETA_STREAM(meta));
-#pragma unroll
-          for (int c = 0; c < L::CHUNKS; ++c) {
-            if (c >= n_chunks) continue;
-            for (int j = 0; j < 8; j += G) {
-              const int thread = min((8 * (2 * c + grp) + j) >> g_shift, x.n_threads - 1);
-              if (meta >= 0 && pos < vis[thread * x.n_streams]) seen[c >> 2] |= ((1u << G) - 1) << (8 * (c & 3) + j);
-            }
-          }
-        }
-        // scores of chunk c in log2 units (capped ones), or what is still to be multiplied by the scale
-        auto scores = [&](int c, uint32_t *r) { tmem_ld8_issue(s_addr + c * 16, r); };
-        auto finish = [&](int c, float *v) {      // scaled, capped, masked
-          if (kCap) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= a.scale_log2 * a.cap_inv;
-            softcap_columns<8>(v, cap, true);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= a.scale_log2;
-          }
-          if (masked) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (!((seen[c >> 2] >> (8 * (c & 3) + j)) & 1)) v[j] = -INFINITY;
-          }
-        };
-        // relative to the references, masked ones -inf
-        auto relative = [&](int c, float *v) {
-          const float4 r0 = *reinterpret_cast<const float4 *>(ref_s + (2 * c + grp) * 8), r1 = *reinterpret_cast<const float4 *>(ref_s + (2 * c + grp) * 8 + 4);
-          if (kCap) {
-            finish(c, v);
-            v[0] += r0.x; v[1] += r0.y; v[2] += r0.z; v[3] += r0.w; v[4] += r1.x; v[5] += r1.y; v[6] += r1.z; v[7] += r1.w;
-          } else {
-            fma2v(v[0], v[1], v[0], v[1], a.scale_log2, r0.x, r0.y);
-            fma2v(v[2], v[3], v[2], v[3], a.scale_log2, r0.z, r0.w);
-            fma2v(v[4], v[5], v[4], v[5], a.scale_log2, r1.x, r1.y);
-            fma2v(v[6], v[7], v[6], v[7], a.scale_log2, r1.z, r1.w);
-            if (masked) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (!((seen[c >> 2] >> (8 * (c & 3) + j)) & 1)) v[j] = -INFINITY;
-            }
-          }
-        };
-        float v[SC][8];
+      };
+      // this token's row of the B operand: its 16-byte chunk x is at x ^ (row % 8) (or ^ (row / 2 % 4) in rows of 64 bytes), and at
+      // head_dim 64 the two halves of the tile have every other chunk
+      const int b_row = D == 128 ? token : token & 63, b_half = D == 128 ? 0 : token >> 6;
+      const uint32_t p_row = L::NARROW
+          ? L::OFF_P + (b_row >> 3) * L::P_GROUP + (b_row & 7) * 64 + ((((b_row >> 1) & 3) ^ b_half) << 4)
+          : L::OFF_P + (b_row >> 3) * L::P_GROUP + (b_row & 7) * 128 + (((b_row & 7) ^ b_half) << 4);
+      auto place = [&](int c) {
+        const int col = L::OW * c;
+        if (L::NARROW) return reinterpret_cast<uint4 *>(sm + (p_row ^ ((col & 3) << 4)));
+        return reinterpret_cast<uint4 *>(sm + (p_row ^ ((col & 7) << 4)) + (col >> 3) * 1024);
+      };
+      uint32_t w[L::CHUNKS][4];
+      // Weights rounded to bf16, as rows of the B operand; returns the largest exponent.  Straight code for every number of chunks
+      // (rows beyond the unit's last are zeros in Q and count for nothing): a branch costs as much as half a chunk, and chunks overlap.
+      auto weights = [&](auto chunks, auto hidden) {
+        constexpr int C = decltype(chunks)::value;
         float top = -INFINITY;
-        if constexpr (kKeep) {
 #pragma unroll
-          for (int c = 0; c < SC; ++c)
-            if (c < n_chunks) scores(c, reinterpret_cast<uint32_t *>(v[c]));
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        for (int c0 = 0; c0 < C; c0 += 4) {
+          float v[4][8];
 #pragma unroll
-          for (int c = 0; c < SC; ++c) tmem_ld_order8(reinterpret_cast<uint32_t *>(v[c]));
+          for (int i = 0; i < 4; ++i)
+            if (c0 + i < C) scores(H * (c0 + i) + half, v[i]);
+          tmem_ld_wait8(reinterpret_cast<uint32_t *>(v[0]));
 #pragma unroll
-          for (int c = 0; c < SC; ++c)
-            if (c < n_chunks) {
-              relative(c, v[c]);
+          for (int i = 1; i < 4; ++i)
+            if (c0 + i < C) tmem_ld_order8(reinterpret_cast<uint32_t *>(v[i]));
 #pragma unroll
-              for (int j = 0; j < 8; ++j) top = fmaxf(top, v[c][j]);
-            }
-        } else {
-#pragma unroll 1
-          for (int c = 0; c < n_chunks; ++c) {
-            scores(c, reinterpret_cast<uint32_t *>(v[0]));
-            tmem_ld_wait8(reinterpret_cast<uint32_t *>(v[0]));
-            relative(c, v[0]);
+          for (int i = 0; i < 4; ++i) {
+            if (c0 + i >= C) continue;
+            float *y = v[i];
+            relative(H * (c0 + i) + half, y, hidden);
+            top = max3(max3(top, y[0], y[1]), y[2], y[3]);
+            top = max3(max3(top, y[4], y[5]), y[6], y[7]);
+            uint32_t *o = w[c0 + i < L::CHUNKS ? c0 + i : 0];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, v[0][j]);
+            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(fast_exp2(y[2 * j]), fast_exp2(y[2 * j + 1]));
+            *place(H * (c0 + i) + half) = make_uint4(o[0], o[1], o[2], o[3]);
           }
         }
-        // ---- the vote.  The word of tile it + 2 is cleared now: everybody has looked at that of tile it - 2, which is the same.
-        if (top > R_SLACK) vote_s[it & 3] = 1;
-        if (gt == 0) vote_s[(it + 2) & 3] = 0;
-        if (!meet()) { ok = false; break; }
-        if (vote_s[it & 3] != 0) {
-          // ---- some row's reference goes up: maxima of all rows over the tile, then O and l brought to the new references
-#pragma unroll 1
-          for (int c = 0; c < n_chunks; ++c) {
-            float y[8];
-            scores(c, reinterpret_cast<uint32_t *>(y));
-            tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
-            finish(c, y);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float m = warp_max(y[j]);
-              if (lane == 0) warp_s[wq * NMAX + (2 * c + grp) * 8 + j] = m;
-            }
-          }
-          if (!meet()) { ok = false; break; }
-          if (keeper) {
-            const float m = fmaxf(fmaxf(warp_s[my_row], warp_s[NMAX + my_row]), fmaxf(warp_s[2 * NMAX + my_row], warp_s[3 * NMAX + my_row]));
-            const float old = ref_s[my_row];
-            float f = 1.f;
-            if (m > -INFINITY && (old == R_UNSET || m + old > R_SLACK)) {
-              f = old == R_UNSET ? 0.f : fast_exp2(-old - m);          // (a row that has seen nothing has nothing to bring along)
-              ref_s[my_row] = -m;
-            }
-            fact_s[my_row] = f;
-          }
-          if (!meet()) { ok = false; break; }
-          if (k > 0) {
-            // the accumulator is quiet once the P.V of the previous tile has finished
-            if (!warp_wait_or_abort(bar + 8 * (L::B_PFREE + ((it - 1) & 1)), ((it - 1) >> 1) & 1, abort_flag, limit)) { ok = false; break; }
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < L::CHUNKS; ++c) {
-              if (c >= n_chunks) continue;
-              float f[8];
-              bool any = false;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                f[j] = fact_s[(2 * c + grp) * 8 + j];
-                any = any || f[j] != 1.f;
-                l[c][j] *= f[j];
-              }
-              if (!any) continue;
-#pragma unroll
-              for (int w = 0; w < L::OW; ++w) {
-                uint32_t o[8];
-                const uint32_t at = tmem + lane_addr + L::COL_O + ob * L::OW * NMAX + w * n + (2 * c + grp) * 8;
-                tmem_ld8_issue(at, o);
-                tmem_ld_wait8(o);
-                // a factor of 0 replaces: what no weight has reached yet is 0 times finite numbers, or of a row that is NaN anyway
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f[j]);
-                tmem_st8(at, o);
-              }
-            }
-            tmem_st_wait();
-          }
-          if constexpr (kKeep) {                 // the scores anew, relative to the new references
-#pragma unroll
-            for (int c = 0; c < SC; ++c)
-              if (c < n_chunks) scores(c, reinterpret_cast<uint32_t *>(v[c]));
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-            for (int c = 0; c < SC; ++c) tmem_ld_order8(reinterpret_cast<uint32_t *>(v[c]));
-#pragma unroll
-            for (int c = 0; c < SC; ++c)
-              if (c < n_chunks) relative(c, v[c]);
-          }
-        }
-        // ---- weights: rounded to bf16, summed as rounded, and stored as rows of the B operand
-        if constexpr (kKeep) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar + 8 * (L::B_SFREE + sb));
-        }
-        if (!warp_wait_or_abort(bar + 8 * (L::B_PFREE + pb), ((it >> 1) & 1) ^ 1, abort_flag, limit)) { ok = false; break; }
-        const int kr = D == 128 ? token : token & 63;                          // row of the operand
-        const int col0 = D == 128 ? 0 : (token >> 6) * (n >> 3);               // its first chunk of 8 columns
-        uint8_t *p_row = sm + L::OFF_P + pb * L::P_BYTES + (kr >> 3) * (L::ATOMS * 1024) + (kr & 7) * 128;
-#pragma unroll
-        for (int c = 0; c < L::CHUNKS; ++c) {
-          if (c >= n_chunks) continue;
-          float *y = v[kKeep ? c : 0];
-          if constexpr (!kKeep) {
-            scores(c, reinterpret_cast<uint32_t *>(y));
-            tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
-            relative(c, y);
-          }
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            w[j] = pack_bf16(fast_exp2(y[2 * j]), fast_exp2(y[2 * j + 1]));
-            add2(l[c][2 * j], l[c][2 * j + 1], bf16_lo(w[j]), bf16_hi(w[j]));
-          }
-          const int col = col0 + 2 * c + grp;
-          *reinterpret_cast<uint4 *>(p_row + (col >> 3) * 1024 + (((col & 7) ^ (kr & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        return top;
+      };
+      auto by_chunks = [&](auto f) {                // f for the number of chunks of this thread, which is n / 8 / H
+#define PASTA_C(cc) \
+  if constexpr (L::CHUNKS >= cc && (H == 2 || cc % 2 == 0)) { if (n == 8 * H * cc) return f(std::integral_constant<int, cc>()); }
+        PASTA_C(2) PASTA_C(3) PASTA_C(4) PASTA_C(5) PASTA_C(6) PASTA_C(7) PASTA_C(8)
+#undef PASTA_C
+        return f(std::integral_constant<int, 1>());
+      };
+      auto all_weights = [&]() {
+        return by_chunks([&](auto chunks) { return masked ? weights(chunks, std::true_type()) : weights(chunks, std::false_type()); });
+      };
+      bool raised = false, left = false;
+      for (;;) {
+        const float top = all_weights();
+        tmem_st_wait();
         fence_proxy_async();
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (!kKeep) mbar_arrive(bar + 8 * (L::B_SFREE + sb));
-          mbar_arrive(bar + 8 * (L::B_PFULL + pb));
-        }
-      }
-      if (!ok) break;
-
-      // ---- epilogue: sums over the tokens, then the rows of O, a thread per channel
-#pragma unroll
-      for (int c = 0; c < L::CHUNKS; ++c) {
-        if (c >= n_chunks) continue;
-        const float t = warp_sum8(l[c], lane);
-        if ((lane & 3) == 0) warp_s[wq * NMAX + (2 * c + grp) * 8 + (lane >> 2)] = t;
-      }
-      if (!meet()) { ok = false; break; }
-      int qn = 0;
-      if (keeper) {
-        const float sum = (warp_s[my_row] + warp_s[NMAX + my_row]) + (warp_s[2 * NMAX + my_row] + warp_s[3 * NMAX + my_row]);
-        const bool spoilt = sum != sum;
-        const float m = spoilt ? not_a_row().x : sum > 0.f ? -ref_s[my_row] : -INFINITY, l_all = spoilt ? not_a_row().y : sum;
-        fact_s[my_row] = spoilt ? NAN : fin ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
-        if (my_row < rows) {
-          if (!fin) {
-            pv.part_ml[static_cast<int64_t>(ll) * pv.rows_per_layer + x.row_base + my_row] = make_float2(m, l_all);
-          } else if (a.lse) {
-            qn = plan[a.off_tq + x.tq_off + (my_row >> g_shift)];
-            a.lse[(static_cast<int64_t>(ll) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (my_row & (G - 1))] = (m + log2f(l_all)) * 0.6931471805599453f;
-          }
-        }
-      }
-      if (!meet() || !warp_wait_or_abort(bar + 8 * (L::B_OFULL + ob), (uc / L::OB) & 1, abort_flag, limit)) { ok = false; break; }
-      tc_fence_after();
-      const uint32_t o_addr = tmem + lane_addr + L::COL_O + ob * L::OW * NMAX + (D == 64 ? (wq >> 1) * n : 0) + grp * 8;
-      float *sum_s = reinterpret_cast<float *>(sm + L::OFF_SUM) + (token & 63);
-      if constexpr (D == 64) {
-        if (wq >= 2) {
+        // ---- everybody is done with the stage, V's operand and the weights stand, and the CTA votes (also on leaving)
+        if (!__syncthreads_or((!raised && top > R_SLACK) || *abort_flag != 0)) break;
+        left = __syncthreads_or(*abort_flag != 0);
+        if (left) break;
+        // ---- some row's reference goes up: maxima of all rows over the tile, then O and l brought to the new references
 #pragma unroll 1
-          for (int c = 0; c < n_chunks; ++c) {
-            uint32_t o[8];
-            tmem_ld8_issue(o_addr + c * 16, o);
-            tmem_ld_wait8(o);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum_s[((2 * c + grp) * 8 + j) * 64] = __uint_as_float(o[j]);
-          }
-        }
-        if (!meet()) { ok = false; break; }
-      }
-      if (D == 128 || wq < 2) {
-#pragma unroll 1
-        for (int c = 0; c < n_chunks; ++c) {
-          uint32_t o[8];
-          tmem_ld8_issue(o_addr + c * 16, o);
-          tmem_ld_wait8(o);
+        for (int c = half; 8 * c < rows; c += H) {
+          float y[8], mine = -INFINITY;
+          scores(c, y);
+          tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
+          if (masked) finish(c, y, std::true_type());
+          else finish(c, y, std::false_type());
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int row = (2 * c + grp) * 8 + j;
-            if (row >= rows) continue;
-            const float f = fact_s[row];
-            float y = __uint_as_float(o[j]);
-            if (D == 64) y += sum_s[row * 64];
-            y = f == 0.f ? 0.f : y * f;                // a final row that saw nothing is written as zeros
-            if (fin) {
-              const int row_q = plan[a.off_tq + x.tq_off + (row >> g_shift)];
-              const int64_t at = ((static_cast<int64_t>(ll) * a.n_queries + row_q) * pv.n_q_heads + x.g * G + (row & (G - 1))) * D + token;
-              if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
-              else static_cast<float *>(a.out)[at] = y;
-            } else {
-              pv.part_o[(static_cast<int64_t>(ll) * pv.rows_per_layer + x.row_base + row) * D + token] = y;
+            const float m = warp_max(y[j]);
+            if (lane == j) mine = m;
+          }
+          if (lane < 8) warp_s[wq * NMAX + 8 * c + lane] = mine;
+        }
+        __syncthreads();
+        if (tid < n) {
+          float f = 1.f;
+          if (tid < rows) {
+            const float m = fmaxf(fmaxf(warp_s[tid], warp_s[NMAX + tid]), fmaxf(warp_s[2 * NMAX + tid], warp_s[3 * NMAX + tid]));
+            const float old = ref_s[tid];
+            if (m > -INFINITY && (old == R_UNSET || m + old > R_SLACK)) {
+              f = old == R_UNSET ? 0.f : fast_exp2(-old - m);          // (a row that has seen nothing has nothing to bring along)
+              ref_s[tid] = -m;
             }
+          }
+          fact_s[tid] = f;
+        }
+        __syncthreads();
+        if (k > 0) {                                 // (the P.V before has finished: it was waited for)
+#pragma unroll
+          for (int i = 0; i < L::CHUNKS; ++i) {
+            const int c = H * i + half;
+            if (8 * c >= rows) continue;
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              f[j] = fact_s[8 * c + j];
+              l[i][j] *= f[j];
+            }
+#pragma unroll 1
+            for (int o2 = 0; o2 < L::OW; ++o2) {
+              uint32_t o[8];
+              const uint32_t at = lane_addr + L::COL_O + 8 * (L::OW * c + o2);
+              tmem_ld8_issue(at, o);
+              tmem_ld_wait8(o);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f[j]);
+              tmem_st8(at, o);
+            }
+          }
+          tmem_st_wait();
+        }
+        raised = true;
+      }
+      if (left) break;
+      if (warp == 0 && !no_copies && k + L::STAGES < nt) copy();
+      if (warp == ((it + 2) & 3) && lane == 0 && !no_mma) {
+        // ---- O^T += V^T . P^T
+        tc_fence_after();
+        const uint32_t idesc = IDESC4_PV | (((L::OW * static_cast<uint32_t>(n)) >> 3) << 17);
+#pragma unroll
+        for (int ks = 0; ks < L::VSTEPS; ++ks) {
+          const uint32_t at = base + L::OFF_P + ks * 2 * L::P_GROUP;
+          mma_ts(tmem + L::COL_O, tmem + L::COL_A + ks * 8, L::NARROW ? smem_desc64(at, 512, L::P_GROUP) : smem_desc(at, 1024, L::P_GROUP), idesc,
+                 k > 0 || ks > 0);
+        }
+        mma_commit(bar + 8 * L::B_PV);
+      }
+      __syncwarp();
+      // ---- the sums, of the weights as rounded
+#pragma unroll
+      for (int i = 0; i < L::CHUNKS; ++i) {
+        if (8 * (H * i + half) >= n) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add_bf16x2(l[i][2 * j], l[i][2 * j + 1], w[i][j]);
+      }
+    }
+    if (__syncthreads_or(*abort_flag != 0)) break;
+
+    // ---- epilogue: sums over the tokens, then the rows of O, a thread per channel
+#pragma unroll
+    for (int i = 0; i < L::CHUNKS; ++i) {
+      const int c = H * i + half;
+      if (8 * c >= rows) continue;
+      const float t = warp_sum8(l[i], lane);
+      if ((lane & 3) == 0) warp_s[wq * NMAX + 8 * c + (lane >> 2)] = t;
+    }
+    __syncthreads();
+    if (tid < rows) {
+      const float sum = (warp_s[tid] + warp_s[NMAX + tid]) + (warp_s[2 * NMAX + tid] + warp_s[3 * NMAX + tid]);
+      const bool spoilt = sum != sum;
+      const float m = spoilt ? not_a_row().x : sum > 0.f ? -ref_s[tid] : -INFINITY, l_all = spoilt ? not_a_row().y : sum;
+      fact_s[tid] = spoilt ? NAN : fin ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
+      if (!fin) {
+        pv.part_ml[static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + tid] = make_float2(m, l_all);
+      } else if (a.lse) {
+        const int qn = plan[a.off_tq + x.tq_off + (tid >> g_shift)];
+        a.lse[(static_cast<int64_t>(layer) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (tid & (G - 1))] = (m + log2f(l_all)) * 0.6931471805599453f;
+      }
+    }
+    cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
+    if (__syncthreads_or(*abort_flag != 0)) break;
+    tc_fence_after();
+    const uint32_t o_addr = lane_addr + L::COL_O + (D == 64 ? (wq >> 1) * 8 : 0);
+    float *sum_s = reinterpret_cast<float *>(sm + L::OFF_P) + (token & 63);
+    if constexpr (D == 64) {
+      if (wq >= 2) {
+#pragma unroll 1
+        for (int c = half; 8 * c < rows; c += H) {
+          uint32_t o[8];
+          tmem_ld8_issue(o_addr + c * 8 * L::OW, o);
+          tmem_ld_wait8(o);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum_s[(c * 8 + j) * 64] = __uint_as_float(o[j]);
+        }
+      }
+      __syncthreads();
+    }
+    if (D == 128 || wq < 2) {
+#pragma unroll 1
+      for (int c = half; 8 * c < rows; c += H) {
+        uint32_t o[8];
+        tmem_ld8_issue(o_addr + c * 8 * L::OW, o);
+        tmem_ld_wait8(o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int row = c * 8 + j;
+          if (row >= rows) continue;
+          const float f = fact_s[row];
+          float y = __uint_as_float(o[j]);
+          if (D == 64) y += sum_s[row * 64];
+          y = f == 0.f ? 0.f : y * f;                // a final row that saw nothing is written as zeros
+          if (fin) {
+            const int row_q = plan[a.off_tq + x.tq_off + (row >> g_shift)];
+            const int64_t at = ((static_cast<int64_t>(layer) * a.n_queries + row_q) * pv.n_q_heads + x.g * G + (row & (G - 1))) * D + token;
+            if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
+            else static_cast<float *>(a.out)[at] = y;
+          } else {
+            pv.part_o[(static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + row) * D + token] = y;
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar + 8 * (L::B_OFREE + ob));
     }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
   }
 
   // ---- tear-down
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {
-    // see attn_tensor.cu: what is still in flight for this CTA (bulk copies, MMAs) ends on its own and is waited for
-    if (warp == 0 && lane == 0) {
-      for (uint32_t j = (prod_it > L::STAGES ? prod_it - L::STAGES : 0); j < prod_it; ++j)
+    // Some wait has run out and the whole CTA has left in the middle of its work: what is still in flight (bulk copies, MMAs) ends on
+    // its own and is waited for.
+    if (warp == 0) {
+      for (uint32_t j = (issued > L::STAGES ? issued - L::STAGES : 0); j < issued; ++j)
         mbar_wait_bounded(bar + 8 * (L::B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
     }
-    if (warp == 1 && lane == 0) {
+    __syncthreads();
+    if (lane == 0 && warp < 4) {                       // every warp that issues MMAs
       mma_commit(bar + 8 * L::B_DRAIN);
       mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
     }
@@ -742,26 +634,28 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     tc_fence_before();
     __syncthreads();
   }
-  if (warp == 2) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+  if (warp == 0) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS) : "memory");
   }
 }
 
 template <int D, int NMAX>
 cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, const TensorArgs &a, const void *q, cudaStream_t st) {
+  using L = U<D, NMAX>;
   static uint64_t prepared[2] = {0, 0};
   const bool cap = pv.softcap_log2 > 0.f;
   const auto kernel = cap ? attn_kv4_kernel<D, NMAX, true> : attn_kv4_kernel<D, NMAX, false>;
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), U<D, NMAX>::SMEM_BYTES, &prepared[cap]);
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), L::SMEM_BYTES, &prepared[cap]);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(kernel, dim3(h.w[PH_T_GRID]), dim3(U_THREADS), U<D, NMAX>::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
+  return launch_overlapped(kernel, dim3(h.w[PH_T_GRID]), dim3(L::THREADS), L::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
 }
 
 template <int D>
 cudaError_t launch_d(const PoolView &pv, const PlanHeader &h, const TensorArgs &a, const void *q, cudaStream_t st) {
   const int rows = h.w[PH_T_MAX_ROWS];
-  const auto launch = rows <= 16 ? launch_t<D, 16> : rows <= 32 ? launch_t<D, 32> : rows <= 64 ? launch_t<D, 64>
-                    : rows <= 96 ? launch_t<D, 96> : launch_t<D, 128>;
+  static_assert(U<D, 32>::RESIDENT == kv4_ctas_per_sm(D, 32) && U<D, D == 128 ? 80 : 64>::RESIDENT == kv4_ctas_per_sm(D, D == 128 ? 80 : 64) &&
+                U<D, 128>::RESIDENT == kv4_ctas_per_sm(D, 128), "the planner counts on it");
+  const auto launch = rows <= 32 ? launch_t<D, 32> : rows <= (D == 128 ? 80 : 64) ? launch_t<D, D == 128 ? 80 : 64> : launch_t<D, 128>;
   return launch(pv, h, a, q, st);
 }
 

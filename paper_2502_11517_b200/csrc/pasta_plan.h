@@ -38,6 +38,10 @@
 #define PASTA_PMETA_STREAM(meta) ((meta) & PASTA_MAX_STREAMS)
 #define PASTA_PMETA_PAGE(meta) (((meta) >> PASTA_PMETA_STREAM_BITS) & (PASTA_MAX_STREAM_PAGES - 1))
 
+// 4-bit pools: CTAs of the tensor-core kernel that share an SM, by the most stacked rows of any t-request of the step (what they
+// need of the 512 TMEM columns decides)
+constexpr int kv4_ctas_per_sm(int head_dim, int rows) { return rows <= 32 ? 4 : rows <= (head_dim == 128 ? 80 : 64) ? 2 : 1; }
+
 // header words
 enum {
   PH_MAGIC = 0,

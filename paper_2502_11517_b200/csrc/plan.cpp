@@ -207,12 +207,18 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   int32_t t_rows = 0;
   bool whole_runs = false;
   if (!treqs.empty()) {
+    int32_t grid = std::max(1, lim.grid);
+    if (lim.kv4) {
+      int32_t rows = 0;
+      for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
+      grid *= kv4_ctas_per_sm(lim.head_dim, rows);
+    }
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
     // run time (equal tile counts do not finish at the same time: SMs differ in the bandwidth they get).  Only when
     // there is enough work for that to matter.
     int64_t all_tiles = 0;
     for (const TReq &t : treqs) all_tiles += int64_t(lim.n_kv_heads) * ((t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES);
-    const bool share_tail = lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * std::max(1, lim.grid);
+    const bool share_tail = lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * grid;
     // Runs of a few tiles go to the pool whole, every so often, until the pool holds its share of their tiles (`owed`
     // counts what they still owe it): a whole run is a unit anyway, so sharing it costs no extra cut and no extra
     // partial rows.  Long runs stay assigned: cutting their ends into short units cost more, in unit changes and
@@ -239,7 +245,6 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         if (kept > 0) total += kept + overhead;
       }
     }
-    const int32_t grid = std::max(1, lim.grid);
     const double target = std::max(total, 1.0) / grid;
     double cum = 0;
     // A small step (one response, a few threads, a context of a few hundred tokens) is not cut at all when every run can
