@@ -30,7 +30,7 @@
 // A CTA walks its units as those of attn_tensor.cu do.  TMEM holds one operand (K, then V in its place), the scores and O^T.
 // The reference of a row is shared by the CTA's warps and raised only when a score exceeds it by more than 2^R_SLACK: the CTA
 // votes on that with the barrier that publishes the weights, and only then the rows' maxima are worked out and O and l brought to them.
-// With 256 threads the two halves of the CTA share the work on every token, channel and eight rows.
+// The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.
 // Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
 #include <type_traits>
 
@@ -46,8 +46,8 @@ constexpr float R_UNSET = 3e38f;                 // minus the reference of a row
 // Sizes of one build: head_dim D, at most NMAX stacked rows.
 template <int D, int NMAX>
 struct U {
-  static constexpr int H = NMAX <= 32 ? 1 : 2, THREADS = 128 * H; // threads that share a token
-  static constexpr int CHUNKS = NMAX / 8 / H;                     // groups of 8 rows per thread: chunk H i + h for half h
+  static constexpr int H = NMAX <= 32 ? 1 : 2, THREADS = 128 * H;      // threads that share a token
+  static constexpr int CHUNKS = (NMAX / 8 + H - 1) / H;           // groups of 8 rows per thread, at most: chunk H i + part for its part
   static constexpr int OW = D == 128 ? 1 : 2;                     // blocks of N columns of an accumulator
   static constexpr int KSTEPS = D / 16, VSTEPS = D == 128 ? 8 : 4;
   static constexpr uint32_t COL_A = 0, COL_S = D / 2, COL_O = COL_S + NMAX;      // (V's operand is D / 2 columns wide, too)
@@ -103,6 +103,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
                ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
                  "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
+__device__ __forceinline__ uint64_t two_floats(float a, float b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+// {x0, x1} = {x0, x1} * s + {c0, c1}
+__device__ __forceinline__ void fma2s(float &x0, float &x1, uint64_t s, float c0, float c1) {
+  asm("{\n\t.reg .b64 x, c;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 c, {%3, %4};\n\tfma.rn.f32x2 x, x, %2, c;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(x0), "+f"(x1) : "l"(s), "f"(c0), "f"(c1));
+}
 // {l0, l1} += the two bf16 numbers of w
 __device__ __forceinline__ void add_bf16x2(float &l0, float &l1, uint32_t w) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}" : "+f"(l0), "+f"(l1) : "r"(w));
@@ -141,9 +151,11 @@ __device__ __forceinline__ float warp_sum8(const float *v, int lane) {
 // Waits for a phase, or for some thread of the CTA to have given up; sets the flag when the time is up.  Whole warps.
 __device__ __forceinline__ void cta_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
-  const long long t0 = clock64();
+  long long t0 = 0;
 #pragma unroll 1
-  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+  for (int i = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++i) {
+    if (i & 31) continue;
+    if (t0 == 0) t0 = clock64();
     if (clock64() - t0 > limit) *abort_flag = 1;
     if (__any_sync(0xffffffffu, *abort_flag != 0)) return;
   }
@@ -181,6 +193,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // no page is seen before a copy says so
+  for (int i = tid; i < L::STAGES * PASTA_TILE_PAGES; i += L::THREADS) meta_s[i] = -1;
   // operand bytes that no copy fills meet zero weights, so they only have to be finite: page slots that a partial tile leaves empty
   for (int i = tid; i < L::STAGES * L::STAGE_BYTES / 16; i += L::THREADS) reinterpret_cast<uint4 *>(sm + L::OFF_STAGE)[i] = make_uint4(0, 0, 0, 0);
   fence_proxy_async();
@@ -195,9 +209,20 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   int32_t *counter = pv.status + PASTA_STATUS_TAIL_COUNTER;
   uint64_t policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-  const int wq = warp & 3, half = warp >> 2;          // the quarter of TMEM this warp reaches, its half of the work
+  const int wq = warp & 3, half = warp >> 2;          // the quarter of TMEM this warp reaches, its part of the work
   const int token = wq * 32 + lane;                   // as a thread of the scores; as one of V and O: channel `token` (head_dim 64: % 64)
   const uint32_t lane_addr = tmem + (static_cast<uint32_t>(wq * 32) << 16);
+  // the constants of kv4_pair in registers: as immediates they take two instructions instead of one
+  uint32_t code_mask = 0x00780078u, code_one = 0x3f803f80u;
+  asm volatile("" : "+r"(code_mask), "+r"(code_one));
+  auto pair_of = [&](uint32_t w, int i) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(__funnelshift_r(w, w, 4 * i)), "r"(code_mask), "r"(code_one));
+    return y;
+  };
+  const uint64_t scale2 = two_floats(a.scale_log2, a.scale_log2);
+  const uint64_t q_desc = smem_desc(base + L::OFF_Q, 16, 1024);
+  const uint64_t p_desc = L::NARROW ? smem_desc64(base + L::OFF_P, 512, L::P_GROUP) : smem_desc(base + L::OFF_P, 1024, L::P_GROUP);
   // test hook: held copies or MMAs, so that what waits for them runs into its limit
   const bool no_copies = pv.debug_hold & 1, no_mma = pv.debug_hold & 2;
   uint32_t it = 0, issued = 0;                        // tiles worked on and copied; MMA phases follow `it`
@@ -306,16 +331,17 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       {
         const uint8_t *block = stage + (token >> 4) * L::BLOCK;
         const uint8_t *at = block + (token & 15) * 16, *at_scale = block + kv4_k_scales(D) + (token & 15) * (D / 16);
-        constexpr int GROUPS = D / 32 / H;
+        constexpr int GROUPS = (D / 32 + H - 1) / H;
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) {
           const int g = half * GROUPS + i;
+          if (GROUPS * H > D / 32 && g >= D / 32) break;
           const uint4 c = *reinterpret_cast<const uint4 *>(at + g * 256);
           const uint32_t t = *reinterpret_cast<const uint16_t *>(at_scale + 2 * g), t2 = t | (t << 16), c2 = kv4_offset_of(t2);
           const uint32_t w[4] = {c.x, c.y, c.z, c.w};
           uint32_t o[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = kv4_value(kv4_pair(w[e >> 2], e & 3), t2, c2);
+          for (int e = 0; e < 16; ++e) o[e] = kv4_value(pair_of(w[e >> 2], e & 3), t2, c2);
           tmem_st16(lane_addr + L::COL_A + g * 16, o);
         }
       }
@@ -328,7 +354,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         const uint32_t idesc = IDESC4 | ((static_cast<uint32_t>(n) >> 3) << 17);
 #pragma unroll
         for (int ks = 0; ks < L::KSTEPS; ++ks)
-          mma_ts(tmem + L::COL_S, tmem + L::COL_A + ks * 8, smem_desc(base + L::OFF_Q + (ks >> 2) * (NMAX * 128) + (ks & 3) * 32, 16, 1024), idesc, ks > 0);
+          mma_ts(tmem + L::COL_S, tmem + L::COL_A + ks * 8, q_desc + (((ks >> 2) * (NMAX * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
         mma_commit(bar + 8 * L::B_QK);
       }
       __syncwarp();
@@ -364,7 +390,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           const uint32_t t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
           uint32_t o[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = kv4_value(kv4_pair(i < 4 ? c.x : c.y, i & 3), t[i], kv4_offset_of(t[i]));
+          for (int i = 0; i < 8; ++i) o[i] = kv4_value(pair_of(i < 4 ? c.x : c.y, i & 3), t[i], kv4_offset_of(t[i]));
           tmem_st8(lane_addr + L::COL_A + (half * PAGES + p) * 8, o);
         }
       }
@@ -397,10 +423,10 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           finish(c, v, hidden);
           v[0] += r0.x; v[1] += r0.y; v[2] += r0.z; v[3] += r0.w; v[4] += r1.x; v[5] += r1.y; v[6] += r1.z; v[7] += r1.w;
         } else {
-          fma2v(v[0], v[1], v[0], v[1], a.scale_log2, r0.x, r0.y);
-          fma2v(v[2], v[3], v[2], v[3], a.scale_log2, r0.z, r0.w);
-          fma2v(v[4], v[5], v[4], v[5], a.scale_log2, r1.x, r1.y);
-          fma2v(v[6], v[7], v[6], v[7], a.scale_log2, r1.z, r1.w);
+          fma2s(v[0], v[1], scale2, r0.x, r0.y);
+          fma2s(v[2], v[3], scale2, r0.z, r0.w);
+          fma2s(v[4], v[5], scale2, r1.x, r1.y);
+          fma2s(v[6], v[7], scale2, r1.z, r1.w);
           if (decltype(hidden)::value) hide(c, v);
         }
       };
@@ -446,12 +472,13 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         }
         return top;
       };
-      auto by_chunks = [&](auto f) {                // f for the number of chunks of this thread, which is n / 8 / H
+      const int my_chunks = ((n >> 3) - half + H - 1) / H;
+      auto by_chunks = [&](auto f) {                // f for the number of chunks of this thread
 #define PASTA_C(cc) \
-  if constexpr (L::CHUNKS >= cc && (H == 2 || cc % 2 == 0)) { if (n == 8 * H * cc) return f(std::integral_constant<int, cc>()); }
-        PASTA_C(2) PASTA_C(3) PASTA_C(4) PASTA_C(5) PASTA_C(6) PASTA_C(7) PASTA_C(8)
+  if constexpr (L::CHUNKS >= cc) { if (my_chunks == cc) return f(std::integral_constant<int, cc>()); }
+        PASTA_C(1) PASTA_C(2) PASTA_C(3) PASTA_C(4) PASTA_C(5) PASTA_C(6) PASTA_C(7) PASTA_C(8)
 #undef PASTA_C
-        return f(std::integral_constant<int, 1>());
+        return -INFINITY;
       };
       auto all_weights = [&]() {
         return by_chunks([&](auto chunks) { return masked ? weights(chunks, std::true_type()) : weights(chunks, std::false_type()); });
@@ -528,11 +555,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         tc_fence_after();
         const uint32_t idesc = IDESC4_PV | (((L::OW * static_cast<uint32_t>(n)) >> 3) << 17);
 #pragma unroll
-        for (int ks = 0; ks < L::VSTEPS; ++ks) {
-          const uint32_t at = base + L::OFF_P + ks * 2 * L::P_GROUP;
-          mma_ts(tmem + L::COL_O, tmem + L::COL_A + ks * 8, L::NARROW ? smem_desc64(at, 512, L::P_GROUP) : smem_desc(at, 1024, L::P_GROUP), idesc,
-                 k > 0 || ks > 0);
-        }
+        for (int ks = 0; ks < L::VSTEPS; ++ks)
+          mma_ts(tmem + L::COL_O, tmem + L::COL_A + ks * 8, p_desc + (ks * 2 * L::P_GROUP >> 4), idesc, k > 0 || ks > 0);
         mma_commit(bar + 8 * L::B_PV);
       }
       __syncwarp();
