@@ -66,8 +66,8 @@ struct U {
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_P = OFF_Q + Q_BYTES;
   static constexpr int OFF_STAGE = OFF_P + P_BYTES;
-  static constexpr int OFF_BAR = OFF_STAGE + STAGES * STAGE_BYTES;       // FULL[STAGES], QK, PV, DRAIN
-  static constexpr int B_FULL = 0, B_QK = STAGES, B_PV = B_QK + 1, B_DRAIN = B_PV + 1, B_COUNT = B_DRAIN + 1;
+  static constexpr int OFF_BAR = OFF_STAGE + STAGES * STAGE_BYTES;
+  static constexpr int B_QK = 0, B_PV = 1, B_DRAIN = 2, B_COUNT = 3;
   static constexpr int OFF_META = OFF_BAR + 8 * ((B_COUNT + 1) & ~1);    // [STAGES] 8 page metas
   static constexpr int OFF_MISC = OFF_META + STAGES * 32;                // tmem base, abort flag, -, -, the unit's record
   static constexpr int OFF_REF = OFF_MISC + 16 + 64;                     // [NMAX] references (negated)
@@ -148,6 +148,21 @@ __device__ __forceinline__ float warp_sum8(const float *v, int lane) {
   return t + __shfl_xor_sync(0xffffffffu, t, 1);
 }
 
+// one lane of a whole warp
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t y;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(y));
+  return y != 0;
+}
+
+// 16 bytes from global to shared memory, not kept in L1 and the first to leave L2
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Waits for a phase, or for some thread of the CTA to have given up; sets the flag when the time is up.  Whole warps.
 __device__ __forceinline__ void cta_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
@@ -180,6 +195,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   volatile int *abort_flag = reinterpret_cast<volatile int *>(misc + 1);
   float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
   float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
+  int32_t *row_s = reinterpret_cast<int32_t *>(warp_s);
   const int32_t *plan = pv.plan;
 
   if (tid == 0) {
@@ -223,63 +239,88 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   const uint64_t scale2 = two_floats(a.scale_log2, a.scale_log2);
   const uint64_t q_desc = smem_desc(base + L::OFF_Q, 16, 1024);
   const uint64_t p_desc = L::NARROW ? smem_desc64(base + L::OFF_P, 512, L::P_GROUP) : smem_desc(base + L::OFF_P, 1024, L::P_GROUP);
-  // test hook: held copies or MMAs, so that what waits for them runs into its limit
-  const bool no_copies = pv.debug_hold & 1, no_mma = pv.debug_hold & 2;
-  uint32_t it = 0, issued = 0;                        // tiles worked on and copied; MMA phases follow `it`
-  int ll = 0, u = u0;
+  // test hook: held MMAs, so that what waits for them runs into its limit
+  const bool no_mma = pv.debug_hold & 2;
+  uint32_t it = 0, copied = 0;                        // tiles worked on (MMA phases follow it); tiles of the unit that were copied
+  int ll = 0, u = u0, layer = 0, asked = 0;
+  UnitInfo x;
 
-  for (;;) {
-    // ---- the next unit: those assigned to the CTA, layer by layer, then those handed out at run time
-    UnitInfo x;
-    int layer;
+  // ---- the next unit: those assigned to the CTA, layer by layer, then those handed out at run time (`taken`, from the counter)
+  auto next_unit = [&](int taken) {
+    int id = u, off = a.off_tunit;
     if (u0 < u1 && ll < a.layer_count) {
-      x = load_unit(plan, a.off_tunit, 0, u);
       layer = ll;
       if (++u == u1) { u = u0; ++ll; }
     } else {
-      if (a.n_dunits == 0) break;
-      if (tid == 0) unit_s[0] = atomicAdd(counter, 1);
-      __syncthreads();
-      const int id = unit_s[0];
-      if (id >= a.n_dunits * a.layer_count) break;
-      layer = id / a.n_dunits;
-      x = load_unit(plan, a.off_dunit, 0, id - layer * a.n_dunits);
-      // (the word is written again behind the unit's barriers)
+      if (a.n_dunits == 0 || taken >= a.n_dunits * a.layer_count) return false;
+      layer = taken / a.n_dunits;
+      id = taken - layer * a.n_dunits;
+      off = a.off_dunit;
     }
+    x = load_unit(plan, off, 0, id);
+    return true;
+  };
+  auto all_assigned = [&]() { return !(u0 < u1 && ll < a.layer_count); };
+  // Copies: every warp has PW pages of a tile, 16 bytes to a lane (bulk copies take 100 to 150 cycles each where eight leave together,
+  // and the next barrier waits for the warps that issue them).  A lane holds a page's id and meta, asked for a tile ahead.
+  constexpr int PW = PASTA_TILE_PAGES / (4 * H), PARTS = L::BLOCK / 16;
+  int next_page = -1, next_meta = -1;                 // lane PW t + i: page i of the t-th tile asked for (-1: no page here)
+  auto ask = [&](int count) {
+    const int at = (x.tile_begin + asked + lane / PW) * PASTA_TILE_PAGES + warp * PW + lane % PW;
+    next_page = next_meta = -1;
+    if (lane < count * PW && at < x.n_pages) {
+      next_page = plan[a.off_pages + x.page_off + at];
+      next_meta = plan[a.off_pmeta + x.page_off + at];
+    }
+    asked += count;
+  };
+  auto copy = [&](int t) {
+    const int s = copied % L::STAGES;
+    if (lane / PW == t) {
+      if (next_page < -1 || next_page >= pv.n_pages) { report(pv.status, PASTA_ERR_DEVICE_CHECK); next_page = next_meta = -1; }
+      meta_s[s * PASTA_TILE_PAGES + warp * PW + lane % PW] = next_meta;
+    }
+    const uint8_t *head = pv.kv_base + (a.layer_begin + layer) * pv.layer_stride + static_cast<int64_t>(x.g) * L::BLOCK;
+    const uint8_t *src[PW];
+    bool there[PW];
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      const int page = __shfl_sync(0xffffffffu, next_page, PW * t + i);
+      there[i] = page >= 0;
+      src[i] = head + static_cast<int64_t>(page) * pv.n_kv_heads * L::BLOCK + (lane - i * PARTS) * 16;
+    }
+    const uint32_t dst = base + L::OFF_STAGE + s * L::STAGE_BYTES + warp * PW * L::BLOCK + lane * 16;
+#pragma unroll
+    for (int i = 0; i < (PW * PARTS + 31) / 32; ++i) {
+      const bool second = PW == 2 && lane + 32 * i >= PARTS;
+      if (lane + 32 * i < PW * PARTS && (second ? there[PW - 1] : there[0])) copy16(dst + i * 512, (second ? src[PW - 1] : src[0]) + i * 512, policy);
+    }
+    ++copied;
+  };
+  // a unit's first tiles; a group of copies per stage, empty where the unit has no tile for it
+  auto first_copies = [&]() {
+    const int nt = x.tile_end - x.tile_begin;
+    asked = 0;
+    copied = 0;
+    ask(min(nt, L::STAGES));
+#pragma unroll 1
+    for (int t = 0; t < L::STAGES; ++t) {
+      if (t < nt) copy(t);
+      copies_commit();
+    }
+    ask(asked < nt);
+  };
+
+  if (all_assigned()) {
+    if (tid == 0) unit_s[0] = a.n_dunits ? atomicAdd(counter, 1) : 0;
+    __syncthreads();
+  }
+  bool more = next_unit(unit_s[0]);
+  if (more) first_copies();
+  while (more) {
     const int nt = x.tile_end - x.tile_begin;
     const int rows = x.n_threads << g_shift, n = (rows + 15) & ~15;
-    const uint8_t *kv_head = pv.kv_base + (a.layer_begin + layer) * pv.layer_stride + static_cast<int64_t>(x.g) * L::BLOCK;
     const bool fin = x.final_rows != 0;
-    // one tile's copies, by the first warp: a lane per page.  Its page id and meta were asked for a tile ahead.
-    int next_page = 0, next_meta = -1, asked = 0;
-    auto ask = [&]() {
-      next_page = 0;
-      next_meta = -1;
-      const int at = (x.tile_begin + asked) * PASTA_TILE_PAGES + lane;
-      if (lane < PASTA_TILE_PAGES && asked < nt && at < x.n_pages) {
-        next_page = plan[a.off_pages + x.page_off + at];
-        next_meta = plan[a.off_pmeta + x.page_off + at];
-      }
-      ++asked;
-    };
-    auto copy = [&]() {
-      const int s = issued % L::STAGES;
-      const int n_valid = min(PASTA_TILE_PAGES, x.n_pages - (x.tile_begin + asked - 1) * PASTA_TILE_PAGES);
-      if (next_page < 0 || next_page >= pv.n_pages) { report(pv.status, PASTA_ERR_DEVICE_CHECK); next_page = 0; next_meta = -1; }
-      if (lane < PASTA_TILE_PAGES) meta_s[s * PASTA_TILE_PAGES + lane] = next_meta;
-      __syncwarp();
-      if (lane == 0) mbar_expect_tx(bar + 8 * (L::B_FULL + s), n_valid * L::BLOCK);
-      __syncwarp();
-      if (lane < n_valid)
-        bulk_g2s_stream(base + L::OFF_STAGE + s * L::STAGE_BYTES + lane * L::BLOCK,
-                        kv_head + static_cast<int64_t>(next_page) * pv.n_kv_heads * L::BLOCK, L::BLOCK, bar + 8 * (L::B_FULL + s), policy);
-      ++issued;
-      ask();
-    };
-    if (warp == 0 && !no_copies) {
-      ask();
-      for (int k = 0; k < L::STAGES && k < nt; ++k) copy();
-    }
 
     // ---- stacked queries, four threads to a row; a row's first reference: NaN spoils a row whose query is not finite
     {
@@ -314,6 +355,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       }
       fence_proxy_async();
     }
+    copies_wait<L::STAGES - 1>();
+    __syncthreads();
     float l[L::CHUNKS][8];
 #pragma unroll
     for (int c = 0; c < L::CHUNKS; ++c)
@@ -321,13 +364,21 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       for (int j = 0; j < 8; ++j) l[c][j] = 0.f;
 
     for (int k = 0; k < nt; ++k, ++it) {
-      const int s = it % L::STAGES;
+      const int s = k % L::STAGES;
       const uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
       // ---- K's codes to the A operand, a thread per token (half the channels); the P.V before has read what it replaces
-      cta_wait(bar + 8 * (L::B_FULL + s), (it / L::STAGES) & 1, abort_flag, limit);
       if (k > 0) cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
       tc_fence_after();
       const int meta = meta_s[s * PASTA_TILE_PAGES + (token >> 4)];
+      // How much of this token's page the request's threads see, 16 threads at a time, one to a lane of the half warp that has the page;
+      // pages that every thread sees in full need no look.
+      const bool masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
+      auto visible = [&](int t0) {
+        const int t = t0 + (lane & 15);
+        if (meta < 0 || t >= x.n_threads) return 0;
+        return plan[a.off_vis + x.vis_off + t * x.n_streams + min(PASTA_PMETA_STREAM(meta), x.n_streams - 1)] - PASTA_PMETA_PAGE(meta) * PASTA_PAGE;
+      };
+      int visible_here = masked ? visible(0) : 0;
       {
         const uint8_t *block = stage + (token >> 4) * L::BLOCK;
         const uint8_t *at = block + (token & 15) * 16, *at_scale = block + kv4_k_scales(D) + (token & 15) * (D / 16);
@@ -348,7 +399,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       tmem_st_wait();
       tc_fence_before();
       __syncthreads();
-      if (warp == (it & 3) && lane == 0 && !no_mma) {
+      if (warp == (it & 3) && !no_mma && elect_lane()) {
         // ---- S^T = K . Q^T
         tc_fence_after();
         const uint32_t idesc = IDESC4 | ((static_cast<uint32_t>(n) >> 3) << 17);
@@ -358,20 +409,18 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         mma_commit(bar + 8 * L::B_QK);
       }
       __syncwarp();
-      // ---- which rows see this token (a bit each); pages that every thread of the request sees in full need no look
-      const bool masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
+      // ---- which rows see this token (a bit each)
       uint32_t seen[(NMAX + 31) / 32];
       if (masked) {
-        const int pos = PASTA_PMETA_PAGE(meta) * PASTA_PAGE + (token & 15);
-        const int32_t *vis = plan + a.off_vis + x.vis_off + (meta < 0 ? 0 : PASTA_PMETA_STREAM(meta));
         int thread = 0;
 #pragma unroll
         for (int w = 0; w < (NMAX + 31) / 32; ++w) {
           seen[w] = 0;
 #pragma unroll 4
-          for (int j = 0; j < 32 && thread < x.n_threads; j += G, ++thread)
-            if (pos < vis[thread * x.n_streams]) seen[w] |= ((1u << G) - 1) << j;
-          if (meta < 0) seen[w] = 0;
+          for (int j = 0; j < 32 && thread < x.n_threads; j += G, ++thread) {
+            if (thread != 0 && (thread & 15) == 0) visible_here = visible(thread);
+            if ((lane & 15) < __shfl_sync(0xffffffffu, visible_here, (lane & 16) | (thread & 15))) seen[w] |= ((1u << G) - 1) << j;
+          }
         }
       }
       cta_wait(bar + 8 * L::B_QK, it & 1, abort_flag, limit);
@@ -441,12 +490,21 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         if (L::NARROW) return reinterpret_cast<uint4 *>(sm + (p_row ^ ((col & 3) << 4)));
         return reinterpret_cast<uint4 *>(sm + (p_row ^ ((col & 7) << 4)) + (col >> 3) * 1024);
       };
-      uint32_t w[L::CHUNKS][4];
       // Weights rounded to bf16, as rows of the B operand; returns the largest exponent.  Straight code for every number of chunks
       // (rows beyond the unit's last are zeros in Q and count for nothing): a branch costs as much as half a chunk, and chunks overlap.
+      // Capped scores take so much code that fetching it costs more than that: a loop over the chunks.
+      auto chunk_weights = [&](int c, float *y, float &top, uint32_t *o, auto hidden) {
+        relative(c, y, hidden);
+        top = max3(max3(top, y[0], y[1]), y[2], y[3]);
+        top = max3(max3(top, y[4], y[5]), y[6], y[7]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = pack_bf16(fast_exp2(y[2 * j]), fast_exp2(y[2 * j + 1]));
+        *place(c) = make_uint4(o[0], o[1], o[2], o[3]);
+      };
       auto weights = [&](auto chunks, auto hidden) {
         constexpr int C = decltype(chunks)::value;
         float top = -INFINITY;
+        uint32_t o[4];
 #pragma unroll
         for (int c0 = 0; c0 < C; c0 += 4) {
           float v[4][8];
@@ -458,17 +516,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           for (int i = 1; i < 4; ++i)
             if (c0 + i < C) tmem_ld_order8(reinterpret_cast<uint32_t *>(v[i]));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (c0 + i >= C) continue;
-            float *y = v[i];
-            relative(H * (c0 + i) + half, y, hidden);
-            top = max3(max3(top, y[0], y[1]), y[2], y[3]);
-            top = max3(max3(top, y[4], y[5]), y[6], y[7]);
-            uint32_t *o = w[c0 + i < L::CHUNKS ? c0 + i : 0];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(fast_exp2(y[2 * j]), fast_exp2(y[2 * j + 1]));
-            *place(H * (c0 + i) + half) = make_uint4(o[0], o[1], o[2], o[3]);
-          }
+          for (int i = 0; i < 4; ++i)
+            if (c0 + i < C) chunk_weights(H * (c0 + i) + half, v[i], top, o, hidden);
         }
         return top;
       };
@@ -481,18 +530,35 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         return -INFINITY;
       };
       auto all_weights = [&]() {
-        return by_chunks([&](auto chunks) { return masked ? weights(chunks, std::true_type()) : weights(chunks, std::false_type()); });
+        if constexpr (kCap) {
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int c = half; 8 * c < n; c += H) {
+            float y[8];
+            uint32_t o[4];
+            scores(c, y);
+            tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
+            if (masked) chunk_weights(c, y, top, o, std::true_type());
+            else chunk_weights(c, y, top, o, std::false_type());
+          }
+          return top;
+        } else {
+          return by_chunks([&](auto chunks) { return masked ? weights(chunks, std::true_type()) : weights(chunks, std::false_type()); });
+        }
       };
-      bool raised = false, left = false;
+      bool raise = k == 0, raised = false, left = false;
       for (;;) {
-        const float top = all_weights();
-        tmem_st_wait();
-        fence_proxy_async();
-        tc_fence_before();
-        // ---- everybody is done with the stage, V's operand and the weights stand, and the CTA votes (also on leaving)
-        if (!__syncthreads_or((!raised && top > R_SLACK) || *abort_flag != 0)) break;
-        left = __syncthreads_or(*abort_flag != 0);
-        if (left) break;
+        if (!raise) {
+          const float top = all_weights();
+          copies_wait<L::STAGES - 2>();                // the next tile's
+          tmem_st_wait();
+          fence_proxy_async();
+          tc_fence_before();
+          // ---- everybody is done with the stage, V's operand and the weights stand, and the CTA votes (also on leaving)
+          if (!__syncthreads_or((!raised && top > R_SLACK) || *abort_flag != 0)) break;
+          left = __syncthreads_or(*abort_flag != 0);
+          if (left) break;
+        }
         // ---- some row's reference goes up: maxima of all rows over the tile, then O and l brought to the new references
 #pragma unroll 1
         for (int c = half; 8 * c < rows; c += H) {
@@ -547,10 +613,15 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           tmem_st_wait();
         }
         raised = true;
+        raise = false;
       }
       if (left) break;
-      if (warp == 0 && !no_copies && k + L::STAGES < nt) copy();
-      if (warp == ((it + 2) & 3) && lane == 0 && !no_mma) {
+      if (k + L::STAGES < nt) {
+        copy(0);
+        ask(asked < nt);
+      }
+      copies_commit();
+      if (warp == ((it + 2) & 3) && !no_mma && elect_lane()) {
         // ---- O^T += V^T . P^T
         tc_fence_after();
         const uint32_t idesc = IDESC4_PV | (((L::OW * static_cast<uint32_t>(n)) >> 3) << 17);
@@ -564,11 +635,16 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
 #pragma unroll
       for (int i = 0; i < L::CHUNKS; ++i) {
         if (8 * (H * i + half) >= n) continue;
+        const uint4 w = *place(H * i + half);
+        const uint32_t o[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) add_bf16x2(l[i][2 * j], l[i][2 * j + 1], w[i][j]);
+        for (int j = 0; j < 4; ++j) add_bf16x2(l[i][2 * j], l[i][2 * j + 1], o[j]);
       }
+      // (a unit's last tile: the unit behind it, if it is one of those handed out at run time)
+      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && all_assigned()) unit_s[0] = atomicAdd(counter, 1);
     }
     if (__syncthreads_or(*abort_flag != 0)) break;
+    const int taken = unit_s[0];
 
     // ---- epilogue: sums over the tokens, then the rows of O, a thread per channel
 #pragma unroll
@@ -584,16 +660,22 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       const bool spoilt = sum != sum;
       const float m = spoilt ? not_a_row().x : sum > 0.f ? -ref_s[tid] : -INFINITY, l_all = spoilt ? not_a_row().y : sum;
       fact_s[tid] = spoilt ? NAN : fin ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
-      if (!fin) {
-        pv.part_ml[static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + tid] = make_float2(m, l_all);
-      } else if (a.lse) {
-        const int qn = plan[a.off_tq + x.tq_off + (tid >> g_shift)];
-        a.lse[(static_cast<int64_t>(layer) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (tid & (G - 1))] = (m + log2f(l_all)) * 0.6931471805599453f;
+      int at;                                          // the row's place among all rows of its kind
+      if (fin) {
+        at = (layer * a.n_queries + plan[a.off_tq + x.tq_off + (tid >> g_shift)]) * pv.n_q_heads + x.g * G + (tid & (G - 1));
+        if (a.lse) a.lse[at] = (m + log2f(l_all)) * 0.6931471805599453f;
+      } else {
+        at = layer * pv.rows_per_layer + x.row_base + tid;
+        pv.part_ml[at] = make_float2(m, l_all);
       }
+      row_s[tid] = at;                                 // (where the thread has read its row's first sum)
     }
     cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
     if (__syncthreads_or(*abort_flag != 0)) break;
     tc_fence_after();
+    // ---- the copies of the unit behind it, under way while this one's rows are written
+    more = next_unit(taken);
+    if (more) first_copies();
     const uint32_t o_addr = lane_addr + L::COL_O + (D == 64 ? (wq >> 1) * 8 : 0);
     float *sum_s = reinterpret_cast<float *>(sm + L::OFF_P) + (token & 63);
     if constexpr (D == 64) {
@@ -623,14 +705,10 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           float y = __uint_as_float(o[j]);
           if (D == 64) y += sum_s[row * 64];
           y = f == 0.f ? 0.f : y * f;                // a final row that saw nothing is written as zeros
-          if (fin) {
-            const int row_q = plan[a.off_tq + x.tq_off + (row >> g_shift)];
-            const int64_t at = ((static_cast<int64_t>(layer) * a.n_queries + row_q) * pv.n_q_heads + x.g * G + (row & (G - 1))) * D + token;
-            if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
-            else static_cast<float *>(a.out)[at] = y;
-          } else {
-            pv.part_o[(static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + row) * D + token] = y;
-          }
+          const int64_t at = static_cast<int64_t>(row_s[row]) * D + token;
+          if (!fin) pv.part_o[at] = y;
+          else if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
+          else static_cast<float *>(a.out)[at] = y;
         }
       }
     }
@@ -640,16 +718,11 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   }
 
   // ---- tear-down
+  copies_wait<0>();
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {
-    // Some wait has run out and the whole CTA has left in the middle of its work: what is still in flight (bulk copies, MMAs) ends on
-    // its own and is waited for.
-    if (warp == 0) {
-      for (uint32_t j = (issued > L::STAGES ? issued - L::STAGES : 0); j < issued; ++j)
-        mbar_wait_bounded(bar + 8 * (L::B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
-    }
-    __syncthreads();
+    // Some wait has run out and the whole CTA has left in the middle of its work: MMAs in flight end on their own and are waited for.
     if (lane == 0 && warp < 4) {                       // every warp that issues MMAs
       mma_commit(bar + 8 * L::B_DRAIN);
       mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
