@@ -41,7 +41,8 @@ namespace pasta {
 namespace {
 
 constexpr float R_SLACK = 10.f;                  // weights are at most 2^10 (bf16 and fp32 keep their precision at any size)
-constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing
+constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing (careful units)
+constexpr float R_FAINT = 8.7e-19f;              // 2^-60: sums below it may have lost weights to fp32's range
 
 // Sizes of one build: head_dim D, at most NMAX stacked rows.
 template <int D, int NMAX>
@@ -73,7 +74,9 @@ struct U {
   static constexpr int OFF_REF = OFF_MISC + 16 + 64;                     // [NMAX] references (negated)
   static constexpr int OFF_FACT = OFF_REF + NMAX * 4;                    // [NMAX] what a raised reference multiplies O and l by; 1 / l
   static constexpr int OFF_WARP = OFF_FACT + NMAX * 4;                   // [4][NMAX] a warp's maxima, or sums
-  static constexpr int SMEM_BYTES = OFF_WARP + 4 * NMAX * 4 + 1024;      // slack to align the base to 1024
+  static constexpr int OFF_SEEN = OFF_WARP + 4 * NMAX * 4;               // [4][8] threads that see something in the tile, by its quarters (16 a word),
+                                                                         // then [4][8] in the whole unit, and [8] that wait for that
+  static constexpr int SMEM_BYTES = OFF_SEEN + (32 + 32 + 8) * 4 + 1024; // slack to align the base to 1024
   static_assert((SMEM_BYTES + 1024) * RESIDENT <= 233472, "shared memory budget");
   static_assert(OFF_P % 1024 == 0 && OFF_STAGE % 16 == 0 && OFF_META % 16 == 0 && OFF_MISC % 16 == 0, "alignment");
 };
@@ -196,6 +199,9 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
   float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
   int32_t *row_s = reinterpret_cast<int32_t *>(warp_s);
+  volatile uint32_t *seen_s = reinterpret_cast<volatile uint32_t *>(sm + L::OFF_SEEN), *saw_s = seen_s + 32, *waiting_s = seen_s + 64;
+  // of threads 16 r to 16 r + 15 those that see their first tokens in this tile
+  auto fresh = [&](int r) { return waiting_s[r] & (seen_s[r] | seen_s[8 + r] | seen_s[16 + r] | seen_s[24 + r]); };
   const int32_t *plan = pv.plan;
 
   if (tid == 0) {
@@ -220,7 +226,6 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   const uint32_t tmem = misc[0];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int u0 = plan[a.off_tcta + 2 * blockIdx.x], u1 = plan[a.off_tcta + 2 * blockIdx.x + 1];
   const long long limit = pv.wait_limit;
   int32_t *counter = pv.status + PASTA_STATUS_TAIL_COUNTER;
   uint64_t policy;
@@ -242,15 +247,26 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   // test hook: held MMAs, so that what waits for them runs into its limit
   const bool no_mma = pv.debug_hold & 2;
   uint32_t it = 0, copied = 0;                        // tiles worked on (MMA phases follow it); tiles of the unit that were copied
-  int ll = 0, u = u0, layer = 0, asked = 0;
+  int ll = -1, u = 0, u1 = 0, layer = 0, asked = 0;
   UnitInfo x;
+  // The units assigned to the CTA in the next layer that has some.  A layer's ranges are taken by other CTAs than the layer's before:
+  // what makes a range slow (masks, unit ends) is the same in every layer.
+  auto next_range = [&]() {
+    while (u == u1 && ++ll < a.layer_count) {
+      const int range = (blockIdx.x + ll * (gridDim.x * 3 / 8 | 1)) % gridDim.x;
+      u = plan[a.off_tcta + 2 * range];
+      u1 = plan[a.off_tcta + 2 * range + 1];
+    }
+  };
+  next_range();
 
   // ---- the next unit: those assigned to the CTA, layer by layer, then those handed out at run time (`taken`, from the counter)
   auto next_unit = [&](int taken) {
     int id = u, off = a.off_tunit;
-    if (u0 < u1 && ll < a.layer_count) {
+    if (u < u1) {
       layer = ll;
-      if (++u == u1) { u = u0; ++ll; }
+      ++u;
+      next_range();
     } else {
       if (a.n_dunits == 0 || taken >= a.n_dunits * a.layer_count) return false;
       layer = taken / a.n_dunits;
@@ -260,7 +276,6 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     x = load_unit(plan, off, 0, id);
     return true;
   };
-  auto all_assigned = [&]() { return !(u0 < u1 && ll < a.layer_count); };
   // Copies: every warp has PW pages of a tile, 16 bytes to a lane (bulk copies take 100 to 150 cycles each where eight leave together,
   // and the next barrier waits for the warps that issue them).  A lane holds a page's id and meta, asked for a tile ahead.
   constexpr int PW = PASTA_TILE_PAGES / (4 * H), PARTS = L::BLOCK / 16;
@@ -298,11 +313,13 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     ++copied;
   };
   // a unit's first tiles; a group of copies per stage, empty where the unit has no tile for it
-  auto first_copies = [&]() {
-    const int nt = x.tile_end - x.tile_begin;
+  auto first_pages = [&]() {
     asked = 0;
     copied = 0;
-    ask(min(nt, L::STAGES));
+    ask(min(x.tile_end - x.tile_begin, L::STAGES));
+  };
+  auto first_copies = [&]() {
+    const int nt = x.tile_end - x.tile_begin;
 #pragma unroll 1
     for (int t = 0; t < L::STAGES; ++t) {
       if (t < nt) copy(t);
@@ -311,12 +328,18 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     ask(asked < nt);
   };
 
-  if (all_assigned()) {
+  if (u == u1) {
     if (tid == 0) unit_s[0] = a.n_dunits ? atomicAdd(counter, 1) : 0;
     __syncthreads();
   }
   bool more = next_unit(unit_s[0]);
-  if (more) first_copies();
+  if (more) {
+    first_pages();
+    first_copies();
+  }
+  // A row's reference is 0 at first: weights are 2^score, scores above R_SLACK raise it, and a row whose sum shows that its scores
+  // are far below (or all minus infinity) has its unit done again, carefully: first references from the first tokens' maxima.
+  bool careful = false;
   while (more) {
     const int nt = x.tile_end - x.tile_begin;
     const int rows = x.n_threads << g_shift, n = (rows + 15) & ~15;
@@ -345,7 +368,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
                         __vmaxu2(__vmaxu2(val[c].y & 0x7fff7fffu, val[c].z & 0x7fff7fffu), val[c].w & 0x7fff7fffu));
         m2 = __vmaxu2(m2, __shfl_xor_sync(0xfu << (lane & 28), m2, 1));
         m2 = __vmaxu2(m2, __shfl_xor_sync(0xfu << (lane & 28), m2, 2));
-        if (part == 0) ref_s[row] = row >= rows ? 0.f : (m2 & 0xffffu) >= 0x7f80u || m2 >= 0x7f800000u ? NAN : R_UNSET;
+        if (part == 0) ref_s[row] = row >= rows ? 0.f : (m2 & 0xffffu) >= 0x7f80u || m2 >= 0x7f800000u ? NAN : careful ? R_UNSET : 0.f;
         uint8_t *dst = sm + L::OFF_Q + (row >> 3) * 1024 + (row & 7) * 128;
 #pragma unroll
         for (int c = 0; c < PER; ++c) {
@@ -355,6 +378,9 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       }
       fence_proxy_async();
     }
+    if (tid < 8) waiting_s[tid] = tid * 16 >= x.n_threads ? 0 : 0xffffu >> max(0, 16 * tid + 16 - x.n_threads);
+    if (tid >= 32 && tid < 64) saw_s[tid - 32] = 0;
+    bool all_seen = !careful;
     copies_wait<L::STAGES - 1>();
     __syncthreads();
     float l[L::CHUNKS][8];
@@ -363,22 +389,36 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
 #pragma unroll
       for (int j = 0; j < 8; ++j) l[c][j] = 0.f;
 
+    // How much of this token's page the request's threads see, 16 threads at a time, one to a lane of the half warp that has the page
+    // (the first 32 threads are looked up a tile ahead); pages that every thread sees in full need no look.
+    int meta = 0, visible_a = 0, visible_b = 0;
+    bool masked = false, saw_all = false;
+    auto visible = [&](int t0) {
+      const int t = t0 + (lane & 15);
+      if (meta < 0 || t >= x.n_threads) return 0;
+      return plan[a.off_vis + x.vis_off + t * x.n_streams + min(PASTA_PMETA_STREAM(meta), x.n_streams - 1)] - PASTA_PMETA_PAGE(meta) * PASTA_PAGE;
+    };
+    auto look = [&](int s) {
+      meta = meta_s[s * PASTA_TILE_PAGES + (token >> 4)];
+      masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
+      if (masked) {
+        visible_a = visible(0);
+        if (x.n_threads > 16) visible_b = visible(16);
+      }
+    };
+    look(0);
     for (int k = 0; k < nt; ++k, ++it) {
       const int s = k % L::STAGES;
       const uint8_t *stage = sm + L::OFF_STAGE + s * L::STAGE_BYTES;
       // ---- K's codes to the A operand, a thread per token (half the channels); the P.V before has read what it replaces
       if (k > 0) cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
       tc_fence_after();
-      const int meta = meta_s[s * PASTA_TILE_PAGES + (token >> 4)];
-      // How much of this token's page the request's threads see, 16 threads at a time, one to a lane of the half warp that has the page;
-      // pages that every thread sees in full need no look.
-      const bool masked = __any_sync(0xffffffffu, meta < 0 || !(meta & PASTA_PMETA_ALL_VISIBLE));
-      auto visible = [&](int t0) {
-        const int t = t0 + (lane & 15);
-        if (meta < 0 || t >= x.n_threads) return 0;
-        return plan[a.off_vis + x.vis_off + t * x.n_streams + min(PASTA_PMETA_STREAM(meta), x.n_streams - 1)] - PASTA_PMETA_PAGE(meta) * PASTA_PAGE;
-      };
-      int visible_here = masked ? visible(0) : 0;
+      if (!all_seen && half == 0) {
+        for (int r = 0; 16 * r < x.n_threads; ++r) {
+          const uint32_t who = masked ? __ballot_sync(0xffffffffu, (r == 0 ? visible_a : r == 1 ? visible_b : visible(16 * r)) > 0) : 0xffffu;
+          if (lane == 0) seen_s[8 * wq + r] = who | (who >> 16);
+        }
+      }
       {
         const uint8_t *block = stage + (token >> 4) * L::BLOCK;
         const uint8_t *at = block + (token & 15) * 16, *at_scale = block + kv4_k_scales(D) + (token & 15) * (D / 16);
@@ -409,19 +449,37 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         mma_commit(bar + 8 * L::B_QK);
       }
       __syncwarp();
-      // ---- which rows see this token (a bit each)
-      uint32_t seen[(NMAX + 31) / 32];
-      if (masked) {
-        int thread = 0;
-#pragma unroll
-        for (int w = 0; w < (NMAX + 31) / 32; ++w) {
-          seen[w] = 0;
-#pragma unroll 4
-          for (int j = 0; j < 32 && thread < x.n_threads; j += G, ++thread) {
-            if (thread != 0 && (thread & 15) == 0) visible_here = visible(thread);
-            if ((lane & 15) < __shfl_sync(0xffffffffu, visible_here, (lane & 16) | (thread & 15))) seen[w] |= ((1u << G) - 1) << j;
-          }
+      bool first = false;
+      if (!all_seen) {
+        all_seen = true;
+        for (int r = 0; 16 * r < x.n_threads; ++r) {
+          const uint32_t f = fresh(r);
+          first |= f != 0;
+          all_seen &= waiting_s[r] == f;
         }
+      }
+      // ---- which threads of the request see this token, a bit each: most see all or nothing of a page, the others are gone through
+      constexpr int WORDS = (NMAX + 31) / 32;
+      uint32_t seen[WORDS];
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 2 * WORDS; ++r) {
+          if (r % 2 == 0) seen[r / 2] = 0;
+          if (16 * r >= x.n_threads) continue;
+          const int v = r == 0 ? visible_a : r == 1 ? visible_b : visible(16 * r);
+          uint32_t who = __ballot_sync(0xffffffffu, v >= PASTA_PAGE);
+          uint32_t some = __ballot_sync(0xffffffffu, v > 0 && v < PASTA_PAGE);
+          some |= some >> 16;
+          if (half == 0 && lane == 0) saw_s[8 * wq + r] |= who | (who >> 16) | some;
+          who >>= lane & 16;
+          for (; some & 0xffffu; some &= some - 1) {
+            const int j = __ffs(some) - 1;
+            if ((lane & 15) < __shfl_sync(0xffffffffu, v, (lane & 16) | j)) who |= 1u << j;
+          }
+          seen[r / 2] |= (who & 0xffffu) << (16 * (r % 2));
+        }
+      } else {
+        saw_all = true;
       }
       cta_wait(bar + 8 * L::B_QK, it & 1, abort_flag, limit);
       tc_fence_after();
@@ -445,13 +503,19 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       }
       // ---- the tile's weights
       auto hide = [&](int c, float *v) {            // c: chunk of rows
+        const int t0 = 8 * c >> g_shift;
         uint32_t w = seen[0];
 #pragma unroll
-        for (int i = 1; i < (NMAX + 31) / 32; ++i) w = (c >> 2) == i ? seen[i] : w;
-        w >>= 8 * (c & 3);
+        for (int i = 1; i < WORDS; ++i) w = (t0 >> 5) == i ? seen[i] : w;
+        w >>= t0 & 31;
+        if (g_shift >= 2) {
+          const bool low = w & 1, high = w & (g_shift == 2 ? 2 : 1);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!((w >> j) & 1)) v[j] = -INFINITY;
+          for (int j = 0; j < 8; ++j) v[j] = (j < 4 ? low : high) ? v[j] : -INFINITY;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = (w >> (j >> g_shift)) & 1 ? v[j] : -INFINITY;
+        }
       };
       // scores of chunk c as they come from the MMA; scaled (log2 units), capped and masked; and relative to the references
       auto scores = [&](int c, float *v) { tmem_ld8_issue(lane_addr + L::COL_S + c * 8, reinterpret_cast<uint32_t *>(v)); };
@@ -546,39 +610,55 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           return by_chunks([&](auto chunks) { return masked ? weights(chunks, std::true_type()) : weights(chunks, std::false_type()); });
         }
       };
-      bool raise = k == 0, raised = false, left = false;
-      for (;;) {
-        if (!raise) {
-          const float top = all_weights();
-          copies_wait<L::STAGES - 2>();                // the next tile's
-          tmem_st_wait();
-          fence_proxy_async();
-          tc_fence_before();
-          // ---- everybody is done with the stage, V's operand and the weights stand, and the CTA votes (also on leaving)
-          if (!__syncthreads_or((!raised && top > R_SLACK) || *abort_flag != 0)) break;
-          left = __syncthreads_or(*abort_flag != 0);
-          if (left) break;
+      // maxima of the rows of a chunk over the warp's tokens
+      auto maxima = [&](int c) {
+        float y[8], mine = -INFINITY;
+        scores(c, y);
+        tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
+        if (masked) finish(c, y, std::true_type());
+        else finish(c, y, std::false_type());
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float m = warp_max(y[j]);
+          if (lane == j) mine = m;
         }
-        // ---- some row's reference goes up: maxima of all rows over the tile, then O and l brought to the new references
+        if (lane < 8) warp_s[wq * NMAX + 8 * c + lane] = mine;
+      };
+      auto maximum = [&]() { return fmaxf(fmaxf(warp_s[tid], warp_s[NMAX + tid]), fmaxf(warp_s[2 * NMAX + tid], warp_s[3 * NMAX + tid])); };
+      if (first) {
+        // ---- rows that see their first tokens get their references before any weight is worked out (their O and l are zero)
 #pragma unroll 1
         for (int c = half; 8 * c < rows; c += H) {
-          float y[8], mine = -INFINITY;
-          scores(c, y);
-          tmem_ld_wait8(reinterpret_cast<uint32_t *>(y));
-          if (masked) finish(c, y, std::true_type());
-          else finish(c, y, std::false_type());
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float m = warp_max(y[j]);
-            if (lane == j) mine = m;
-          }
-          if (lane < 8) warp_s[wq * NMAX + 8 * c + lane] = mine;
+          const int t0 = 8 * c >> g_shift, t1 = (8 * c + 7) >> g_shift;
+          if (fresh(t0 >> 4) & ((2u << (t1 & 15)) - (1u << (t0 & 15)))) maxima(c);
         }
+        __syncthreads();
+        if (tid < rows && ((fresh(tid >> g_shift >> 4) >> (tid >> g_shift & 15)) & 1) && ref_s[tid] == R_UNSET) {
+          const float m = maximum();
+          if (m > -INFINITY) ref_s[tid] = -m;
+        }
+        __syncthreads();
+        if (tid < 8) waiting_s[tid] &= ~fresh(tid);
+      }
+      bool raised = false, left = false;
+      for (;;) {
+        const float top = all_weights();
+        copies_wait<L::STAGES - 2>();                // the next tile's
+        tmem_st_wait();
+        fence_proxy_async();
+        tc_fence_before();
+        // ---- everybody is done with the stage, V's operand and the weights stand, and the CTA votes (also on leaving)
+        if (!__syncthreads_or((!raised && top > R_SLACK) || *abort_flag != 0)) break;
+        left = __syncthreads_or(*abort_flag != 0);
+        if (left) break;
+        // ---- some row's reference goes up: maxima of all rows over the tile, then O and l brought to the new references
+#pragma unroll 1
+        for (int c = half; 8 * c < rows; c += H) maxima(c);
         __syncthreads();
         if (tid < n) {
           float f = 1.f;
           if (tid < rows) {
-            const float m = fmaxf(fmaxf(warp_s[tid], warp_s[NMAX + tid]), fmaxf(warp_s[2 * NMAX + tid], warp_s[3 * NMAX + tid]));
+            const float m = maximum();
             const float old = ref_s[tid];
             if (m > -INFINITY && (old == R_UNSET || m + old > R_SLACK)) {
               f = old == R_UNSET ? 0.f : fast_exp2(-old - m);          // (a row that has seen nothing has nothing to bring along)
@@ -613,7 +693,6 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
           tmem_st_wait();
         }
         raised = true;
-        raise = false;
       }
       if (left) break;
       if (k + L::STAGES < nt) {
@@ -640,11 +719,12 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
 #pragma unroll
         for (int j = 0; j < 4; ++j) add_bf16x2(l[i][2 * j], l[i][2 * j + 1], o[j]);
       }
+      if (k + 1 < nt) look((k + 1) % L::STAGES);
       // (a unit's last tile: the unit behind it, if it is one of those handed out at run time)
-      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && all_assigned()) unit_s[0] = atomicAdd(counter, 1);
+      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && u == u1 && !careful) unit_s[0] = atomicAdd(counter, 1);
     }
+    if (saw_all && half == 0 && lane < 8) saw_s[8 * wq + lane] = 0xffffu;
     if (__syncthreads_or(*abort_flag != 0)) break;
-    const int taken = unit_s[0];
 
     // ---- epilogue: sums over the tokens, then the rows of O, a thread per channel
 #pragma unroll
@@ -655,6 +735,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       if ((lane & 3) == 0) warp_s[wq * NMAX + 8 * c + (lane >> 2)] = t;
     }
     __syncthreads();
+    bool faint = false;
     if (tid < rows) {
       const float sum = (warp_s[tid] + warp_s[NMAX + tid]) + (warp_s[2 * NMAX + tid] + warp_s[3 * NMAX + tid]);
       const bool spoilt = sum != sum;
@@ -668,14 +749,27 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         at = layer * pv.rows_per_layer + x.row_base + tid;
         pv.part_ml[at] = make_float2(m, l_all);
       }
+      const int thread = tid >> g_shift;
+      const uint32_t saw = saw_s[thread >> 4] | saw_s[8 + (thread >> 4)] | saw_s[16 + (thread >> 4)] | saw_s[24 + (thread >> 4)];
+      faint = !careful && sum < R_FAINT && ((saw >> (thread & 15)) & 1);
       row_s[tid] = at;                                 // (where the thread has read its row's first sum)
     }
     cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
-    if (__syncthreads_or(*abort_flag != 0)) break;
+    const bool again = __syncthreads_or(faint || *abort_flag != 0);
+    if (again && __syncthreads_or(*abort_flag != 0)) break;
     tc_fence_after();
     // ---- the copies of the unit behind it, under way while this one's rows are written
-    more = next_unit(taken);
-    if (more) first_copies();
+    const int taken = unit_s[0];
+    if (again) careful = true;
+    else {
+      careful = false;
+      more = next_unit(taken);
+    }
+    if (more) {
+      first_pages();
+      first_copies();
+    }
+    if (again) continue;
     const uint32_t o_addr = lane_addr + L::COL_O + (D == 64 ? (wq >> 1) * 8 : 0);
     float *sum_s = reinterpret_cast<float *>(sm + L::OFF_P) + (token & 63);
     if constexpr (D == 64) {

@@ -235,7 +235,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
       }
     }
-    const double overhead = 1.0;
+    const double overhead = lim.kv4 ? 2.0 : 1.0;       // what a unit's beginning and end take, in tiles
     const int32_t min_piece = 1;
     double total = 0;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
