@@ -10,6 +10,9 @@ namespace pasta {
 // one response with 10-tile runs: a CTA that walks a run alone needs 2.9 us per tile more, the merge kernel that cutting
 // brings with it 10.7 us, so cutting pays from the fourth tile on.
 constexpr int32_t kWholeRunSlackTiles = 3;
+// 4-bit pools, in thousands of cycles (measured with full SMs): a tile and each of its rows (padded to 16), without and with capped
+// scores, what masks multiply that by, and a unit's beginning and end and each of its rows.
+constexpr double kKv4Tile = 2.9, kKv4TileRow = 0.029, kKv4CappedRow = 0.13, kKv4Masked = 1.15, kKv4Unit = 5.5, kKv4UnitRow = 0.09;
 // Even cuts (8-bit pools, head_dim 64): pieces of at least 2 tiles and about one per resident CTA, and runs left whole while
 // the longest is at most 12 tiles longer than an even share (they then go to CTAs of six warps, which walk a tile in a third
 // of the time).  Measured, us for 1, 4, 12, 32 and 100 responses of 8 to 20 rows: 12.0, 18.0, 17.7, 30.6, 75.3; pieces of at
@@ -235,16 +238,44 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
       }
     }
-    const double overhead = lim.kv4 ? 2.0 : 1.0;       // what a unit's beginning and end take, in tiles
+    const double overhead = 1.0;
     const int32_t min_piece = 1;
-    double total = 0;
+    // 4-bit pools: pieces of equal cost instead.  cost[] of a t-request's tiles, summed up from its first.
+    static thread_local std::vector<double> cost;
+    static thread_local std::vector<size_t> cost0;
+    cost.clear(); cost0.clear();
+    auto padded = [&](size_t ti) { return (treqs[ti].n_threads * G + 15) & ~15; };
+    auto unit_cost = [&](size_t ti) { return kKv4Unit + kKv4UnitRow * padded(ti); };
+    double total = 0, unassigned = 0, left = 0;           // unassigned: cost of what has no CTA; left: of the present CTA's share
+    int32_t cta = -1;
+    if (lim.kv4) {
+      for (size_t ti = 0; ti < treqs.size(); ++ti) {
+        const TReq &t = treqs[ti];
+        cost0.push_back(cost.size());
+        const int32_t n_tiles = (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
+        const double plain = kKv4Tile + (lim.capped ? kKv4CappedRow : kKv4TileRow) * padded(ti);
+        double sum = 0;
+        cost.push_back(0);
+        for (int32_t k = 0; k < n_tiles; ++k) {
+          bool all = (k + 1) * PASTA_TILE_PAGES <= t.n_pages;
+          for (int32_t j = k * PASTA_TILE_PAGES; all && j < (k + 1) * PASTA_TILE_PAGES; ++j) all = pmeta[t.page_off + j] & PASTA_PMETA_ALL_VISIBLE;
+          cost.push_back(sum += all ? plain : plain * kKv4Masked);
+        }
+      }
+    }
+    bool any_run = false;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
       for (int32_t g = 0; g < lim.n_kv_heads; ++g) {
         const int32_t kept = n_tiles - tail[ti * lim.n_kv_heads + g];
         if (kept > 0) total += kept + overhead;
+        if (kept > 0 && lim.kv4) {
+          any_run = true;
+          unassigned += cost[cost0[ti] + kept] + unit_cost(ti);
+        }
       }
     }
+    if (any_run) unassigned += grid * unit_cost(0);        // about a cut per CTA
     const double target = std::max(total, 1.0) / grid;
     double cum = 0;
     // A small step (one response, a few threads, a context of a few hundred tokens) is not cut at all when every run can
@@ -307,6 +338,26 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
             unit_cta.push_back(run_no++);
             t_rows += rows;
             break;
+          }
+          if (lim.kv4) {
+            const double *sums = &cost[cost0[ti]], unit = unit_cost(ti);
+            // the next CTA takes an even share of what remains, unless what the present one has left is worth a unit
+            if (cta < 0 || (cta + 1 < grid && left < unit + 0.5 * (sums[begin + 1] - sums[begin]))) {
+              ++cta;
+              left = unassigned / (grid - cta);
+            }
+            int32_t end = n_tiles;
+            if (cta + 1 < grid) {
+              end = begin + 1;
+              while (end < n_tiles && 0.5 * (sums[end] + sums[end + 1]) - sums[begin] <= left - unit) ++end;
+            }
+            tunits.push_back(TUnit{static_cast<int32_t>(ti), g, begin, end, t_rows});
+            unit_cta.push_back(cta);
+            t_rows += rows;
+            left -= unit + sums[end] - sums[begin];
+            unassigned = std::max(0., unassigned - unit - (sums[end] - sums[begin]));
+            begin = end;
+            continue;
           }
           int32_t c = std::min<int32_t>(grid - 1, static_cast<int32_t>(cum / target));
           if (c + 1 < grid && (c + 1) * target - cum < min_piece) ++c;   // too close to the CTA's end: next one

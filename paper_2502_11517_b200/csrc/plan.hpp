@@ -17,6 +17,7 @@ struct PlanLimits {
   int32_t tail_percent;  // share of every long run's tiles that is handed out at run time (0: everything is assigned)
   int32_t tail_tiles;    // tiles per unit of that share
   bool kv4 = false;      // 4-bit pool: `grid` is multiplied by kv4_ctas_per_sm of the step's rows
+  bool capped = false;      // scores are capped
   bool even_cuts = false;   // t-units are launched one per CTA (8-bit pools): runs are cut into pieces of one length
 };
 
