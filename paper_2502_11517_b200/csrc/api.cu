@@ -602,7 +602,7 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
       mask |= 2;
     }
     if (timed) PASTA_CUDA(cudaEventRecord(ev[2], st));
-    if (plan_needs_merge(p->hdr)) {
+    if (plan_needs_merge(p->hdr, p->pv.kv4)) {
       PASTA_CUDA(launch_merge(p->pv, p->hdr, cnt, og, lg, st, out_bf16));
       p->launches += 1;
       mask |= 4;

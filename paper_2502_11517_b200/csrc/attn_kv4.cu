@@ -32,6 +32,7 @@
 // votes on that with the barrier that publishes the weights, and only then the rows' maxima are worked out and O and l brought to them.
 // The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.
 // Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
+#include <algorithm>
 #include <type_traits>
 
 #include "tensor_common.cuh"
@@ -207,6 +208,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   if (tid == 0) {
     for (int b = 0; b < L::B_COUNT; ++b) mbar_init(bar + 8 * b, b == L::B_DRAIN ? 4 : 1);
     misc[1] = 0;
+    unit_s[0] = -1;                                   // the last number taken
     mbar_init_fence();
   }
   fence_proxy_async();
@@ -260,6 +262,16 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   };
   next_range();
 
+  // (where nothing is assigned in advance, the first units go to the CTAs in order and the counter counts those behind them)
+  const bool none_assigned = a.n_tunits == 0;
+  const int counted_from = none_assigned ? gridDim.x : 0, n_shared = a.n_dunits * a.layer_count;
+  // The first thread takes numbers until one is past the last unit.  Every CTA ends with one such number, and the CTA that has the last
+  // of them sets the counter back.
+  auto take = [&]() {
+    const int number = counted_from + atomicAdd(counter, 1);
+    if (number == n_shared + static_cast<int>(gridDim.x) - 1) *counter = 0;
+    unit_s[0] = number;
+  };
   // ---- the next unit: those assigned to the CTA, layer by layer, then those handed out at run time (`taken`, from the counter)
   auto next_unit = [&](int taken) {
     int id = u, off = a.off_tunit;
@@ -268,9 +280,9 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       ++u;
       next_range();
     } else {
-      if (a.n_dunits == 0 || taken >= a.n_dunits * a.layer_count) return false;
-      layer = taken / a.n_dunits;
-      id = taken - layer * a.n_dunits;
+      if (a.n_dunits == 0 || taken >= n_shared) return false;
+      id = taken / a.layer_count;
+      layer = taken - id * a.layer_count;
       off = a.off_dunit;
     }
     x = load_unit(plan, off, 0, id);
@@ -328,11 +340,11 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     ask(asked < nt);
   };
 
-  if (u == u1) {
-    if (tid == 0) unit_s[0] = a.n_dunits ? atomicAdd(counter, 1) : 0;
+  if (u == u1 && !none_assigned && a.n_dunits != 0) {
+    if (tid == 0) take();
     __syncthreads();
   }
-  bool more = next_unit(unit_s[0]);
+  bool more = next_unit(none_assigned ? blockIdx.x : unit_s[0]);
   if (more) {
     first_pages();
     first_copies();
@@ -721,7 +733,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       }
       if (k + 1 < nt) look((k + 1) % L::STAGES);
       // (a unit's last tile: the unit behind it, if it is one of those handed out at run time)
-      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && u == u1 && !careful) unit_s[0] = atomicAdd(counter, 1);
+      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && u == u1 && !careful) take();
     }
     if (saw_all && half == 0 && lane < 8) saw_s[8 * wq + lane] = 0xffffu;
     if (__syncthreads_or(*abort_flag != 0)) break;
@@ -821,7 +833,10 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       mma_commit(bar + 8 * L::B_DRAIN);
       mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
     }
-    if (tid == 0) report(pv.status, PASTA_ERR_TIMEOUT);
+    if (tid == 0) {
+      while (a.n_dunits != 0 && unit_s[0] < n_shared) take();
+      report(pv.status, PASTA_ERR_TIMEOUT);
+    }
     tc_fence_before();
     __syncthreads();
   }
@@ -838,7 +853,8 @@ cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, const TensorArgs &
   const auto kernel = cap ? attn_kv4_kernel<D, NMAX, true> : attn_kv4_kernel<D, NMAX, false>;
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void *>(kernel), L::SMEM_BYTES, &prepared[cap]);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(kernel, dim3(h.w[PH_T_GRID]), dim3(L::THREADS), L::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
+  const int grid = a.n_tunits ? h.w[PH_T_GRID] : static_cast<int>(std::min<int64_t>(h.w[PH_T_GRID], int64_t(a.n_dunits) * a.layer_count));
+  return launch_overlapped(kernel, dim3(grid), dim3(L::THREADS), L::SMEM_BYTES, st, pv, a, static_cast<const __nv_bfloat16 *>(q));
 }
 
 template <int D>
@@ -859,7 +875,7 @@ cudaError_t launch_attn_kv4(const PoolView &pv, const PlanHeader &h, int32_t lay
   a.off_tunit = h.w[PH_OFF_TUNIT]; a.off_treq = h.w[PH_OFF_TREQ]; a.off_tcta = h.w[PH_OFF_TCTA];
   a.off_pages = h.w[PH_OFF_PAGES]; a.off_pmeta = h.w[PH_OFF_PMETA]; a.off_vis = h.w[PH_OFF_VIS];
   a.off_tq = h.w[PH_OFF_TQ];
-  a.off_dunit = h.w[PH_OFF_DUNIT]; a.n_dunits = h.w[PH_N_DUNITS];
+  a.off_dunit = h.w[PH_OFF_DUNIT]; a.n_dunits = h.w[PH_N_DUNITS]; a.n_tunits = h.w[PH_N_TUNITS];
   a.n_queries = h.w[PH_N_QUERIES]; a.layer_begin = layer_begin; a.layer_count = layer_count;
   a.scale_log2 = scale_log2;
   a.cap_inv = pv.softcap_log2 > 0.f ? 1.f / pv.softcap_log2 : 0.f;

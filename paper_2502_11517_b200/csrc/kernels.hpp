@@ -120,7 +120,8 @@ cudaError_t launch_stream_read(const void *src, size_t bytes, int mode, void *si
 // False when every row of the step leaves the tensor-core kernel as the output (all its units final, nothing on the
 // warp path): the merge then has nothing to do and is not launched.  A plan with shared units keeps its merge launch,
 // which also puts their counter back to zero.
-inline bool plan_needs_merge(const PlanHeader &h) { return h.w[PH_N_PARTIAL] > 0 || h.w[PH_N_DUNITS] > 0; }
+// (the kernel of 4-bit pools sets the counter of shared units back itself)
+inline bool plan_needs_merge(const PlanHeader &h, bool kv4) { return h.w[PH_N_PARTIAL] > 0 || (h.w[PH_N_DUNITS] > 0 && !kv4); }
 // out: device fp32 [layer_count, n, Hq, D], or bf16 of the same shape when out_bf16
 cudaError_t launch_merge(const PoolView &pv, const PlanHeader &h, int32_t layer_count, void *out, float *lse,
                          cudaStream_t st, bool out_bf16 = false);

@@ -13,6 +13,9 @@ constexpr int32_t kWholeRunSlackTiles = 3;
 // 4-bit pools, in thousands of cycles (measured with full SMs): a tile and each of its rows (padded to 16), without and with capped
 // scores, what masks multiply that by, and a unit's beginning and end and each of its rows.
 constexpr double kKv4Tile = 2.9, kKv4TileRow = 0.029, kKv4CappedRow = 0.13, kKv4Masked = 1.15, kKv4Unit = 5.5, kKv4UnitRow = 0.09;
+// A run stays whole up to so many shares and what the merge kernel behind cut runs takes: a launch of one layer then loses little to
+// its longest run, launches of several layers lose nothing.
+constexpr double kKv4WholeShares = 2, kKv4Merge = 40;
 // Even cuts (8-bit pools, head_dim 64): pieces of at least 2 tiles and about one per resident CTA, and runs left whole while
 // the longest is at most 12 tiles longer than an even share (they then go to CTAs of six warps, which walk a tile in a third
 // of the time).  Measured, us for 1, 4, 12, 32 and 100 responses of 8 to 20 rows: 12.0, 18.0, 17.7, 30.6, 75.3; pieces of at
@@ -216,12 +219,35 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
       grid *= kv4_ctas_per_sm(lim.head_dim, rows);
     }
+    // 4-bit pools: what a t-request's tiles cost, summed up from its first, and what all of them cost.
+    static thread_local std::vector<double> cost;
+    static thread_local std::vector<size_t> cost0;
+    cost.clear(); cost0.clear();
+    auto padded = [&](size_t ti) { return (treqs[ti].n_threads * G + 15) & ~15; };
+    auto unit_cost = [&](size_t ti) { return kKv4Unit + kKv4UnitRow * padded(ti); };
+    double all_cost = 0;
+    if (lim.kv4) {
+      for (size_t ti = 0; ti < treqs.size(); ++ti) {
+        const TReq &t = treqs[ti];
+        cost0.push_back(cost.size());
+        const int32_t n_tiles = (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
+        const double plain = kKv4Tile + (lim.capped ? kKv4CappedRow : kKv4TileRow) * padded(ti);
+        double sum = 0;
+        cost.push_back(0);
+        for (int32_t k = 0; k < n_tiles; ++k) {
+          bool all = (k + 1) * PASTA_TILE_PAGES <= t.n_pages;
+          for (int32_t j = k * PASTA_TILE_PAGES; all && j < (k + 1) * PASTA_TILE_PAGES; ++j) all = pmeta[t.page_off + j] & PASTA_PMETA_ALL_VISIBLE;
+          cost.push_back(sum += all ? plain : plain * kKv4Masked);
+        }
+        all_cost += lim.n_kv_heads * (sum + unit_cost(ti));
+      }
+    }
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
     // run time (equal tile counts do not finish at the same time: SMs differ in the bandwidth they get).  Only when
     // there is enough work for that to matter.
     int64_t all_tiles = 0;
     for (const TReq &t : treqs) all_tiles += int64_t(lim.n_kv_heads) * ((t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES);
-    const bool share_tail = lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * grid;
+    const bool share_tail = !lim.kv4 && lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * grid;
     // Runs of a few tiles go to the pool whole, every so often, until the pool holds its share of their tiles (`owed`
     // counts what they still owe it): a whole run is a unit anyway, so sharing it costs no extra cut and no extra
     // partial rows.  Long runs stay assigned: cutting their ends into short units cost more, in unit changes and
@@ -238,31 +264,20 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
       }
     }
-    const double overhead = 1.0;
-    const int32_t min_piece = 1;
-    // 4-bit pools: pieces of equal cost instead.  cost[] of a t-request's tiles, summed up from its first.
-    static thread_local std::vector<double> cost;
-    static thread_local std::vector<size_t> cost0;
-    cost.clear(); cost0.clear();
-    auto padded = [&](size_t ti) { return (treqs[ti].n_threads * G + 15) & ~15; };
-    auto unit_cost = [&](size_t ti) { return kKv4Unit + kKv4UnitRow * padded(ti); };
-    double total = 0, unassigned = 0, left = 0;           // unassigned: cost of what has no CTA; left: of the present CTA's share
-    int32_t cta = -1;
-    if (lim.kv4) {
+    // 4-bit pools: every run that is not much longer than an even share goes to the pool whole, the longest first and all layers of one
+    // before the next, so that the short ones even out what CTAs and units take.  (Measured, us, against equal shares in advance:
+    // 170 for 187 with 64 requests of 4 to 9 threads, 182 for 250 with capped scores, 49 for 54 with 1 to 5 threads.)
+    if (lim.kv4 && lim.tail_percent > 0) {
+      const double longest = kKv4WholeShares * all_cost / grid + kKv4Merge;
       for (size_t ti = 0; ti < treqs.size(); ++ti) {
-        const TReq &t = treqs[ti];
-        cost0.push_back(cost.size());
-        const int32_t n_tiles = (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
-        const double plain = kKv4Tile + (lim.capped ? kKv4CappedRow : kKv4TileRow) * padded(ti);
-        double sum = 0;
-        cost.push_back(0);
-        for (int32_t k = 0; k < n_tiles; ++k) {
-          bool all = (k + 1) * PASTA_TILE_PAGES <= t.n_pages;
-          for (int32_t j = k * PASTA_TILE_PAGES; all && j < (k + 1) * PASTA_TILE_PAGES; ++j) all = pmeta[t.page_off + j] & PASTA_PMETA_ALL_VISIBLE;
-          cost.push_back(sum += all ? plain : plain * kKv4Masked);
-        }
+        const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
+        if (cost[cost0[ti] + n_tiles] + unit_cost(ti) <= longest) std::fill_n(tail.begin() + ti * lim.n_kv_heads, lim.n_kv_heads, n_tiles);
       }
     }
+    const double overhead = 1.0;
+    const int32_t min_piece = 1;
+    double total = 0, unassigned = 0, left = 0;           // unassigned: cost of what has no CTA; left: of the present CTA's share
+    int32_t cta = -1;
     bool any_run = false;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
@@ -294,7 +309,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       }
       // (8-bit pools: whole runs go to CTAs of six warps, a third as many to an SM)
       const int32_t ctas = lim.even_cuts ? std::max(1, grid / 3) : grid;
-      whole_runs = n_runs > 0 && n_runs <= ctas &&
+      whole_runs = !lim.kv4 && n_runs > 0 && n_runs <= ctas &&
                    longest <= kept_tiles / ctas + (lim.even_cuts ? kEvenWholeSlackTiles : kWholeRunSlackTiles);
     }
     // One CTA per unit (no persistent ranges): a run is cut into equal pieces of at most `piece` tiles, long enough to
@@ -312,7 +327,14 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       }
     }
     int32_t run_no = 0;
-    for (size_t ti = 0; ti < treqs.size(); ++ti) {
+    static thread_local std::vector<size_t> order;
+    order.resize(treqs.size());
+    for (size_t i = 0; i < order.size(); ++i) order[i] = i;
+    if (lim.kv4) {
+      auto cost_of = [&](size_t ti) { return cost[cost0[ti] + (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES]; };
+      std::stable_sort(order.begin(), order.end(), [&](size_t a, size_t b) { return cost_of(a) > cost_of(b); });
+    }
+    for (const size_t ti : order) {
       const int32_t all = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
       const int32_t rows = treqs[ti].n_threads * G;
       for (int32_t g = 0; g < lim.n_kv_heads; ++g) {
@@ -375,8 +397,9 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
         trange[(ti * lim.n_kv_heads + g) * 2 + 1] = static_cast<int32_t>(tunits.size());
         drange[(ti * lim.n_kv_heads + g) * 2] = static_cast<int32_t>(dunits.size());
-        for (int32_t b2 = n_tiles; b2 < all; b2 += lim.tail_tiles) {
-          dunits.push_back(TUnit{static_cast<int32_t>(ti), g, b2, std::min(all, b2 + lim.tail_tiles), t_rows});
+        const int32_t piece2 = lim.kv4 ? all : lim.tail_tiles;
+        for (int32_t b2 = n_tiles; b2 < all; b2 += piece2) {
+          dunits.push_back(TUnit{static_cast<int32_t>(ti), g, b2, std::min(all, b2 + piece2), t_rows});
           t_rows += rows;
         }
         drange[(ti * lim.n_kv_heads + g) * 2 + 1] = static_cast<int32_t>(dunits.size());

@@ -261,6 +261,7 @@ __device__ __forceinline__ UnitInfo load_unit(const int32_t *plan, int off_tunit
 
 struct TensorArgs {
   int32_t off_tunit, off_treq, off_tcta, off_pages, off_pmeta, off_vis, off_tq;
+  int32_t n_tunits;                 // (4-bit pools) units assigned to CTAs in advance, per layer
   int32_t off_dunit, n_dunits;      // units no CTA owns in advance (per layer): taken from a counter at run time
   int32_t n_queries, layer_begin, layer_count;
   float scale_log2;
@@ -273,14 +274,14 @@ struct TensorArgs {
 // A role's place in its CTA's sequence of units: first the units assigned to the CTA, layer by layer, whose records every
 // role reads from the plan itself; then units of the shared pool (whole short runs kept back by the planner), taken from
 // a counter in global memory.  Only the producer, which gets to every unit first, touches the counter: it publishes the
-// record (and layer) of each shared unit it takes in a ring of kRing slots in shared memory, and the other roles read
+// record (and layer) of each shared unit it takes in a ring of T_RING slots in shared memory, and the other roles read
 // the records from there in the same order, without a round trip to global memory at the start of a unit.  A record
 // with tile_end = 0 ends the sequence.  The producer is at most its stages' number of tiles, hence units, ahead of the tile whose
 // P.V has finished, and no role is a whole unit behind that one when it reads its next record, so a slot is not
 // overwritten before everybody has read it.
 struct Walk { int ll, u, k; };
 
-template <bool kProducer, bool kShared, int kRing = T_RING>
+template <bool kProducer, bool kShared>
 __device__ __forceinline__ bool next_unit(Walk &w, const TensorArgs &a, const int32_t *plan, int u0, int u1, volatile int *ring,
                                           int32_t *counter, int lane, bool whole_warp, volatile int *abort_flag,
                                           long long limit, bool &ok, UnitInfo &x, int &ll) {
@@ -292,7 +293,7 @@ __device__ __forceinline__ bool next_unit(Walk &w, const TensorArgs &a, const in
   }
   if (!kShared) return false;        // this build of the kernel serves plans without shared units
   if (a.n_dunits == 0) return false;
-  int32_t *slot = const_cast<int32_t *>(reinterpret_cast<volatile int32_t *>(ring)) + 2 + 16 * (w.k % kRing);
+  int32_t *slot = const_cast<int32_t *>(reinterpret_cast<volatile int32_t *>(ring)) + 2 + 16 * (w.k % T_RING);
   if (kProducer) {
     int id = -1;
     if (lane == 0) {
