@@ -12,7 +12,8 @@
 // a division per element:
 //   bf16 numbers   x / s is at least 2^-10 away from k + 1/2 unless it is k + 1/2, so x (1/s) is rounded to a multiple of 2^-13
 //                  first (a tie comes out as the tie it is) and to a whole number then;
-//   rotated keys   (fp32) n0 = nearest to x (1/s), then x - n0 s, which is exact, is compared with s / 2.
+//   rotated keys   (fp32) the whole number nearest to x (1/s); a lane that has a quotient within 2^-18 of the middle of two codes
+//                  (one in about 10^4) compares x - n s, which is exact, with s / 2.
 // An element that is not finite is stored as zero and reported (PASTA_ERR_DEVICE_CHECK), as in an 8-bit pool.
 //
 // What bounds it: memory.  2 bytes of bf16 in and 9/16 of a byte out per element, one pass.
@@ -29,22 +30,54 @@ namespace {
 
 constexpr float kScaleMin = 0x1p-110f, kScaleMax = 31 * 0x1p106f;
 
-// The scale of a group whose largest magnitude is amax (finite).  amax / 7 rounded to fp32 is never below a number of five
-// bits that the quotient exceeds (its distance is at least 1/7 of a step of amax, more than half a step of the quotient).
+// Two fp32 numbers in a 64-bit register: one instruction for both.
+using float_pair = unsigned long long;
+__device__ __forceinline__ float_pair pair_of(float a, float b) {
+  float_pair y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void both(float_pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ float_pair fma_pair(float_pair a, float_pair b, float_pair c) {
+  float_pair y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+__device__ __forceinline__ float_pair add_pair(float_pair a, float_pair b) {
+  float_pair y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ float_pair same(float a) { return pair_of(a, a); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float s) {      // to an ulp
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+  return y;
+}
+
+// The scale of a group whose largest magnitude is amax (finite).  The constant is less than 1/7 by more than the product's rounding,
+// so what rounding up to five bits gives is the scale or the number of five bits below it; 7 s is exact.
 __device__ __forceinline__ float group_scale(float amax) {
-  const float s = __uint_as_float((__float_as_uint(__fdiv_rn(amax, 7.f)) + 0x7ffffu) & 0xfff80000u);
+  float s = __uint_as_float((__float_as_uint(amax * 0.14285709f) + 0x7ffffu) & 0xfff80000u);
+  if (7.f * s < amax) s = __uint_as_float(__float_as_uint(s) + 0x80000u);
   return fminf(fmaxf(s, kScaleMin), kScaleMax);
 }
 __device__ __forceinline__ uint32_t scale_bits(float s) { return __float_as_uint(16.f * s) >> 16; }      // t, a bf16 number
 
-// whole number of scales nearest to a bf16 number x, as fp32 (|x| <= 7 s); r = 1 / s
-__device__ __forceinline__ float code_of_bf16(float x, float r) {
-  // 1536 = 1.5 * 2^10: the sum is a multiple of 2^-13; 12582912 = 1.5 * 2^23
-  return ((fmaf(x, r, 1536.f) - 1536.f) + 12582912.f) - 12582912.f;
+constexpr float kWhole = 12582912.f;              // 1.5 * 2^23: a sum with it is a whole number
+// whole numbers of scales nearest to two bf16 numbers, as fp32 (|x| <= 7 s); r = 1 / s
+__device__ __forceinline__ float_pair codes_of_bf16(float_pair x, float_pair r) {
+  // 1536 = 1.5 * 2^10: the sum is a multiple of 2^-13
+  return add_pair(add_pair(fma_pair(x, r, same(1536.f)), same(kWhole - 1536.f)), same(-kWhole));
 }
 // the same of any fp32 number
 __device__ __forceinline__ float code_of_fp32(float x, float s, float r) {
-  float n = fmaf(x, r, 12582912.f) - 12582912.f;
+  float n = fmaf(x, r, kWhole) - kWhole;
   const float e = fmaf(-n, s, x), half = 0.5f * s;
   if (fabsf(e) >= half) {
     const bool odd = static_cast<int>(n) & 1;
@@ -52,32 +85,51 @@ __device__ __forceinline__ float code_of_fp32(float x, float s, float r) {
   }
   return n;
 }
-// Word of eight codes n[0..7].  The sums are whole numbers below 2^24, hence exact.
-__device__ __forceinline__ uint32_t code_word(const float *n) {
-  const float lo = fmaf(n[6], 4096.f, fmaf(n[4], 256.f, fmaf(n[2], 16.f, n[0]))) + (8388608.f + 34952.f);      // 34952: 8 in each code
-  const float hi = fmaf(n[7], 4096.f, fmaf(n[5], 256.f, fmaf(n[3], 16.f, n[1]))) + (8388608.f + 34952.f);
+// Halves of the words of eight codes n[0..7]: lo from the even ones, hi from the odd ones; two words (or both halves of one) at a time.
+// The sums are whole numbers below 2^24, hence exact.
+__device__ __forceinline__ float_pair code_halves(float_pair n0, float_pair n1, float_pair n2, float_pair n3) {
+  return add_pair(fma_pair(n3, same(4096.f), fma_pair(n2, same(256.f), fma_pair(n1, same(16.f), n0))), same(8388608.f + 34952.f));      // 34952: 8 in each code
+}
+__device__ __forceinline__ uint32_t code_word(float lo, float hi) {
   const uint32_t w = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
   return __funnelshift_l(w, w, 3);
 }
 
 // 16 elements of a K row (16-element chunk c of token row r), as fp32 numbers of a bf16 row or of a rotated one; two lanes
-// share a group.
+// share a group.  amax: the largest magnitude of the 16.
 template <int D, bool kRotated>
-__device__ __forceinline__ void store_k16(uint8_t *block, int r, int c, bool valid, float *x) {
-  float amax = 0.f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[e]));
+__device__ __forceinline__ void store_k16(uint8_t *block, int r, int c, bool valid, float *x, float amax) {
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-  const float s = group_scale(amax), inv = __frcp_rn(s);
+  const float s = group_scale(amax), inv = reciprocal(s);
   if (s >= kScaleMax) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = fminf(fmaxf(x[e], -7.f * s), 7.f * s);
   }
-  float n[16];
+  float_pair n[8];
+  if constexpr (kRotated) {
+    // The quotient is good to 2^-19, so the code is the nearest one unless the quotient is that close to the middle of two.
+    float far = 0.f;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) n[e] = kRotated ? code_of_fp32(x[e], s, inv) : code_of_bf16(x[e], inv);
+    for (int i = 0; i < 8; ++i) {
+      const float_pair quot = fma_pair(pair_of(x[2 * i], x[2 * i + 1]), same(inv), same(0.f));
+      n[i] = add_pair(add_pair(quot, same(kWhole)), same(-kWhole));
+      float d0, d1;
+      both(fma_pair(n[i], same(-1.f), quot), d0, d1);
+      far = max3(far, fabsf(d0), fabsf(d1));
+    }
+    if (far > 0.5f - 0x1p-18f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[i] = pair_of(code_of_fp32(x[2 * i], s, inv), code_of_fp32(x[2 * i + 1], s, inv));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n[i] = codes_of_bf16(pair_of(x[2 * i], x[2 * i + 1]), same(inv));
+  }
   if (!valid) return;
-  *reinterpret_cast<uint2 *>(block + (c >> 1) * 256 + r * 16 + (c & 1) * 8) = make_uint2(code_word(n), code_word(n + 8));
+  float lo[2], hi[2];
+  both(code_halves(n[0], n[1], n[2], n[3]), lo[0], hi[0]);
+  both(code_halves(n[4], n[5], n[6], n[7]), lo[1], hi[1]);
+  *reinterpret_cast<uint2 *>(block + (c >> 1) * 256 + r * 16 + (c & 1) * 8) = make_uint2(code_word(lo[0], hi[0]), code_word(lo[1], hi[1]));
   if ((c & 1) == 0)
     *reinterpret_cast<uint16_t *>(block + kv4_k_scales(D) + (r * (D / kKv4Group) + (c >> 1)) * 2) = static_cast<uint16_t>(scale_bits(s));
 }
@@ -92,26 +144,30 @@ __device__ __forceinline__ bool clean_word(uint32_t &w) {
 
 // K of tokens in rows off0 .. off0 + cnt - 1 of a page, one kv head, by a warp.  rows: the tokens' K, `stride` elements apart.
 // stage: this warp's room for the rotated rows of one pass (32 x 16 floats).
+// The rows of a pass are asked for before those of the pass ahead of it are worked on.
 template <int D, bool kRope>
 __device__ __forceinline__ bool append_k(uint8_t *block, const __nv_bfloat16 *rows, int64_t stride, int off0, int cnt,
                                          const RopeForm &form, const double2 *turn, float *stage) {
   constexpr int LPT = D / 16, TPI = 32 / LPT;
   const int lane = threadIdx.x & 31, c = lane % LPT;
+  const int c_a = kRope ? rope_chunk_a(form, c) : 2 * c, c_b = kRope ? rope_chunk_b(form, c) : 2 * c + 1;
+  const uint4 *row = reinterpret_cast<const uint4 *>(rows + (lane / LPT) * stride);
+  const int64_t step = TPI * stride / 8;
   bool bad = false;
-  for (int r0 = 0; r0 < cnt; r0 += TPI) {
-    const int r = r0 + lane / LPT;
+  uint4 next_a = make_uint4(0, 0, 0, 0), next_b = next_a;
+  if (lane / LPT < cnt) { next_a = __ldg(row + c_a); next_b = __ldg(row + c_b); }
+#pragma unroll 1
+  for (int r = lane / LPT; r - lane / LPT < cnt; r += TPI) {
     const bool valid = r < cnt;
-    const uint4 *row = reinterpret_cast<const uint4 *>(rows + r * stride);
-    float x[16];
+    uint4 a = next_a, b = next_b;
+    row += step;
+    next_a = next_b = make_uint4(0, 0, 0, 0);
+    if (r + TPI < cnt) { next_a = __ldg(row + c_a); next_b = __ldg(row + c_b); }
+    const bool odd_ones = chunk_not_finite(a) || chunk_not_finite(b);
+    float x[16], amax = 0.f;
     if constexpr (kRope) {
-      const int c_a = rope_chunk_a(form, c), c_b = rope_chunk_b(form, c);
       const bool turns = c < form.slots, alternate = form.interleaved && turns;
-      uint4 lo4 = make_uint4(0, 0, 0, 0), hi4 = lo4;
-      if (valid) { lo4 = __ldg(row + c_a); hi4 = __ldg(row + c_b); }
-      if (chunk_not_finite(lo4) || chunk_not_finite(hi4)) { bad = true; rope_clean(lo4, hi4, alternate, turns); }
-      float y[16], lo[8], hi[8];
-      rope_slot<D>(lo4, hi4, alternate, turn + (valid ? r : 0) * (D / 2), c, y);
-      rope_unslot(y, alternate, lo, hi);
+      if (odd_ones) { bad = true; rope_clean(a, b, alternate, turns); }
       // the rotated row's chunks change hands through shared memory, so that a lane holds 16 neighbouring elements
       float *mine = stage + (lane / LPT) * D;
       auto put = [&](int chunk, const float *v) {
@@ -119,36 +175,49 @@ __device__ __forceinline__ bool append_k(uint8_t *block, const __nv_bfloat16 *ro
         dst[0] = make_float4(v[0], v[1], v[2], v[3]);
         dst[1] = make_float4(v[4], v[5], v[6], v[7]);
       };
-      put(c_a, lo);
-      put(c_b, hi);
-      __syncwarp();
+      float y[16], lo[8], hi[8];
+      const double2 *t = turn + (valid ? r : 0) * (D / 2);
+      if (form.interleaved) {                     // (uniform: chunks stay with their lane)
+        rope_slot<D>(a, b, turns, t, c, y);
+        rope_unslot(y, turns, lo, hi);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 v = reinterpret_cast<const float4 *>(mine + c * 16)[e];
-        x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+        for (int e = 0; e < 8; ++e) { x[e] = lo[e]; x[8 + e] = hi[e]; }
+      } else {
+        rope_slot<D>(a, b, false, t, c, y);
+        put(c_a, y);
+        put(c_b, y + 8);
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 v = reinterpret_cast<const float4 *>(mine + c * 16)[e];
+          x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      float top = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
-      if (top == INFINITY) {                      // a rotation that left fp32 (no NaN: its operands are finite)
+      for (int e = 0; e < 16; e += 2) amax = max3(amax, fabsf(x[e]), fabsf(x[e + 1]));
+      if (amax == INFINITY) {                     // a rotation that left fp32 (no NaN: its operands are finite)
         bad = true;
+        amax = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = fabsf(x[e]) == INFINITY ? 0.f : x[e];
+        for (int e = 0; e < 16; ++e) {
+          x[e] = fabsf(x[e]) == INFINITY ? 0.f : x[e];
+          amax = fmaxf(amax, fabsf(x[e]));
+        }
       }
     } else {
-      uint4 a = make_uint4(0, 0, 0, 0), b = a;
-      if (valid) { a = __ldg(row + 2 * c); b = __ldg(row + 2 * c + 1); }
       uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-      if (chunk_not_finite(a) || chunk_not_finite(b)) {
+      if (odd_ones) {
         bad = true;
 #pragma unroll
         for (int i = 0; i < 8; ++i) clean_word(w[i]);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) amax = max3(amax, fabsf(x[e]), fabsf(x[e + 1]));
     }
-    store_k16<D, kRope>(block, off0 + r, c, valid, x);
+    store_k16<D, kRope>(block, off0 + r, c, valid, x, amax);
   }
   return bad;
 }
@@ -209,22 +278,19 @@ __device__ __forceinline__ bool append_v(uint8_t *block, const __nv_bfloat16 *ro
     // lane i of a group works out the scale of token i, and keeps it; the others ask for 1 / s
     const int who = lane & 7;
     const uint32_t pair = (who & 4) ? ((who & 2) ? m[3] : m[2]) : ((who & 2) ? m[1] : m[0]);
-    const float s = group_scale((who & 1) ? bf16_hi(pair) : bf16_lo(pair)), inv = __frcp_rn(s);
+    const float s = group_scale((who & 1) ? bf16_hi(pair) : bf16_lo(pair)), inv = reciprocal(s);
     if ((lane & (LPG - 1)) < 8 && 8 * h + who >= lo && 8 * h + who < hi)
       *reinterpret_cast<uint16_t *>(block + kv4_v_scales(D) + (lane / LPG) * 32 + (8 * h + who) * 2) = static_cast<uint16_t>(scale_bits(s));
     const bool clamp = __any_sync(0xffffffffu, s >= kScaleMax);
-    float n[CH][8];
+    float_pair n[CH / 2][8];                            // of two neighbouring channels
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float r = __shfl_sync(0xffffffffu, inv, (lane & ~7) | i);
-      float v[CH];
 #pragma unroll
-      for (int w = 0; w < CH / 2; ++w) { v[2 * w] = bf16_lo(x[i][w]); v[2 * w + 1] = bf16_hi(x[i][w]); }
-#pragma unroll
-      for (int ch = 0; ch < CH; ++ch) {
-        if (clamp) v[ch] = fminf(fmaxf(v[ch], -7.f / r), 7.f / r);
-        n[ch][i] = code_of_bf16(v[ch], r);
-        if (clamp) n[ch][i] = fminf(fmaxf(n[ch][i], -7.f), 7.f);
+      for (int w = 0; w < CH / 2; ++w) {
+        float v0 = bf16_lo(x[i][w]), v1 = bf16_hi(x[i][w]);
+        if (clamp) { v0 = fminf(fmaxf(v0, -7.f / r), 7.f / r); v1 = fminf(fmaxf(v1, -7.f / r), 7.f / r); }
+        n[w][i] = codes_of_bf16(pair_of(v0, v1), same(r));
       }
     }
     uint32_t *dst = reinterpret_cast<uint32_t *>(block + kv4_v_codes(D)) + lane * CH * 2 + h;
@@ -236,10 +302,16 @@ __device__ __forceinline__ bool append_v(uint8_t *block, const __nv_bfloat16 *ro
       keep = __funnelshift_l(keep, keep, 3);
     }
 #pragma unroll
-    for (int ch = 0; ch < CH; ++ch) {
-      uint32_t w = code_word(n[ch]);
-      if (keep) w = (w & ~keep) | (dst[2 * ch] & keep);
-      dst[2 * ch] = w;
+    for (int w = 0; w < CH / 2; ++w) {
+      float lo[2], hi[2];
+      both(code_halves(n[w][0], n[w][2], n[w][4], n[w][6]), lo[0], lo[1]);
+      both(code_halves(n[w][1], n[w][3], n[w][5], n[w][7]), hi[0], hi[1]);
+#pragma unroll
+      for (int ch = 2 * w; ch < 2 * w + 2; ++ch) {
+        uint32_t word = code_word(lo[ch & 1], hi[ch & 1]);
+        if (keep) word = (word & ~keep) | (dst[2 * ch] & keep);
+        dst[2 * ch] = word;
+      }
     }
   }
   return bad;
