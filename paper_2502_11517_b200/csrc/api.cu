@@ -410,7 +410,7 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
     PASTA_CUDA(append_codes(p, slots, pos, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new, rope_table(p, theta),
                             static_cast<cudaStream_t>(stream)));
   else if (!usual_rope(p))
-    PASTA_CUDA(launch_kv_append_form(p->pv, slots, pos, 0, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new,
+    PASTA_CUDA(launch_kv_append_form(p->pv, slots, pos, n_app, layer_begin, layer_count, tokens_stride(p, n_app), k_new, v_new,
                                      *rope_table(p, theta), static_cast<cudaStream_t>(stream)));
   else
     PASTA_CUDA(launch_kv_append_rope(p->pv, slots, pos, 0, n_app, layer_begin, layer_count, k_new, v_new, theta,
@@ -642,6 +642,11 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
                       theta > 0.f ? rope_table(p, theta) : nullptr, st, &p->launches));
     return PASTA_OK;
   }
+  if (form) {
+    PASTA_CUDA(launch_kv_append_run_form(p->pv, pages.data() + at0 / PASTA_PAGE, slot.offset, pos0, m, layer_begin, layer_count,
+                                         tokens_stride(p, m), k, v, *rope_table(p, theta), st, &p->launches));
+    return PASTA_OK;
+  }
   std::vector<int32_t> words;
   for (int32_t begin = 0; begin < m; begin += kRunChunk) {
     const int32_t cnt = std::min(kRunChunk, m - begin);
@@ -653,13 +658,6 @@ static pasta_status_t append_run_impl(pasta_pool_t *p, int32_t req, int32_t thre
     }
     s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
     if (s != PASTA_OK) return s;
-    if (form) {                                      // all layers in one launch
-      PASTA_CUDA(launch_kv_append_form(p->pv, p->run_slots_dev, nullptr, pos0 + begin, cnt, layer_begin, layer_count, tokens_stride(p, m),
-                                       static_cast<const uint16_t *>(k) + begin * tok, static_cast<const uint16_t *>(v) + begin * tok,
-                                       *rope_table(p, theta), st));
-      p->launches += 1;
-      continue;
-    }
     for (int32_t l = 0; l < layer_count; ++l) {     // the run's layers are [layer_count, m, …]: one launch per layer and chunk
       const uint16_t *kl = static_cast<const uint16_t *>(k) + (size_t(l) * m + begin) * tok;
       const uint16_t *vl = static_cast<const uint16_t *>(v) + (size_t(l) * m + begin) * tok;

@@ -102,10 +102,13 @@ cudaError_t launch_kv4_append_run(const PoolView &pv, const int32_t *pages, int3
 cudaError_t launch_kv4_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
                                 int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st,
                                 int64_t *launches);
-// K1 of a bf16 pool with K rotated in any form; pos: device, or null for pos0, pos0 + 1, ...
-cudaError_t launch_kv_append_form(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t pos0, int32_t n_tok,
-                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
-                                  const void *v_new, const RopeForm &form, cudaStream_t st);
+// K1 of a bf16 pool with K rotated in any form: the tokens of a step (slots, pos: device), and a run on its pages
+cudaError_t launch_kv_append_form(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
+                                  int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                                  const RopeForm &form, cudaStream_t st);
+cudaError_t launch_kv_append_run_form(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                                      int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                      const void *v_new, const RopeForm &form, cudaStream_t st, int64_t *launches);
 // the step's queries rotated in any form, q -> q_out (which may be q)
 cudaError_t launch_rope_queries_form(const PoolView &pv, const int32_t *pos, int32_t n, int32_t layer_count, const void *q, void *q_out,
                                      const RopeForm &form, cudaStream_t st);

@@ -8,6 +8,7 @@
 
 #include "device_common.cuh"
 #include "kernels.hpp"
+#include "page_run.cuh"
 #include "rope_form.cuh"
 
 namespace pasta {
@@ -32,7 +33,8 @@ __device__ __forceinline__ void rotate_slot(uint4 &lo4, uint4 &hi4, const RopeFo
   const bool turns = p < f.slots, alternate = f.interleaved && turns;
   if (!turns) return;
   float y[16], lo[8], hi[8];
-  rope_slot<D>(lo4, hi4, alternate, turn, p, y);
+  if (alternate) rope_slot<D>(lo4, hi4, true, turn, p, y);          // (uniform over the rotated slots: straight code for either layout)
+  else rope_slot<D>(lo4, hi4, false, turn, p, y);
   if (chunk_not_finite(lo4) || chunk_not_finite(hi4)) {
     const uint32_t w[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
 #pragma unroll
@@ -63,10 +65,39 @@ __device__ __forceinline__ void turns_of_group(const RopeForm &f, const int32_t 
   __syncthreads();
 }
 
-// grid (groups of `per` tokens, slices of the layers).  slots: device, 2 words per token (page, row).
-template <int D>
+// The rows of a CTA's slice, (layer, token, head), in steps of all its warps' rows: a division per row would cost as much as a third of
+// its rotation.
+struct RowWalk {
+  int g, r, ll, dg, dr, dl, heads, cnt;
+  __device__ __forceinline__ RowWalk(int first, int step, int heads_, int cnt_) : heads(heads_), cnt(cnt_) {
+    g = first % heads; r = first / heads % cnt; ll = first / (heads * cnt);
+    dg = step % heads; dr = step / heads % cnt; dl = step / (heads * cnt);
+  }
+  __device__ __forceinline__ void next() {
+    g += dg; r += dr; ll += dl;
+    if (g >= heads) { g -= heads; ++r; }
+    if (r >= cnt) { r -= cnt; ++ll; }
+  }
+};
+
+// Where tokens go: slots in device memory (2 words per token: page, row), or the pages of a run.
+struct StepSlots {
+  const int32_t *slots;
+  __device__ __forceinline__ int2 at(int tok) const { return make_int2(slots[2 * tok], slots[2 * tok + 1]); }
+};
+template <int N>
+struct RunSlots {
+  PageList<N> pages;
+  int32_t first_offset;
+  __device__ __forceinline__ int2 at(int tok) const {
+    return make_int2(pages.page[(first_offset + tok) / PASTA_PAGE], (first_offset + tok) % PASTA_PAGE);
+  }
+};
+
+// grid (groups of `per` tokens, slices of the layers).  A row is asked for before the row ahead of it is rotated.
+template <int D, typename Slots>
 __global__ void __launch_bounds__(R_THREADS, 2)
-append_form_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t pos0, int32_t n_tok,
+append_form_kernel(PoolView pv, const __grid_constant__ Slots slots, const int32_t *__restrict__ pos, int32_t pos0, int32_t n_tok,
                    int32_t per, int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
                    const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm form) {
   constexpr int LPT = D / 16, ROWS = 32 / LPT;
@@ -74,32 +105,39 @@ append_form_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t
   grid_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, p = lane % LPT;
   const int first = blockIdx.x * per, cnt = min(per, n_tok - first), H = pv.n_kv_heads;
-  turns_of_group<D>(form, pos, pos0, first, cnt, turn);
   const int c_a = rope_chunk_a(form, p), c_b = rope_chunk_b(form, p);
   const int ll0 = blockIdx.y * layers_per_cta, layers = min(layers_per_cta, layer_count - ll0);
-  // rows of the slice: (layer, token, head), K and V of each
-  const int rows = layers * cnt * H;
-  for (int row = warp * ROWS + lane / LPT; row < rows; row += R_WARPS * ROWS) {
-    const int g = row % H, r = row / H % cnt, ll = ll0 + row / (H * cnt), tok = first + r;
-    const int page = slots[2 * tok], off = slots[2 * tok + 1];
-    if (page < 0 || page >= pv.n_pages || off < 0 || off >= PASTA_PAGE) {
+  RowWalk w(warp * ROWS + lane / LPT, R_WARPS * ROWS, H, cnt);
+  uint4 next[4];
+  auto load = [&]() {
+    const int64_t at = (ll0 + w.ll) * in_layer_stride + (static_cast<int64_t>(first + w.r) * H + w.g) * D;
+    const uint4 *k = reinterpret_cast<const uint4 *>(k_new + at), *v = reinterpret_cast<const uint4 *>(v_new + at);
+    next[0] = __ldg(k + c_a); next[1] = __ldg(k + c_b);
+    next[2] = __ldg(v + 2 * p); next[3] = __ldg(v + 2 * p + 1);
+  };
+  if (w.ll < layers) load();
+  turns_of_group<D>(form, pos, pos0, first, cnt, turn);
+  while (w.ll < layers) {
+    const int g = w.g, r = w.r, ll = ll0 + w.ll;
+    uint4 ka = next[0], kb = next[1];
+    const uint4 va = next[2], vb = next[3];
+    w.next();
+    if (w.ll < layers) load();
+    const int2 slot = slots.at(first + r);
+    if (slot.x < 0 || slot.x >= pv.n_pages || slot.y < 0 || slot.y >= PASTA_PAGE) {
       report(pv.status, PASTA_ERR_DEVICE_CHECK);
       continue;
     }
-    const int64_t at = ll * in_layer_stride + (static_cast<int64_t>(tok) * H + g) * D;
-    const uint4 *k = reinterpret_cast<const uint4 *>(k_new + at), *v = reinterpret_cast<const uint4 *>(v_new + at);
-    uint4 ka = __ldg(k + c_a), kb = __ldg(k + c_b);
-    const uint4 va = __ldg(v + 2 * p), vb = __ldg(v + 2 * p + 1);
     rotate_slot<D>(ka, kb, form, turn + r * (D / 2), p);
-    uint8_t *block = pv.kv_base + (layer_begin + ll) * pv.layer_stride + (static_cast<int64_t>(page) * H + g) * kv_block_bytes(D);
-    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 0, off, c_a)) = ka;
-    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 0, off, c_b)) = kb;
-    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 1, off, 2 * p)) = va;
-    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 1, off, 2 * p + 1)) = vb;
+    uint8_t *block = pv.kv_base + (layer_begin + ll) * pv.layer_stride + (static_cast<int64_t>(slot.x) * H + g) * kv_block_bytes(D);
+    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 0, slot.y, c_a)) = ka;
+    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 0, slot.y, c_b)) = kb;
+    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 1, slot.y, 2 * p)) = va;
+    *reinterpret_cast<uint4 *>(block + kv_chunk_offset(D / 64, 1, slot.y, 2 * p + 1)) = vb;
   }
 }
 
-// q, q_out [layer_count, n, n_heads, D], possibly the same array: a lane reads its slot before it writes it
+// q, q_out [layer_count, n, n_heads, D], possibly the same array: a lane reads its slot before it writes it, and no other lane does
 template <int D>
 __global__ void __launch_bounds__(R_THREADS, 2)
 queries_form_kernel(const int32_t *__restrict__ pos, int32_t n, int32_t per, int32_t n_heads, int32_t layer_count, int32_t layers_per_cta,
@@ -109,16 +147,25 @@ queries_form_kernel(const int32_t *__restrict__ pos, int32_t n, int32_t per, int
   grid_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, p = lane % LPT;
   const int first = blockIdx.x * per, cnt = min(per, n - first);
-  turns_of_group<D>(form, pos, 0, first, cnt, turn);
   const int c_a = rope_chunk_a(form, p), c_b = rope_chunk_b(form, p);
   const int ll0 = blockIdx.y * layers_per_cta, layers = min(layers_per_cta, layer_count - ll0);
-  const int rows = layers * cnt * n_heads;
-  for (int row = warp * ROWS + lane / LPT; row < rows; row += R_WARPS * ROWS) {
-    const int h = row % n_heads, r = row / n_heads % cnt, ll = ll0 + row / (n_heads * cnt);
-    const int64_t at = ((static_cast<int64_t>(ll) * n + first + r) * n_heads + h) * D;
-    const uint4 *src = reinterpret_cast<const uint4 *>(q + at);
-    uint4 *dst = reinterpret_cast<uint4 *>(q_out + at);
-    uint4 a = src[c_a], b = src[c_b];
+  RowWalk w(warp * ROWS + lane / LPT, R_WARPS * ROWS, n_heads, cnt);
+  int64_t next_at = 0;
+  uint4 next_a = make_uint4(0, 0, 0, 0), next_b = next_a;
+  auto load = [&]() {
+    next_at = ((static_cast<int64_t>(ll0 + w.ll) * n + first + w.r) * n_heads + w.g) * D;
+    const uint4 *src = reinterpret_cast<const uint4 *>(q + next_at);
+    next_a = src[c_a];
+    next_b = src[c_b];
+  };
+  if (w.ll < layers) load();
+  turns_of_group<D>(form, pos, 0, first, cnt, turn);
+  while (w.ll < layers) {
+    const int r = w.r;
+    uint4 *dst = reinterpret_cast<uint4 *>(q_out + next_at);
+    uint4 a = next_a, b = next_b;
+    w.next();
+    if (w.ll < layers) load();
     rotate_slot<D>(a, b, form, turn + r * (D / 2), p);
     dst[c_a] = a;
     dst[c_b] = b;
@@ -138,16 +185,56 @@ Split split_of(int n_tok, int layer_count) {
 
 }  // namespace
 
-cudaError_t launch_kv_append_form(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t pos0, int32_t n_tok,
-                                  int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
-                                  const void *v_new, const RopeForm &form, cudaStream_t st) {
-  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
+namespace {
+
+template <typename Slots>
+cudaError_t launch_append(const PoolView &pv, const Slots &slots, const int32_t *pos, int32_t pos0, int32_t n_tok, int32_t layer_begin,
+                          int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new, const RopeForm &form,
+                          cudaStream_t st) {
   const Split s = split_of(n_tok, layer_count);
   const dim3 grid((n_tok + s.per - 1) / s.per, (layer_count + s.layers - 1) / s.layers);
-  const auto kernel = pv.head_dim == 128 ? append_form_kernel<128> : append_form_kernel<64>;
+  const auto kernel = pv.head_dim == 128 ? append_form_kernel<128, Slots> : append_form_kernel<64, Slots>;
   kernel<<<grid, R_THREADS, 0, st>>>(pv, slots, pos, pos0, n_tok, s.per, layer_begin, layer_count, s.layers, in_layer_stride,
                                      static_cast<const __nv_bfloat16 *>(k_new), static_cast<const __nv_bfloat16 *>(v_new), form);
   return cudaGetLastError();
+}
+
+template <int N>
+cudaError_t launch_append_run(const PoolView &pv, const int32_t *pages, int32_t n, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                              int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                              const RopeForm &form, cudaStream_t st) {
+  return launch_append(pv, RunSlots<N>{list_of<N>(pages, n), first_offset}, nullptr, pos0, n_tok, layer_begin, layer_count, in_layer_stride,
+                       k_new, v_new, form, st);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append_form(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t n_tok, int32_t layer_begin,
+                                  int32_t layer_count, int64_t in_layer_stride, const void *k_new, const void *v_new,
+                                  const RopeForm &form, cudaStream_t st) {
+  if (n_tok == 0 || layer_count == 0) return cudaSuccess;
+  return launch_append(pv, StepSlots{slots}, pos, 0, n_tok, layer_begin, layer_count, in_layer_stride, k_new, v_new, form, st);
+}
+
+cudaError_t launch_kv_append_run_form(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t pos0, int32_t n_tok,
+                                      int32_t layer_begin, int32_t layer_count, int64_t in_layer_stride, const void *k_new,
+                                      const void *v_new, const RopeForm &form, cudaStream_t st, int64_t *launches) {
+  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(k_new), *v = static_cast<const __nv_bfloat16 *>(v_new);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * pv.head_dim;
+  if (layer_count == 0) return cudaSuccess;
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const auto launch = n <= kPagesSmall ? launch_append_run<kPagesSmall> : launch_append_run<kPagesLarge>;
+    const cudaError_t e = launch(pv, pages, n, first_offset, pos0 + done, cnt, layer_begin, layer_count, in_layer_stride, k + done * tok,
+                                 v + done * tok, form, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
 }
 
 cudaError_t launch_rope_queries_form(const PoolView &pv, const int32_t *pos, int32_t n, int32_t layer_count, const void *q, void *q_out,
