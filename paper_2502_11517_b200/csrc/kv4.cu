@@ -70,10 +70,10 @@ __device__ __forceinline__ float group_scale(float amax) {
 __device__ __forceinline__ uint32_t scale_bits(float s) { return __float_as_uint(16.f * s) >> 16; }      // t, a bf16 number
 
 constexpr float kWhole = 12582912.f;              // 1.5 * 2^23: a sum with it is a whole number
+constexpr float kFine = 1536.f;                   // 1.5 * 2^10: a sum with it is a multiple of 2^-13
 // whole numbers of scales nearest to two bf16 numbers, as fp32 (|x| <= 7 s); r = 1 / s
 __device__ __forceinline__ float_pair codes_of_bf16(float_pair x, float_pair r) {
-  // 1536 = 1.5 * 2^10: the sum is a multiple of 2^-13
-  return add_pair(add_pair(fma_pair(x, r, same(1536.f)), same(kWhole - 1536.f)), same(-kWhole));
+  return add_pair(add_pair(fma_pair(x, r, same(kFine)), same(kWhole - kFine)), same(-kWhole));
 }
 // the same of any fp32 number
 __device__ __forceinline__ float code_of_fp32(float x, float s, float r) {
@@ -96,28 +96,30 @@ __device__ __forceinline__ uint32_t code_word(float lo, float hi) {
 }
 
 // 16 elements of a K row (16-element chunk c of token row r), as fp32 numbers of a bf16 row or of a rotated one; two lanes
-// share a group.  amax: the largest magnitude of the 16.
+// share a group.  amax: the largest magnitude of the 16; turned: they were rotated.  Whole warps.
 template <int D, bool kRotated>
-__device__ __forceinline__ void store_k16(uint8_t *block, int r, int c, bool valid, float *x, float amax) {
+__device__ __forceinline__ void store_k16(uint8_t *block, int r, int c, bool valid, bool turned, float *x, float amax) {
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
   const float s = group_scale(amax), inv = reciprocal(s);
-  if (s >= kScaleMax) {
+  if (__any_sync(0xffffffffu, s >= kScaleMax)) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = fminf(fmaxf(x[e], -7.f * s), 7.f * s);
   }
   float_pair n[8];
   if constexpr (kRotated) {
-    // The quotient is good to 2^-19, so the code is the nearest one unless the quotient is that close to the middle of two.
+    // Rotated elements: the quotient is good to 2^-19, so the code is the nearest one unless the quotient is that close to the middle
+    // of two.  The others are bf16 numbers.
+    const float grid = turned ? 0.f : kFine;
     float far = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float_pair quot = fma_pair(pair_of(x[2 * i], x[2 * i + 1]), same(inv), same(0.f));
-      n[i] = add_pair(add_pair(quot, same(kWhole)), same(-kWhole));
+      const float_pair quot = fma_pair(pair_of(x[2 * i], x[2 * i + 1]), same(inv), same(grid));
+      n[i] = add_pair(add_pair(quot, same(kWhole - grid)), same(-kWhole));
       float d0, d1;
       both(fma_pair(n[i], same(-1.f), quot), d0, d1);
       far = max3(far, fabsf(d0), fabsf(d1));
     }
-    if (far > 0.5f - 0x1p-18f) {
+    if (turned && far > 0.5f - 0x1p-18f) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) n[i] = pair_of(code_of_fp32(x[2 * i], s, inv), code_of_fp32(x[2 * i + 1], s, inv));
     }
@@ -217,7 +219,7 @@ __device__ __forceinline__ bool append_k(uint8_t *block, const __nv_bfloat16 *ro
 #pragma unroll
       for (int e = 0; e < 16; e += 2) amax = max3(amax, fabsf(x[e]), fabsf(x[e + 1]));
     }
-    store_k16<D, kRope>(block, off0 + r, c, valid, x, amax);
+    store_k16<D, kRope>(block, off0 + r, c, valid, kRope && c < form.slots, x, amax);
   }
   return bad;
 }
@@ -286,10 +288,12 @@ __device__ __forceinline__ bool append_v(uint8_t *block, const __nv_bfloat16 *ro
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float r = __shfl_sync(0xffffffffu, inv, (lane & ~7) | i);
+      float most = 0.f;
+      if (clamp) most = 7.f * __shfl_sync(0xffffffffu, s, (lane & ~7) | i);
 #pragma unroll
       for (int w = 0; w < CH / 2; ++w) {
         float v0 = bf16_lo(x[i][w]), v1 = bf16_hi(x[i][w]);
-        if (clamp) { v0 = fminf(fmaxf(v0, -7.f / r), 7.f / r); v1 = fminf(fmaxf(v1, -7.f / r), 7.f / r); }
+        if (clamp) { v0 = fminf(fmaxf(v0, -most), most); v1 = fminf(fmaxf(v1, -most), most); }
         n[w][i] = codes_of_bf16(pair_of(v0, v1), same(r));
       }
     }
@@ -348,7 +352,7 @@ __device__ __forceinline__ void append_page4(const PoolView &pv, int page, int o
 // Tokens of a step: slots[2 i], slots[2 i + 1] are token i's page and row.  One CTA per group of tokens that are neighbours in
 // one page (the CTA of a group's first token takes it) and slice of the layers.
 template <int D, bool kRope>
-__global__ void __launch_bounds__(A_THREADS, 2)
+__global__ void __launch_bounds__(A_THREADS, 3)
 kv4_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t *__restrict__ pos, int32_t n_tok,
                   int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
                   const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm form) {
@@ -377,7 +381,7 @@ kv4_append_kernel(PoolView pv, const int32_t *__restrict__ slots, const int32_t 
 // A run: n_tok tokens of one stream at consecutive positions, the first at row first_offset of the first page.  One CTA per
 // page and slice of the layers.
 template <int D, bool kRope, int N>
-__global__ void __launch_bounds__(A_THREADS, 2)
+__global__ void __launch_bounds__(A_THREADS, 3)
 kv4_append_run_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t pos0, int32_t n_tok, int32_t first_offset,
                       int32_t layer_begin, int32_t layer_count, int32_t layers_per_cta, int64_t in_layer_stride,
                       const __nv_bfloat16 *__restrict__ k_new, const __nv_bfloat16 *__restrict__ v_new, const __grid_constant__ RopeForm form) {
