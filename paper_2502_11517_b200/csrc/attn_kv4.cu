@@ -249,7 +249,9 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   // test hook: held MMAs, so that what waits for them runs into its limit
   const bool no_mma = pv.debug_hold & 2;
   uint32_t it = 0, copied = 0;                        // tiles worked on (MMA phases follow it); tiles of the unit that were copied
-  int ll = -1, u = 0, u1 = 0, layer = 0, asked = 0;
+  // (where nothing is assigned in advance, the first units go to the CTAs in order and the counter counts those behind them)
+  const bool none_assigned = a.n_tunits == 0;
+  int ll = none_assigned ? a.layer_count : -1, u = 0, u1 = 0, layer = 0, asked = 0;
   UnitInfo x;
   // The units assigned to the CTA in the next layer that has some.  A layer's ranges are taken by other CTAs than the layer's before:
   // what makes a range slow (masks, unit ends) is the same in every layer.
@@ -262,8 +264,6 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   };
   next_range();
 
-  // (where nothing is assigned in advance, the first units go to the CTAs in order and the counter counts those behind them)
-  const bool none_assigned = a.n_tunits == 0;
   const int counted_from = none_assigned ? gridDim.x : 0, n_shared = a.n_dunits * a.layer_count;
   // The first thread takes numbers until one is past the last unit.  Every CTA ends with one such number, and the CTA that has the last
   // of them sets the counter back.
