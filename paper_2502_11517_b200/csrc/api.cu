@@ -804,29 +804,9 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
   if (m == 0 || layer_count == 0) return PASTA_OK;
   if (!k_out || !v_out || misaligned(p, k_out, v_out)) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const size_t tok = size_t(p->cfg.n_kv_heads) * p->cfg.head_dim;
-  if (p->pv.kv8 || p->pv.kv4) {
-    const auto launch = p->pv.kv8 ? launch_kv8_read_run : launch_kv4_read_run;
-    PASTA_CUDA(launch(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count, tokens_stride(p, m),
-                      k_out, v_out, st, &p->launches));
-    return PASTA_OK;
-  }
-  std::vector<int32_t> words;
-  for (int32_t begin = 0; begin < m; begin += kRunChunk) {
-    const int32_t cnt = std::min(kRunChunk, m - begin);
-    words.resize(size_t(cnt) * 2);
-    for (int32_t i = 0; i < cnt; ++i) {
-      const int32_t t = start + begin + i;
-      words[2 * i] = sm.pages[t / PASTA_PAGE];
-      words[2 * i + 1] = t % PASTA_PAGE;
-    }
-    pasta_status_t s = upload(p, words.data(), words.size(), p->run_slots_dev, st);
-    if (s != PASTA_OK) return s;
-    for (int32_t l = 0; l < layer_count; ++l)
-      PASTA_CUDA(launch_kv_read(p->pv, p->run_slots_dev, cnt, layer_begin + l, static_cast<uint16_t *>(k_out) + (size_t(l) * m + begin) * tok,
-                                static_cast<uint16_t *>(v_out) + (size_t(l) * m + begin) * tok, st));
-    p->launches += layer_count;
-  }
+  const auto launch = p->pv.kv8 ? launch_kv8_read_run : p->pv.kv4 ? launch_kv4_read_run : launch_kv_read_run;
+  PASTA_CUDA(launch(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count, tokens_stride(p, m),
+                    k_out, v_out, st, &p->launches));
   return PASTA_OK;
 }
 

@@ -3,6 +3,7 @@
 #include <cuda_fp16.h>
 #include "device_common.cuh"
 #include "kernels.hpp"
+#include "page_run.cuh"
 
 #include <cmath>
 
@@ -45,8 +46,10 @@ __global__ void kv_append_kernel(PoolView pv, const int32_t *__restrict__ slots,
   *reinterpret_cast<uint4 *>(block + kv_chunk_offset(pv.head_dim >> 6, kv, off, c)) = __ldg(src);
 }
 
-__global__ void kv_read_kernel(PoolView pv, const int32_t *__restrict__ slots, int32_t n_tok, int32_t layer,
-                               uint4 *__restrict__ k_out, uint4 *__restrict__ v_out) {
+// A run read back: a thread per 16 bytes of blockIdx.y's layer.  Its pages are kernel arguments, so nothing is uploaded first.
+template <int N>
+__global__ void kv_read_kernel(PoolView pv, const __grid_constant__ PageList<N> pages, int32_t n_tok, int32_t first_offset, int32_t layer_begin,
+                               int64_t out_layer_stride, uint4 *__restrict__ k_out, uint4 *__restrict__ v_out) {
   const int chunks = pv.head_dim >> 3;
   const int64_t total = static_cast<int64_t>(n_tok) * pv.n_kv_heads * 2 * chunks;
   const int64_t idx = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
@@ -57,14 +60,14 @@ __global__ void kv_read_kernel(PoolView pv, const int32_t *__restrict__ slots, i
   rest >>= 1;
   const int g = static_cast<int>(rest % pv.n_kv_heads);
   const int a = static_cast<int>(rest / pv.n_kv_heads);
-  const int page = slots[2 * a], off = slots[2 * a + 1];
-  if (page < 0 || page >= pv.n_pages || off < 0 || off >= PASTA_PAGE) {
+  const int page = pages.page[(first_offset + a) / PASTA_PAGE], off = (first_offset + a) % PASTA_PAGE;
+  if (page < 0 || page >= pv.n_pages) {
     report(pv.status, PASTA_ERR_DEVICE_CHECK);
     return;
   }
-  const uint8_t *block = pv.kv_base + layer * pv.layer_stride +
+  const uint8_t *block = pv.kv_base + (layer_begin + static_cast<int64_t>(blockIdx.y)) * pv.layer_stride +
                          (static_cast<int64_t>(page) * pv.n_kv_heads + g) * kv_block_bytes(pv.head_dim);
-  uint4 *dst = (kv ? v_out : k_out) + (static_cast<int64_t>(a) * pv.n_kv_heads + g) * chunks + c;
+  uint4 *dst = (kv ? v_out : k_out) + blockIdx.y * out_layer_stride + (static_cast<int64_t>(a) * pv.n_kv_heads + g) * chunks + c;
   *dst = *reinterpret_cast<const uint4 *>(block + kv_chunk_offset(pv.head_dim >> 6, kv, off, c));
 }
 
@@ -314,15 +317,32 @@ cudaError_t launch_kv_append(const PoolView &pv, const int32_t *slots, int32_t n
   return cudaGetLastError();
 }
 
-cudaError_t launch_kv_read(const PoolView &pv, const int32_t *slots, int32_t n_tok, int32_t layer,
-                           void *k_out, void *v_out, cudaStream_t st) {
+template <int N>
+static cudaError_t launch_read_pages(const PoolView &pv, const int32_t *pages, int n_pages, int32_t n_tok, int32_t first_offset,
+                                     int32_t layer_begin, int32_t layer_count, int64_t out_layer_stride, uint4 *k, uint4 *v, cudaStream_t st) {
   const int64_t total = static_cast<int64_t>(n_tok) * pv.n_kv_heads * 2 * (pv.head_dim >> 3);
-  if (total == 0) return cudaSuccess;
   const int threads = 256;
-  const int64_t blocks = (total + threads - 1) / threads;
-  kv_read_kernel<<<static_cast<unsigned>(blocks), threads, 0, st>>>(
-      pv, slots, n_tok, layer, static_cast<uint4 *>(k_out), static_cast<uint4 *>(v_out));
+  const dim3 grid(static_cast<unsigned>((total + threads - 1) / threads), layer_count);
+  kv_read_kernel<N><<<grid, threads, 0, st>>>(pv, list_of<N>(pages, n_pages), n_tok, first_offset, layer_begin, out_layer_stride, k, v);
   return cudaGetLastError();
+}
+
+cudaError_t launch_kv_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
+                               int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st, int64_t *launches) {
+  uint4 *k = static_cast<uint4 *>(k_out), *v = static_cast<uint4 *>(v_out);
+  const int64_t tok = static_cast<int64_t>(pv.n_kv_heads) * (pv.head_dim >> 3);      // 16-byte chunks of a token
+  for (int32_t done = 0; done < n_tok;) {
+    const int32_t left = n_tok - done, all = (first_offset + left + PASTA_PAGE - 1) / PASTA_PAGE;
+    const int32_t n = std::min(all, kPagesLarge), cnt = std::min(left, n * PASTA_PAGE - first_offset);
+    const auto launch = n <= kPagesSmall ? launch_read_pages<kPagesSmall> : launch_read_pages<kPagesLarge>;
+    const cudaError_t e = launch(pv, pages, n, cnt, first_offset, layer_begin, layer_count, out_layer_stride >> 3, k + done * tok, v + done * tok, st);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    pages += n;
+    done += cnt;
+    first_offset = 0;
+  }
+  return cudaSuccess;
 }
 
 // =============================================================================================

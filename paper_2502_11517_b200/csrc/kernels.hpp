@@ -48,9 +48,9 @@ cudaError_t launch_overlapped(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
 // K1: copies the new tokens of `layer_count` layers into their slots.  slots: device, 2 words per token.
 cudaError_t launch_kv_append(const PoolView &pv, const int32_t *slots, int32_t n_tok, int32_t layer_begin,
                              int32_t layer_count, const void *k_new, const void *v_new, cudaStream_t st);
-// inverse of K1 for one layer: gathers the listed slots into dense [n_tok, Hkv, D] arrays
-cudaError_t launch_kv_read(const PoolView &pv, const int32_t *slots, int32_t n_tok, int32_t layer,
-                           void *k_out, void *v_out, cudaStream_t st);
+// inverse of K1: a run of a bf16 pool into dense [layer_count, n_tok, Hkv, D] arrays (out_layer_stride: elements between layers)
+cudaError_t launch_kv_read_run(const PoolView &pv, const int32_t *pages, int32_t first_offset, int32_t n_tok, int32_t layer_begin,
+                               int32_t layer_count, int64_t out_layer_stride, void *k_out, void *v_out, cudaStream_t st, int64_t *launches);
 // K1 with rotary embedding of K by position id (pos: device array, or NULL for consecutive ids pos0, pos0 + 1, ...)
 cudaError_t launch_kv_append_rope(const PoolView &pv, const int32_t *slots, const int32_t *pos, int32_t pos0, int32_t n_tok,
                                   int32_t layer_begin, int32_t layer_count, const void *k_new, const void *v_new,

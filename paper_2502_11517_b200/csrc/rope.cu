@@ -177,7 +177,7 @@ queries_form_kernel(const int32_t *__restrict__ pos, int32_t n, int32_t per, int
 struct Split { int per, layers; };
 Split split_of(int n_tok, int layer_count) {
   const int want = 148 * 2;
-  const int per = std::min(PASTA_PAGE, std::max(1, n_tok / want));
+  const int per = std::min(PASTA_PAGE, (n_tok + want - 1) / want);
   const int groups = (n_tok + per - 1) / per;
   const int slices = std::min(layer_count, std::max(1, (want + groups - 1) / groups));
   return {per, (layer_count + slices - 1) / slices};

@@ -261,7 +261,7 @@ __device__ __forceinline__ UnitInfo load_unit(const int32_t *plan, int off_tunit
 
 struct TensorArgs {
   int32_t off_tunit, off_treq, off_tcta, off_pages, off_pmeta, off_vis, off_tq;
-  int32_t n_tunits;                 // (4-bit pools) units assigned to CTAs in advance, per layer
+  int32_t n_tunits = 0;             // (4-bit pools) units assigned to CTAs in advance, per layer
   int32_t off_dunit, n_dunits;      // units no CTA owns in advance (per layer): taken from a counter at run time
   int32_t n_queries, layer_begin, layer_count;
   float scale_log2;
