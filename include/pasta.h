@@ -93,8 +93,8 @@ enum {
  * is appended again.  With the rotary appends K is rotated in 64 bits, rounded to fp32 and then quantised.
  * An element that is not finite is stored as zero (with a rotary append both elements of a rotated pair), and pasta_pool_status reports
  * PASTA_ERR_DEVICE_CHECK: everything in a 4-bit pool is finite.
- * A query row with an element that is not finite, or whose scores leave the range of fp32, comes out as NaN, its lse not finite,
- * capped or not; other rows are untouched.
+ * A query row with an element that is not finite, or with a score above the range of fp32, comes out as NaN, its lse not finite,
+ * capped or not; other rows are untouched.  A score below that range weighs nothing.
  * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
  * out have to be 16-byte aligned, else INVALID_ARG).  pasta_kv_bytes is n_layers * n_pages * n_kv_heads * 18 * head_dim.
  * Requests of up to 128 stacked rows (threads x group) and 4095 streams run on tensor cores, with either head_dim: queries,
@@ -473,7 +473,8 @@ pasta_status_t pasta_debug_set_wait_limit(pasta_pool_t *pool, int64_t cycles);
  * the launches that follow, the roles that wait for them give up after the pool's wait limit, every CTA drains what
  * it has in flight, frees its tensor memory and returns, and the status word holds PASTA_ERR_TIMEOUT.  The outputs
  * of such a launch are undefined.  In the kernel of 8-bit pools with head_dim 64, 1 holds the copies back and 2 the warps that
- * make none.  Set a short limit first (pasta_debug_set_wait_limit); 0 switches the hook off.
+ * make none; in that of 4-bit pools 2 holds the matrix products back and the other bits nothing.  Set a short limit first
+ * (pasta_debug_set_wait_limit); 0 switches the hook off.
  */
 pasta_status_t pasta_debug_hold_roles(pasta_pool_t *pool, int32_t role_mask);
 /*
@@ -482,7 +483,9 @@ pasta_status_t pasta_debug_hold_roles(pasta_pool_t *pool, int32_t role_mask);
  * one is kept back, `percent` of their tiles in all (0 to 50; 10 by default), in units of at most `tiles` tiles (2 to
  * 1024; 16 by default).  The CTAs take these from a shared counter once their own work is done: SMs that stream faster
  * than others then do more of it.  0 percent assigns everything in advance.  Takes effect from the next
- * pasta_step_begin, and only for steps large enough for it to matter (16 tiles per CTA).
+ * pasta_step_begin, and only for steps large enough for it to matter (16 tiles per CTA).  On a 4-bit pool every run that is not
+ * much longer than an even share is handed out at run time, whole; 0 percent assigns everything in advance there too, and
+ * `tiles` says nothing.
  */
 pasta_status_t pasta_debug_set_tail(pasta_pool_t *pool, int32_t percent, int32_t tiles);
 /*

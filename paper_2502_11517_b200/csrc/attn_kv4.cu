@@ -18,18 +18,25 @@
 // at a time in turn).  The two diagonal blocks are what is wanted and are added up at a unit's end; the other two cost nothing
 // that matters at these N.
 //
-// What bounds it: instructions (some 250 per warp and tile of 128 tokens for K's codes, 330 for V's, 35 for every 8 rows of the
-// softmax, on each of the four schedulers) against the 785 cycles that the tile's 18 KB take at the measured copy bandwidth.  A warp
-// alone issues one every four or five cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so several CTAs share an SM and
-// fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows,
-// two of 256 threads and 256 columns for up to 80 (64 at head_dim 64), one above.
-// Every warp does everything in turn.  (Measured, with the roles on warps of their own and one CTA to an SM, in three forms:
-// 290 to 390 us for the batched case and 310 to 410 for the long prefix; hand-overs and the four programs' instruction fetches took
-// more than the work.)
+// What bounds it: instructions and their latency.  A tile of 128 tokens and 68 rows takes 7100 warp instructions (a quarter to each
+// scheduler: some 1800, of which K's codes, V's codes and the softmax are 1000), against the 785 cycles that its 18 KB take at the
+// measured copy bandwidth.  A warp alone issues one every seven cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so
+// CTAs share an SM and fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows, two of 256 threads and
+// 256 columns for up to 80 (64 at head_dim 64), one above: TMEM decides.  Schedulers issue in 53 % of the cycles; a tile takes 2500
+// (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 152 us (39 us for the bytes alone), 8 prefixes of
+// 32768 tokens and 68 rows 236 us (52), 64 capped short responses 157 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
+// Built and measured slower: roles on warps of their own and one CTA to an SM, in three forms (290 to 390 us for the first, 310 to 410
+// for the second: hand-overs and four programs' instruction fetches); twice the threads per CTA at 64 registers (302 and 418); bulk
+// copies in place of 16-byte ones (192 and 277 for 191 and 274 then); one body for the chunks of the softmax instead of one for
+// every number of them (154 and 243 for 152 and 236).
 //
-// A CTA walks its units as those of attn_tensor.cu do.  TMEM holds one operand (K, then V in its place), the scores and O^T.
-// The reference of a row is shared by the CTA's warps and raised only when a score exceeds it by more than 2^R_SLACK: the CTA
-// votes on that with the barrier that publishes the weights, and only then the rows' maxima are worked out and O and l brought to them.
+// A CTA walks units as those of attn_tensor.cu do, but most are handed out at run time, whole runs, the longest first.  TMEM holds one
+// operand (K, then V in its place), the scores and O^T.  Every warp does everything in turn.
+// References: a weight is 2^(score - ref), and any ref that keeps weights inside the range of fp32 and bf16 (which share their exponents)
+// gives the same relative precision.  So a row's ref starts at 0 and nobody looks for maxima.  When a score exceeds its row's ref by
+// more than 2^R_SLACK (the CTA votes on that with the barrier that publishes the weights), the rows' maxima over the tile are worked out, and
+// O and l brought to them.  A row that saw tokens but whose sum came out below 2^-60 has scores far below 0: its unit is done again,
+// with first references from the maxima of the first tokens each row sees.
 // The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.
 // Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
 #include <algorithm>
@@ -266,7 +273,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
 
   const int counted_from = none_assigned ? gridDim.x : 0, n_shared = a.n_dunits * a.layer_count;
   // The first thread takes numbers until one is past the last unit.  Every CTA ends with one such number, and the CTA that has the last
-  // of them sets the counter back.
+  // of them sets the counter back.  Nobody counts where the first units are all there are.
+  const bool counted = a.n_dunits != 0 && n_shared > counted_from;
   auto take = [&]() {
     const int number = counted_from + atomicAdd(counter, 1);
     if (number == n_shared + static_cast<int>(gridDim.x) - 1) *counter = 0;
@@ -280,7 +288,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       ++u;
       next_range();
     } else {
-      if (a.n_dunits == 0 || taken >= n_shared) return false;
+      if (taken >= n_shared) return false;
       id = taken / a.layer_count;
       layer = taken - id * a.layer_count;
       off = a.off_dunit;
@@ -340,7 +348,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     ask(asked < nt);
   };
 
-  if (u == u1 && !none_assigned && a.n_dunits != 0) {
+  if (u == u1 && !none_assigned && counted) {
     if (tid == 0) take();
     __syncthreads();
   }
@@ -493,6 +501,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       } else {
         saw_all = true;
       }
+      // (a unit's last tile: the unit behind it, if it is one of those handed out at run time, while the scores are worked out)
+      if (k + 1 == nt && tid == 0 && counted && u == u1 && !careful) take();
       cta_wait(bar + 8 * L::B_QK, it & 1, abort_flag, limit);
       tc_fence_after();
       // ---- V's codes to the A operand, in K's place, a thread per channel (half the pages)
@@ -732,8 +742,6 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
         for (int j = 0; j < 4; ++j) add_bf16x2(l[i][2 * j], l[i][2 * j + 1], o[j]);
       }
       if (k + 1 < nt) look((k + 1) % L::STAGES);
-      // (a unit's last tile: the unit behind it, if it is one of those handed out at run time)
-      if (k + 1 == nt && tid == 0 && a.n_dunits != 0 && u == u1 && !careful) take();
     }
     if (saw_all && half == 0 && lane < 8) saw_s[8 * wq + lane] = 0xffffu;
     if (__syncthreads_or(*abort_flag != 0)) break;
@@ -771,7 +779,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     if (again && __syncthreads_or(*abort_flag != 0)) break;
     tc_fence_after();
     // ---- the copies of the unit behind it, under way while this one's rows are written
-    const int taken = unit_s[0];
+    const int taken = counted ? unit_s[0] : n_shared;
     if (again) careful = true;
     else {
       careful = false;
@@ -834,7 +842,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
     }
     if (tid == 0) {
-      while (a.n_dunits != 0 && unit_s[0] < n_shared) take();
+      while (counted && unit_s[0] < n_shared) take();
       report(pv.status, PASTA_ERR_TIMEOUT);
     }
     tc_fence_before();

@@ -435,7 +435,8 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     n_wunits = 0;
     for (int32_t i = 0; i < n; ++i) n_wunits += static_cast<int64_t>(q_nw[i]) * lim.n_kv_heads;
     if (t_rows + n_wunits * G <= lim.max_rows) break;
-    if (!dunits.empty()) return without_tail(pool, entries, slots, lim, out);    // the shared tail costs rows: do without
+    // the shared tail costs rows: do without (whole runs, as 4-bit pools hand out, cost none)
+    if (!dunits.empty() && !lim.kv4) return without_tail(pool, entries, slots, lim, out);
     if (chunk >= (1 << 24)) return PASTA_ERR_CAPACITY;
     chunk *= 2;
   }

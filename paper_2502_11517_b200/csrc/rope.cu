@@ -3,7 +3,10 @@
 // A CTA takes a group of neighbouring tokens and a slice of the layers: it works out the tokens' sines and cosines (64 bits)
 // once, into shared memory, and applies them to every head and layer of the slice.  A warp rotates 32 / (head_dim / 16) rows at
 // a time, a lane one slot of 16 elements: two 16-byte loads, eight rotations, two 16-byte stores.
-// What bounds it: memory for long prompts (2 bytes in, 2 out per element), the chain sine -> rotation -> store for a step.
+// What bounds it: for long prompts the instructions around the 64-bit rotation (a quarter of them are; conversions and exponents' bits
+// the rest) and the latency of 16 warps per SM (three CTAs in 80 registers spill: 44 to 62 us for the queries), 50 to 60 % of what
+// the bytes take; for a step the chain sine -> rotation -> store.  16384 tokens of a bf16 pool 30 us (26 for the bytes at the copy rate),
+// 1024 query tokens of 8 layers and 32 heads 35 us (20).
 #include <algorithm>
 
 #include "device_common.cuh"
