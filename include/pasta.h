@@ -97,7 +97,7 @@ enum {
  * capped or not; other rows are untouched.  A score below that range weighs nothing.
  * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
  * out have to be 16-byte aligned, else INVALID_ARG).  pasta_kv_bytes is n_layers * n_pages * n_kv_heads * 18 * head_dim.
- * Requests of up to 128 stacked rows (threads x group) and 4095 streams run on tensor cores, with either head_dim: queries,
+ * Requests of up to 640 stacked rows (queries of the step x group; 512 with head_dim 64) and 4095 streams run on tensor cores: queries,
  * and K and V as held, enter unrounded, a softmax weight as bf16 (2^-8 of itself; the weights' sum is that of the rounded ones), sums
  * are fp32.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the warp-shuffle kernel, which rounds no weight.
  */

@@ -46,9 +46,13 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
   const int slots = (c.flags & PASTA_FLAG_KV_INT4) ? 4 * grid : (c.flags & PASTA_FLAG_KV_FP8) && c.head_dim == 64 ? 6 * grid : grid;
   d->max_queries = c.max_step_queries ? c.max_step_queries
                                       : static_cast<int32_t>(std::min<int64_t>(int64_t(c.max_requests) * 17, 1 << 20));
+  // t-requests, and how often a page can be listed by them
+  const bool int4 = (c.flags & PASTA_FLAG_KV_INT4) != 0;
+  const int64_t parts = int4 ? std::min<int64_t>(kKv4MaxParts, (int64_t(d->max_queries) * d->group + kv4_max_rows(c.head_dim) - 1) / kv4_max_rows(c.head_dim) + 1) : 1;
+  const int64_t n_treq = int4 ? std::min<int64_t>(c.max_requests * parts, std::max(d->max_queries, c.max_requests)) : c.max_requests;
   // units of the shared tail, at most: its share of all tiles in pieces of kTailTiles, plus one ragged piece per run
   const int64_t tail_units = int64_t(c.n_pages) * c.n_kv_heads / PASTA_TILE_PAGES * kTailPercent / 100 / kTailTiles +
-                             int64_t(c.max_requests) * c.n_kv_heads;
+                             n_treq * c.n_kv_heads;
   const int64_t unit_rows = std::min<int64_t>(PASTA_MAX_ROWS, int64_t(c.max_threads_per_request) * d->group);
   d->max_rows = c.max_partial_rows ? c.max_partial_rows
                                    : static_cast<int32_t>(std::min<int64_t>(
@@ -56,11 +60,11 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                                              tail_units * unit_rows, 1 << 28));
   d->layers_per_launch = c.max_layers_per_launch ? std::min(c.max_layers_per_launch, c.n_layers)
                                                  : std::min(c.n_layers, 8);
-  const int64_t nq = d->max_queries, nr = c.max_requests;
-  d->max_words = PH_WORDS + 2 * nq + PQ_WORDS * nq + PT_WORDS * nr + 2 * nr * c.n_kv_heads +
-                 PU_WORDS * (nr * c.n_kv_heads + slots) + 2 * slots + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
-                 2 * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
-                 PU_WORDS * tail_units + 2 * nr * c.n_kv_heads + 8;
+  const int64_t nq = d->max_queries;
+  d->max_words = PH_WORDS + 2 * nq + PQ_WORDS * nq + PT_WORDS * n_treq + 2 * n_treq * c.n_kv_heads +
+                 PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
+                 2 * parts * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
+                 PU_WORDS * tail_units + 2 * n_treq * c.n_kv_heads + 8;
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
   const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0, kv4 = (c.flags & PASTA_FLAG_KV_INT4) != 0;
   if (kv8 && kv4) return PASTA_ERR_INVALID_ARG;

@@ -22,7 +22,7 @@
 // scheduler: some 1800, of which K's codes, V's codes and the softmax are 1000), against the 785 cycles that its 18 KB take at the
 // measured copy bandwidth.  A warp alone issues one every seven cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so
 // CTAs share an SM and fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows, two of 256 threads and
-// 256 columns for up to 80 (64 at head_dim 64), one above: TMEM decides.  Schedulers issue in 53 % of the cycles; a tile takes 2500
+// 256 columns for up to 80 (64 at head_dim 64); requests with more rows are split by the planner.  Schedulers issue in 53 % of the cycles; a tile takes 2500
 // (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 152 us (39 us for the bytes alone), 8 prefixes of
 // 32768 tokens and 68 rows 236 us (52), 64 capped short responses 157 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
 // Built and measured slower: roles on warps of their own and one CTA to an SM, in three forms (290 to 390 us for the first, 310 to 410
@@ -56,15 +56,16 @@ constexpr float R_FAINT = 8.7e-19f;              // 2^-60: sums below it may hav
 template <int D, int NMAX>
 struct U {
   static constexpr int H = NMAX <= 32 ? 1 : 2, THREADS = 128 * H;      // threads that share a token
-  static constexpr int CHUNKS = (NMAX / 8 + H - 1) / H;           // groups of 8 rows per thread, at most: chunk H i + part for its part
+  static constexpr int CHUNKS = NMAX / 8 / H;                     // groups of 8 rows per thread, at most: chunk H i + part for its part
+  static_assert(NMAX % (8 * H) == 0 && CHUNKS <= 5, "numbers of chunks");
   static constexpr int OW = D == 128 ? 1 : 2;                     // blocks of N columns of an accumulator
   static constexpr int KSTEPS = D / 16, VSTEPS = D == 128 ? 8 : 4;
   static constexpr uint32_t COL_A = 0, COL_S = D / 2, COL_O = COL_S + NMAX;      // (V's operand is D / 2 columns wide, too)
-  static constexpr uint32_t COLS_USED = COL_O + OW * NMAX, COLS = COLS_USED <= 128 ? 128 : COLS_USED <= 256 ? 256 : 512;
-  static_assert(COLS_USED <= 512, "tensor memory budget");
+  static constexpr uint32_t COLS_USED = COL_O + OW * NMAX, COLS = COLS_USED <= 128 ? 128 : 256;
+  static_assert(COLS_USED <= 256, "tensor memory budget");
   static constexpr int RESIDENT = 512 / COLS;                     // CTAs on an SM
   static constexpr int BLOCK = kv4_block_bytes(D), STAGE_BYTES = PASTA_TILE_PAGES * BLOCK;
-  static constexpr int STAGES = D == 128 && NMAX <= 32 ? 2 : RESIDENT > 1 ? 3 : 6;
+  static constexpr int STAGES = D == 128 && NMAX <= 32 ? 2 : 3;
   // a row of weights: 128 bytes per 64 columns, or 64 bytes where they are at most 32 (so that four CTAs fit)
   static constexpr bool NARROW = OW * NMAX <= 32;
   static constexpr int ATOMS = (OW * NMAX + 63) / 64, P_GROUP = NARROW ? 512 : ATOMS * 1024;      // bytes of 8 rows
@@ -610,8 +611,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       const int my_chunks = ((n >> 3) - half + H - 1) / H;
       auto by_chunks = [&](auto f) {                // f for the number of chunks of this thread
 #define PASTA_C(cc) \
-  if constexpr (L::CHUNKS >= cc) { if (my_chunks == cc) return f(std::integral_constant<int, cc>()); }
-        PASTA_C(1) PASTA_C(2) PASTA_C(3) PASTA_C(4) PASTA_C(5) PASTA_C(6) PASTA_C(7) PASTA_C(8)
+  if constexpr (L::CHUNKS >= cc && cc * H % 2 == 0) { if (my_chunks == cc) return f(std::integral_constant<int, cc>()); }
+        PASTA_C(1) PASTA_C(2) PASTA_C(3) PASTA_C(4) PASTA_C(5)
 #undef PASTA_C
         return -INFINITY;
       };
@@ -868,9 +869,9 @@ cudaError_t launch_t(const PoolView &pv, const PlanHeader &h, const TensorArgs &
 template <int D>
 cudaError_t launch_d(const PoolView &pv, const PlanHeader &h, const TensorArgs &a, const void *q, cudaStream_t st) {
   const int rows = h.w[PH_T_MAX_ROWS];
-  static_assert(U<D, 32>::RESIDENT == kv4_ctas_per_sm(D, 32) && U<D, D == 128 ? 80 : 64>::RESIDENT == kv4_ctas_per_sm(D, D == 128 ? 80 : 64) &&
-                U<D, 128>::RESIDENT == kv4_ctas_per_sm(D, 128), "the planner counts on it");
-  const auto launch = rows <= 32 ? launch_t<D, 32> : rows <= (D == 128 ? 80 : 64) ? launch_t<D, D == 128 ? 80 : 64> : launch_t<D, 128>;
+  constexpr int MOST = kv4_max_rows(D);
+  static_assert(U<D, 32>::RESIDENT == kv4_ctas_per_sm(32) && U<D, MOST>::RESIDENT == kv4_ctas_per_sm(MOST), "the planner counts on it");
+  const auto launch = rows <= 32 ? launch_t<D, 32> : launch_t<D, MOST>;
   return launch(pv, h, a, q, st);
 }
 

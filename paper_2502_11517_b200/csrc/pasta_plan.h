@@ -38,9 +38,12 @@
 #define PASTA_PMETA_STREAM(meta) ((meta) & PASTA_MAX_STREAMS)
 #define PASTA_PMETA_PAGE(meta) (((meta) >> PASTA_PMETA_STREAM_BITS) & (PASTA_MAX_STREAM_PAGES - 1))
 
-// 4-bit pools: CTAs of the tensor-core kernel that share an SM, by the most stacked rows of any t-request of the step (what they
-// need of the 512 TMEM columns decides)
-constexpr int kv4_ctas_per_sm(int head_dim, int rows) { return rows <= 32 ? 4 : rows <= (head_dim == 128 ? 80 : 64) ? 2 : 1; }
+// 4-bit pools: the most stacked rows of a t-request (a request with more is split into t-requests of even size, up to so many), and the
+// CTAs of the tensor-core kernel that share an SM, by the most rows of any t-request of the step.  What a CTA needs of the 512 TMEM
+// columns decides: with 128 rows there is room for one only, which takes longer per tile than two halves of the rows in two.
+constexpr int kv4_max_rows(int head_dim) { return head_dim == 128 ? 80 : 64; }
+constexpr int kKv4MaxParts = 8;
+constexpr int kv4_ctas_per_sm(int rows) { return rows <= 32 ? 4 : 2; }
 
 // header words
 enum {

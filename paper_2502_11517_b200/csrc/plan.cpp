@@ -100,6 +100,22 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     }
   }
 
+  // 4-bit pools: the queries of a request with many become several t-requests
+  if (lim.kv4) {
+    const int32_t most = kv4_max_rows(lim.head_dim) / G;
+    std::vector<int32_t> reqs, begins;
+    for (size_t g = 0; g < req_order.size(); ++g) {
+      const int32_t T = group_begin[g + 1] - group_begin[g];
+      int32_t parts = (T + most - 1) / most;
+      if (parts > kKv4MaxParts || !lim.tensor_path) parts = 1;
+      const int32_t per = (T + parts - 1) / parts;
+      for (int32_t at = 0; at < T; at += per) { reqs.push_back(req_order[g]); begins.push_back(group_begin[g] + at); }
+    }
+    begins.push_back(n);
+    req_order.swap(reqs);
+    group_begin.swap(begins);
+  }
+
   pages.clear(); pmeta.clear(); vis_tab.clear(); tq_tab.clear();
   std::vector<TReq> treqs;
   std::vector<WPiece> wpieces;
@@ -144,7 +160,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     // A request whose stacked rows fit one MMA tile sends EVERY stream it reads through the tensor-core kernel, the
     // private chunks too: rows that may not see a page are masked there, the MMA costs the same for any number of
     // valid rows, and the pass stays bandwidth-bound; the warp kernel is left with what does not fit.
-    bool tensor = lim.tensor_path && T >= 1 && T * G <= PASTA_MAX_ROWS;
+    bool tensor = lim.tensor_path && T >= 1 && T * G <= (lim.kv4 ? kv4_max_rows(lim.head_dim) : PASTA_MAX_ROWS);
     int32_t n_shared = 0;
     if (tensor) {
       bool too_long = false;                 // a page's meta word has 18 bits for its index within the stream
@@ -217,7 +233,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     if (lim.kv4) {
       int32_t rows = 0;
       for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
-      grid *= kv4_ctas_per_sm(lim.head_dim, rows);
+      grid *= kv4_ctas_per_sm(rows);
     }
     // 4-bit pools: what a t-request's tiles cost, summed up from its first, and what all of them cost.
     static thread_local std::vector<double> cost;

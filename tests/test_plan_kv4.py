@@ -74,3 +74,30 @@ def test_without_room_for_more_rows():
     script = cfg4_long_prefix(2, 3000, 3)
     with pytest.raises(binding.PastaError):
         check_script(script, flags=binding.FLAG_KV_INT4, max_partial_rows=8)
+
+
+@pytest.mark.parametrize("threads,parts", [(20, 1), (21, 2), (40, 2), (41, 3), (160, 8), (161, 0)])
+def test_requests_of_many_threads_are_split(threads, parts):
+    """80 rows to a part, 8 parts at most, more rows take the warp path; every query is in one part."""
+    pool = binding.Pool(1, 8, 2, 128, 40 + 2 * threads, 1, threads, 2 * threads + 2,
+                        flags=binding.FLAG_KV_INT4 | binding.FLAG_HOST_ONLY, max_step_queries=threads)
+    pool.request_begin()
+    pool.kv_append_run(0, 0, 200)
+    for t in range(1, threads):
+        assert pool.thread_spawn(0) == t
+        pool.kv_append_run(0, t, 1 + t % 20)
+    pool.step_begin([0] * threads, list(range(threads)), [0] * threads)
+    w = np.array(pool.plan_words())
+    assert w[3] == parts and w[4] + w[23] >= 2 * parts and (w[5] > 0) == (parts == 0)
+    rng = np.random.default_rng(2)
+    K, V = rng.standard_normal((2, 40 + 2 * threads, 16, 2, 128))
+    q = rng.standard_normal((threads, 8, 128))
+    got, _ = plan_interpreter.run_plan(w, K, V, q, 2)
+    streams = pool.dump()["requests"][0]["streams"]
+    for t in range(threads):
+        k, v = (np.concatenate([X[streams[i]["pages"]].reshape(-1, 2, 128)[:streams[i]["len"]] for i in ([0, t] if t else [0])]) for X in (K, V))
+        for h in range(8):
+            s = k[:, h // 4] @ q[t, h] / np.sqrt(128)
+            p = np.exp(s - s.max())
+            np.testing.assert_allclose(got[t, h], p @ v[:, h // 4] / p.sum(), rtol=0, atol=1e-11)
+    pool.close()
