@@ -483,9 +483,9 @@ pasta_status_t pasta_debug_hold_roles(pasta_pool_t *pool, int32_t role_mask);
  * one is kept back, `percent` of their tiles in all (0 to 50; 10 by default), in units of at most `tiles` tiles (2 to
  * 1024; 16 by default).  The CTAs take these from a shared counter once their own work is done: SMs that stream faster
  * than others then do more of it.  0 percent assigns everything in advance.  Takes effect from the next
- * pasta_step_begin, and only for steps large enough for it to matter (16 tiles per CTA).  On a 4-bit pool every run that is not
- * much longer than an even share is handed out at run time, whole; 0 percent assigns everything in advance there too, and
- * `tiles` says nothing.
+ * pasta_step_begin, and only for steps large enough for it to matter (16 tiles per CTA).  On a 4-bit pool the planner
+ * hands out whole runs where none is too long for that; 0 percent assigns everything in advance there too, and the numbers say
+ * nothing else.
  */
 pasta_status_t pasta_debug_set_tail(pasta_pool_t *pool, int32_t percent, int32_t tiles);
 /*

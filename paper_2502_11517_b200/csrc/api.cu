@@ -232,6 +232,7 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.tail_tiles = p->tail_tiles;
   l.kv4 = (p->cfg.flags & PASTA_FLAG_KV_INT4) != 0;
   l.capped = p->pv.softcap_log2 > 0.f;
+  l.layers = p->d.layers_per_launch;
   return l;
 }
 

@@ -353,7 +353,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     if (tid == 0) take();
     __syncthreads();
   }
-  bool more = next_unit(none_assigned ? blockIdx.x : unit_s[0]);
+  bool more = next_unit(none_assigned ? blockIdx.x : counted ? unit_s[0] : n_shared);
   if (more) {
     first_pages();
     first_copies();

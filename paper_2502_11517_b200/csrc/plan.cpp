@@ -13,9 +13,8 @@ constexpr int32_t kWholeRunSlackTiles = 3;
 // 4-bit pools, in thousands of cycles (measured with full SMs): a tile and each of its rows (padded to 16), without and with capped
 // scores, what masks multiply that by, and a unit's beginning and end and each of its rows.
 constexpr double kKv4Tile = 2.9, kKv4TileRow = 0.029, kKv4CappedRow = 0.13, kKv4Masked = 1.15, kKv4Unit = 5.5, kKv4UnitRow = 0.09;
-// A run stays whole up to so many shares and what the merge kernel behind cut runs takes: a launch of one layer then loses little to
-// its longest run, launches of several layers lose nothing.
-constexpr double kKv4WholeShares = 2, kKv4Merge = 40;
+// What shares cut in advance lose to one another, the merge kernel behind them, and how long a run handed out behind them may be.
+constexpr double kKv4CutLoss = 1.1, kKv4Merge = 19., kKv4Filling = 0.25;
 // Even cuts (8-bit pools, head_dim 64): pieces of at least 2 tiles and about one per resident CTA, and runs left whole while
 // the longest is at most 12 tiles longer than an even share (they then go to CTAs of six warps, which walk a tile in a third
 // of the time).  Measured, us for 1, 4, 12, 32 and 100 responses of 8 to 20 rows: 12.0, 18.0, 17.7, 30.6, 75.3; pieces of at
@@ -280,33 +279,40 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
       }
     }
-    // 4-bit pools: every run that is not much longer than an even share goes to the pool whole, the longest first and all layers of one
-    // before the next, so that the short ones even out what CTAs and units take.  (Measured, us, against equal shares in advance:
-    // 170 for 187 with 64 requests of 4 to 9 threads, 182 for 250 with capped scores, 49 for 54 with 1 to 5 threads.)
-    if (lim.kv4 && lim.tail_percent > 0) {
-      const double longest = kKv4WholeShares * all_cost / grid + kKv4Merge;
-      for (size_t ti = 0; ti < treqs.size(); ++ti) {
-        const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
-        if (cost[cost0[ti] + n_tiles] + unit_cost(ti) <= longest) std::fill_n(tail.begin() + ti * lim.n_kv_heads, lim.n_kv_heads, n_tiles);
-      }
+    // 4-bit pools: runs go to the pool whole, the longest first and all layers of one before the next, so that the short ones even out what
+    // CTAs and units take, as long as none takes longer than a launch (of as many layers as the pool's launches have at most) in
+    // which every run is cut into shares.  Where some do, they are cut, and only runs much shorter than a share are handed out behind
+    // them.  Measured, us, whole and cut: 64 requests of 1 to 9 threads 89 and 100 for one layer, 151 and 182 for two; 32 of them 80 and
+    // 61; with capped scores 76 and 80, four layers 157 and 250; 1 to 5 threads of head_dim 64 40 and 34, two layers 46 and 53.
+    if (lim.kv4 && lim.tail_percent > 0 && !treqs.empty()) {
+      double units = 0, longest = 0;
+      auto run_cost = [&](size_t ti) { return cost[cost0[ti] + (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES] + unit_cost(ti); };
+      for (size_t ti = 0; ti < treqs.size(); ++ti) { units += unit_cost(ti); longest = std::max(longest, run_cost(ti)); }
+      const double launch = lim.layers * (all_cost / grid + units / treqs.size());
+      const double most = longest <= kKv4CutLoss * launch + kKv4Merge ? longest : kKv4Filling * launch;
+      for (size_t ti = 0; ti < treqs.size(); ++ti)
+        if (run_cost(ti) <= most)
+          std::fill_n(tail.begin() + ti * lim.n_kv_heads, lim.n_kv_heads, (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES);
     }
     const double overhead = 1.0;
     const int32_t min_piece = 1;
     double total = 0, unassigned = 0, left = 0;           // unassigned: cost of what has no CTA; left: of the present CTA's share
     int32_t cta = -1;
-    bool any_run = false;
+    int64_t runs = 0;
+    double units = 0;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
       for (int32_t g = 0; g < lim.n_kv_heads; ++g) {
         const int32_t kept = n_tiles - tail[ti * lim.n_kv_heads + g];
         if (kept > 0) total += kept + overhead;
         if (kept > 0 && lim.kv4) {
-          any_run = true;
+          ++runs;
+          units += unit_cost(ti);
           unassigned += cost[cost0[ti] + kept] + unit_cost(ti);
         }
       }
     }
-    if (any_run) unassigned += grid * unit_cost(0);        // about a cut per CTA
+    const double cut = runs ? units / runs : 0;           // about one more unit for every CTA
     const double target = std::max(total, 1.0) / grid;
     double cum = 0;
     // A small step (one response, a few threads, a context of a few hundred tokens) is not cut at all when every run can
@@ -382,7 +388,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
             // the next CTA takes an even share of what remains, unless what the present one has left is worth a unit
             if (cta < 0 || (cta + 1 < grid && left < unit + 0.5 * (sums[begin + 1] - sums[begin]))) {
               ++cta;
-              left = unassigned / (grid - cta);
+              left = (unassigned + cut * (grid - cta - 1)) / (grid - cta);
             }
             int32_t end = n_tiles;
             if (cta + 1 < grid) {
@@ -393,7 +399,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
             unit_cta.push_back(cta);
             t_rows += rows;
             left -= unit + sums[end] - sums[begin];
-            unassigned = std::max(0., unassigned - unit - (sums[end] - sums[begin]));
+            unassigned = std::max(0., unassigned - (sums[end] - sums[begin]) - (end == n_tiles ? unit : 0.));
             begin = end;
             continue;
           }

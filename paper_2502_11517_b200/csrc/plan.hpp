@@ -18,6 +18,7 @@ struct PlanLimits {
   int32_t tail_tiles;    // tiles per unit of that share
   bool kv4 = false;      // 4-bit pool: `grid` is multiplied by kv4_ctas_per_sm of the step's rows
   bool capped = false;      // scores are capped
+  int32_t layers = 1;       // layers of a launch, at most
   bool even_cuts = false;   // t-units are launched one per CTA (8-bit pools): runs are cut into pieces of one length
 };
 

@@ -39,8 +39,6 @@ def test_held_products(lib, lengths, threads, d):
     ref, out = (torch.zeros(q.shape, device="cuda") for _ in range(2))
     words = pool.plan_words()                          # units assigned in advance, units handed out at run time
     assert words[4] + words[23] > 0
-    if len(lengths) != 1:
-        assert words[23] > 0
     pool.decode_attn(q, ref)
     torch.cuda.synchronize()
     assert pool.status() == lib.OK

@@ -30,28 +30,30 @@ def _shares(script, steps=None, **kw):
             plan_interpreter.STATS.get("no_merge_plans", 0) - before[1], stats["steps"])
 
 
-@pytest.mark.parametrize("maker,whole", [(lambda: cfg1_tiny(), True), (lambda: cfg3_batched(24, 1, prefix_range=(20, 900)), True),
-                                         (lambda: cfg4_long_prefix(2, 3000, 3), False)])
-def test_short_runs_stay_whole_and_long_ones_are_cut(maker, whole):
-    assigned, shared, final, steps = _shares(maker())
+@pytest.mark.parametrize("maker,layers,whole", [(lambda: cfg1_tiny(), 1, True), (lambda: cfg3_batched(24, 1, prefix_range=(20, 900)), 8, True),
+                                                (lambda: cfg3_batched(24, 1, prefix_range=(20, 900)), 1, False),
+                                                (lambda: cfg4_long_prefix(2, 3000, 3), 1, False)])
+def test_runs_stay_whole_unless_they_take_longer_than_a_launch(maker, layers, whole):
+    """Launches of several layers have other units to fill the time that the longest run takes; one layer's have not."""
+    assigned, shared, final, steps = _shares(maker(), layers=layers)
     if whole:
         assert assigned == 0 and shared > 0 and final == steps
     else:
-        assert assigned > 0 and shared == 0
+        assert assigned > 0 and final < steps
 
 
 def test_a_step_of_both():
-    """Two long texts among short ones: the long ones are cut over the CTAs, the others are handed out whole."""
-    lengths = [9000] + [40 + 90 * i for i in range(12)] + [7000]
+    """Two long texts among short ones: the long ones are cut over the CTAs, short ones are handed out whole."""
+    lengths = [90000] + [40 + 90 * i for i in range(12)] + [70000]
     geo = Geometry(1, 4, 2, 128, 16)
-    pool = binding.Pool(1, geo.n_q_heads, geo.n_kv_heads, geo.head_dim, sum(n // 16 + 2 for n in lengths), len(lengths), 1, 2,
+    pool = binding.Pool(8, geo.n_q_heads, geo.n_kv_heads, geo.head_dim, sum(n // 16 + 2 for n in lengths), len(lengths), 1, 2,
                         flags=binding.FLAG_KV_INT4 | binding.FLAG_HOST_ONLY)
     for r, n in enumerate(lengths):
         assert pool.request_begin() == r
         pool.kv_append_run(r, 0, n)
     pool.step_begin(list(range(len(lengths))), [0] * len(lengths), [0] * len(lengths))
     w = np.array(pool.plan_words())
-    assert w[4] > 4 and w[23] == 2 * 12
+    assert w[4] > 4 and 0 < w[23] <= 2 * 12
     # (every CTA takes part in handing out; those with nothing assigned come last, and are not what the interpreter looks at)
     cta = w[w[14]: w[14] + 2 * w[8]].reshape(-1, 2)
     w[8] = int((cta[:, 1] > cta[:, 0]).sum())
