@@ -23,14 +23,14 @@
 // measured copy bandwidth.  A warp alone issues one every seven cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so
 // CTAs share an SM and fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows, two of 256 threads and
 // 256 columns for up to 80 (64 at head_dim 64); requests with more rows are split by the planner.  Schedulers issue in 53 % of the cycles; a tile takes 2500
-// (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 152 us (39 us for the bytes alone), 8 prefixes of
-// 32768 tokens and 68 rows 236 us (52), 64 capped short responses 157 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
+// (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 151 us (39 us for the bytes alone), 8 prefixes of
+// 32768 tokens and 68 rows 232 us (52), 64 capped short responses 157 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
 // Built and measured slower: roles on warps of their own and one CTA to an SM, in three forms (290 to 390 us for the first, 310 to 410
 // for the second: hand-overs and four programs' instruction fetches); twice the threads per CTA at 64 registers (302 and 418); bulk
 // copies in place of 16-byte ones (192 and 277 for 191 and 274 then); one body for the chunks of the softmax instead of one for
 // every number of them (154 and 243 for 152 and 236).
 //
-// A CTA walks units as those of attn_tensor.cu do, but most are handed out at run time, whole runs, the longest first.  TMEM holds one
+// A CTA walks units as those of attn_tensor.cu do, but where runs are short they are handed out at run time, whole, the longest first.  TMEM holds one
 // operand (K, then V in its place), the scores and O^T.  Every warp does everything in turn.
 // References: a weight is 2^(score - ref), and any ref that keeps weights inside the range of fp32 and bf16 (which share their exponents)
 // gives the same relative precision.  So a row's ref starts at 0 and nobody looks for maxima.  When a score exceeds its row's ref by

@@ -282,8 +282,8 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     // 4-bit pools: runs go to the pool whole, the longest first and all layers of one before the next, so that the short ones even out what
     // CTAs and units take, as long as none takes longer than a launch (of as many layers as the pool's launches have at most) in
     // which every run is cut into shares.  Where some do, they are cut, and only runs much shorter than a share are handed out behind
-    // them.  Measured, us, whole and cut: 64 requests of 1 to 9 threads 89 and 100 for one layer, 151 and 182 for two; 32 of them 80 and
-    // 61; with capped scores 76 and 80, four layers 157 and 250; 1 to 5 threads of head_dim 64 40 and 34, two layers 46 and 53.
+    // them.  Measured, us, whole and cut: 64 requests of 1 to 9 threads 89 and 101 for one layer, 160 and 181 for two; 32 of them 80 and
+    // 61; 64 with capped scores 76 and 75, four layers 167 and 235; 1 to 5 threads of head_dim 64 40 and 32, two layers 45 and 50.
     if (lim.kv4 && lim.tail_percent > 0 && !treqs.empty()) {
       double units = 0, longest = 0;
       auto run_cost = [&](size_t ti) { return cost[cost0[ti] + (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES] + unit_cost(ti); };
