@@ -34,7 +34,7 @@
 // operand (K, then V in its place), the scores and O^T.  Every warp does everything in turn.
 // References: a weight is 2^(score - ref), and any ref that keeps weights inside the range of fp32 and bf16 (which share their exponents)
 // gives the same relative precision.  So a row's ref starts at 0 and nobody looks for maxima.  When a score exceeds its row's ref by
-// more than 2^R_SLACK (the CTA votes on that with the barrier that publishes the weights), the rows' maxima over the tile are worked out, and
+// more than R_SLACK (the CTA votes on that with the barrier that publishes the weights), the rows' maxima over the tile are worked out, and
 // O and l brought to them.  A row that saw tokens but whose sum came out below 2^-60 has scores far below 0: its unit is done again,
 // with first references from the maxima of the first tokens each row sees.
 // The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.

@@ -761,3 +761,27 @@ def test_refusals(lib):
     assert lib.lib().pasta_kv_read_layers(pool._h, 0, 1, 0, 0, 0, 20, lib._dev(odd), lib._dev(good), None) == lib.INVALID_ARG
     pool.decode_attn(q, out[:1024])
     assert pool.status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("length", [100, 3000])
+@pytest.mark.parametrize("levels", [(-5, -30, -39, -41), (-43, -60, -86, -88), (-95, -104, -140, 3), (20, 88, 300, -700)])
+def test_rows_at_levels_from_faint_to_large(lib, d, length, levels):
+    """Four rows of one unit whose scores all lie around the given numbers (natural units): some are within the range of a weight
+    whose reference is zero, some below it, some above."""
+    import torch
+    q = torch.tensor(levels, dtype=torch.float32)[:, None] * torch.ones(4, d) / 8
+    q = q.to(torch.bfloat16)[None, None]                                  # [1, 1, 4, d]
+    k = torch.ones((1, length, 1, d)) * (8 / d ** 0.5) * (1 + 0.02 * _randn((1, length, 1, 1), 4).float())
+    k, v = k.to(torch.bfloat16), _randn((1, length, 1, d), 2)
+    pool = _pool(lib, length // 16 + 2, hq=4, hkv=1, d=d)
+    model, store = PoolModel(length // 16 + 2, 16, None, 1, 1, 4), Kv4Store(length // 16 + 2, 16, 1, d)
+    pool.request_begin(); model.request_begin()
+    pool.kv_append_run(0, 0, length, k.cuda(), v.cuda()); store.write(model.append_run(0, 0, length), k[0], v[0])
+    pool.step_begin([0], [0], [0])
+    out = torch.empty((1, 1, 4, d), device="cuda"); lse = torch.empty((1, 1, 4), device="cuda")
+    for _ in range(2):
+        pool.decode_attn(q.cuda(), out, lse)
+        want, want_lse = decode_attention_capped(model, store, [(0, 0)], q[0])
+        compare(out[0], lse[0], want, want_lse, q[0].float().numpy(), store)
+    assert pool.status() == lib.OK
