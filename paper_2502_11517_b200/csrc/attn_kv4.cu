@@ -160,7 +160,7 @@ __device__ __forceinline__ float warp_sum8(const float *v, int lane) {
   return t + __shfl_xor_sync(0xffffffffu, t, 1);
 }
 
-// one lane of a whole warp
+// one lane of a whole warp, the same one every time
 __device__ __forceinline__ bool elect_lane() {
   uint32_t y;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(y));
@@ -838,7 +838,8 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   __syncthreads();
   if (*abort_flag) {
     // Some wait has run out and the whole CTA has left in the middle of its work: MMAs in flight end on their own and are waited for.
-    if (lane == 0 && warp < 4) {                       // every warp that issues MMAs
+    // A commit follows the MMAs of the thread that makes it, so the lane that is elected to issue them makes it.
+    if (warp < 4 && elect_lane()) {                    // every warp that issues MMAs
       mma_commit(bar + 8 * L::B_DRAIN);
       mbar_wait_bounded(bar + 8 * L::B_DRAIN, 0);
     }

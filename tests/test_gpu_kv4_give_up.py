@@ -71,3 +71,26 @@ def test_copies_and_the_warp_shuffle_kernel_have_nothing_to_hold(lib, d):
         pool.decode_attn(_randn((1, 1, 8, d), 3).cuda(), out)
         assert pool.status() == lib.OK and bool((out != 0).any())
         pool.close()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("threads", [2, 17])
+@pytest.mark.parametrize("lengths", [[300], [120 + 37 * i for i in range(40)], [30000, 200, 300, 25000]], ids=["one", "many", "mixed"])
+def test_giving_up_while_products_are_under_way(lib, lengths, threads, d):
+    """A limit so short that a wait for a product that has just begun may give up: the CTA waits for it before it frees the tensor
+    memory, and the launches behind it find everything as it was."""
+    import torch
+    pool, q = _filled(lib, lengths, threads, 8, 2, d, 2)
+    ref, out = (torch.zeros(q.shape, device="cuda") for _ in range(2))
+    pool.decode_attn(q, ref)
+    assert pool.status() == lib.OK
+    for _ in range(5):
+        pool.debug_set_wait_limit(1)
+        for _ in range(3):
+            pool.decode_attn(q, out)
+        status = pool.status()
+        assert status == lib.TIMEOUT or (status == lib.OK and torch.equal(out, ref))
+        pool.debug_set_wait_limit(0)
+        pool.decode_attn(q, out)
+        assert torch.equal(out, ref) and pool.status() == lib.OK
+    pool.close()
