@@ -37,6 +37,10 @@
 // more than R_SLACK (the CTA votes on that with the barrier that publishes the weights), the rows' maxima over the tile are worked out, and
 // O and l brought to them.  A row that saw tokens but whose sum came out below 2^-60 has scores far below 0: its unit is done again,
 // with first references from the maxima of the first tokens each row sees.
+// A reference is a score rounded to fp32, and what a score exceeds it by comes out of one multiply-add, unrounded.  The two differ by half a
+// step of the score: nothing near 0, but whole powers of two from 2^24 on, and from 2^31 weights that are infinite, or all zero.  So the unit
+// of a row with a reference beyond R_FAR is done again without tensor cores (plain_rows), where a row's largest score is exactly its
+// reference.  (Rounded products beside the others on the tensor path cost every step 3 to 7 % for want of registers.)
 // The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.
 // Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
 #include <algorithm>
@@ -49,6 +53,7 @@ namespace pasta {
 namespace {
 
 constexpr float R_SLACK = 10.f;                  // weights are at most 2^10 (bf16 and fp32 keep their precision at any size)
+constexpr float R_FAR = 16777216.f;              // 2^24: beyond it a score and its rounding differ by whole powers of two
 constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing (careful units)
 constexpr float R_FAINT = 8.7e-19f;              // 2^-60: sums below it may have lost weights to fp32's range
 
@@ -160,6 +165,8 @@ __device__ __forceinline__ float warp_sum8(const float *v, int lane) {
   return t + __shfl_xor_sync(0xffffffffu, t, 1);
 }
 
+__device__ __forceinline__ bool is_far(float ref) { return fabsf(ref) >= R_FAR && fabsf(ref) < INFINITY && ref != R_UNSET; }
+
 // one lane of a whole warp, the same one every time
 __device__ __forceinline__ bool elect_lane() {
   uint32_t y;
@@ -188,6 +195,93 @@ __device__ __forceinline__ void cta_wait(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// A unit's rows without tensor cores, a warp to a row: a lane has half of a token's channels for the scores, and D / 32 channels
+// of V.  o is kept as the mean of the values so far, so nothing leaves the range of what is held.
+template <int D, int kWarps>
+__device__ __forceinline__ void plain_rows(const PoolView &pv, const TensorArgs &a, const __nv_bfloat16 *q, const UnitInfo &x, int layer) {
+  constexpr int E = D / 32, BLOCK = kv4_block_bytes(D);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = pv.n_q_heads / pv.n_kv_heads, g_shift = 31 - __clz(G);
+  const int32_t *plan = pv.plan;
+  const uint8_t *head = pv.kv_base + (a.layer_begin + layer) * pv.layer_stride + static_cast<int64_t>(x.g) * BLOCK;
+  const int last = min(x.tile_end * PASTA_TILE_PAGES, x.n_pages), r = lane & 15;
+#pragma unroll 1
+  for (int row = warp; row < x.n_threads << g_shift; row += kWarps) {
+    const int thread = row >> g_shift, qn = plan[a.off_tq + x.tq_off + thread];
+    const int64_t at = (static_cast<int64_t>(layer) * a.n_queries + qn) * pv.n_q_heads + x.g * G + (row & (G - 1));
+    const uint32_t *q_row = reinterpret_cast<const uint32_t *>(q + at * D);
+    float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int p = x.tile_begin * PASTA_TILE_PAGES; p < last; ++p) {
+      const int page = plan[a.off_pages + x.page_off + p], meta = plan[a.off_pmeta + x.page_off + p];
+      if (page < 0 || page >= pv.n_pages || meta < 0) continue;               // (reported when it was to be copied)
+      const int sees = plan[a.off_vis + x.vis_off + thread * x.n_streams + min(PASTA_PMETA_STREAM(meta), x.n_streams - 1)] -
+                       PASTA_PMETA_PAGE(meta) * PASTA_PAGE;
+      if (sees <= 0) continue;
+      const uint8_t *block = head + static_cast<int64_t>(page) * pv.n_kv_heads * BLOCK;
+      float s = 0.f;
+#pragma unroll 1
+      for (int g = lane >> 4; g < D / kKv4Group; g += 2) {
+        const uint4 c = *reinterpret_cast<const uint4 *>(block + g * 256 + r * 16);
+        const uint32_t t = *reinterpret_cast<const uint16_t *>(block + kv4_k_scales(D) + (r * (D / kKv4Group) + g) * 2);
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w}, t2 = t | (t << 16), c2 = kv4_offset_of(t2);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t k = kv4_value(kv4_pair(w[i >> 2], i & 3), t2, c2), qi = __ldg(q_row + g * 16 + i);
+          s = fmaf(bf16_hi(k), bf16_hi(qi), fmaf(bf16_lo(k), bf16_lo(qi), s));
+        }
+      }
+      s = __fmul_rn(s + __shfl_xor_sync(0xffffffffu, s, 16), a.scale_log2);
+      if (r >= sees) s = -INFINITY;
+      float top = s;
+#pragma unroll
+      for (int i = 8; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+      top = fmaxf(m, top);
+      const float ref = top > -INFINITY ? top : 0.f;                           // (scores below the range of fp32 weigh nothing)
+      float w = fast_exp2(__fadd_rn(s, -ref)), sum = w;
+#pragma unroll
+      for (int i = 8; i > 0; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+      const float before = l * fast_exp2(m - ref);
+      m = top;
+      l = before + sum;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      w *= inv;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint2 c = *reinterpret_cast<const uint2 *>(block + kv4_v_codes(D) + (lane * E + e) * 8);
+        o[e] *= before * inv;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t t2 = *reinterpret_cast<const uint32_t *>(block + kv4_v_scales(D) + (lane * E / kKv4Group) * 32 + j * 4);
+          const uint32_t v = kv4_value(kv4_pair(j < 4 ? c.x : c.y, j & 3), t2, kv4_offset_of(t2));
+          o[e] = fmaf(__shfl_sync(0xffffffffu, w, 2 * j), bf16_lo(v), o[e]);
+          o[e] = fmaf(__shfl_sync(0xffffffffu, w, 2 * j + 1), bf16_hi(v), o[e]);
+        }
+      }
+    }
+    if (l != l) {                                                              // a query that is not finite, or a score above the range of fp32
+      m = not_a_row().x;
+      l = not_a_row().y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = NAN;
+    }
+    if (x.final_rows != 0) {
+      if (a.lse && lane == 0) a.lse[at] = (m + log2f(l)) * 0.6931471805599453f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.out)[at * D + lane * E + e] = __float2bfloat16_rn(o[e]);
+        else static_cast<float *>(a.out)[at * D + lane * E + e] = o[e];
+      }
+    } else {
+      const int64_t part = static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + row;
+      if (lane == 0) pv.part_ml[part] = make_float2(m, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) pv.part_o[part * D + lane * E + e] = o[e] * l;
+    }
+  }
+}
+
 template <int D, int NMAX, bool kCap>
 __global__ void __launch_bounds__(U<D, NMAX>::THREADS, U<D, NMAX>::RESIDENT)
 attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) {
@@ -205,6 +299,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);
   int32_t *unit_s = reinterpret_cast<int32_t *>(misc + 4);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(misc + 1);
+  volatile int *far_flag = reinterpret_cast<volatile int *>(misc + 2);        // a row of the unit is_far
   float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
   float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
   int32_t *row_s = reinterpret_cast<int32_t *>(warp_s);
@@ -215,7 +310,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
 
   if (tid == 0) {
     for (int b = 0; b < L::B_COUNT; ++b) mbar_init(bar + 8 * b, b == L::B_DRAIN ? 4 : 1);
-    misc[1] = 0;
+    misc[1] = misc[2] = 0;
     unit_s[0] = -1;                                   // the last number taken
     mbar_init_fence();
   }
@@ -361,7 +456,9 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   // A row's reference is 0 at first: weights are 2^score, scores above R_SLACK raise it, and a row whose sum shows that its scores
   // are far below (or all minus infinity) has its unit done again, carefully: first references from the first tokens' maxima.
   bool careful = false;
+units:
   while (more) {
+    if (!kCap && careful && *far_flag != 0) break;                // to be done without tensor cores
     const int nt = x.tile_end - x.tile_begin;
     const int rows = x.n_threads << g_shift, n = (rows + 15) & ~15;
     const bool fin = x.final_rows != 0;
@@ -773,6 +870,10 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
       const int thread = tid >> g_shift;
       const uint32_t saw = saw_s[thread >> 4] | saw_s[8 + (thread >> 4)] | saw_s[16 + (thread >> 4)] | saw_s[24 + (thread >> 4)];
       faint = !careful && sum < R_FAINT && ((saw >> (thread & 15)) & 1);
+      if (!kCap && is_far(ref_s[tid])) {
+        faint = true;
+        *far_flag = 1;
+      }
       row_s[tid] = at;                                 // (where the thread has read its row's first sum)
     }
     cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
@@ -830,6 +931,22 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+  }
+
+  if (!kCap && more && *abort_flag == 0) {
+    // ---- a unit with a row that is too far from 0 (out here its code costs the units of the loop no registers)
+    plain_rows<D, L::THREADS / 32>(pv, a, q, x, layer);
+    copies_wait<0>();
+    __syncthreads();
+    if (tid == 0) *far_flag = 0;
+    careful = false;
+    more = next_unit(counted ? unit_s[0] : n_shared);
+    if (more) {
+      first_pages();
+      first_copies();
+    }
+    __syncthreads();
+    goto units;
   }
 
   // ---- tear-down
