@@ -32,15 +32,18 @@
 //
 // A CTA walks units as those of attn_tensor.cu do, but where runs are short they are handed out at run time, whole, the longest first.  TMEM holds one
 // operand (K, then V in its place), the scores and O^T.  Every warp does everything in turn.
-// References: a weight is 2^(score - ref), and any ref that keeps weights inside the range of fp32 and bf16 (which share their exponents)
-// gives the same relative precision.  So a row's ref starts at 0 and nobody looks for maxima.  When a score exceeds its row's ref by
+// References: a weight is 2^(score - ref), and any ref that keeps weights, and their products with values, inside the range of fp32 and bf16
+// (which share their exponents) gives the same relative precision.  So a row's ref starts at 0 and nobody looks for maxima.  When a score exceeds its row's ref by
 // more than R_SLACK (the CTA votes on that with the barrier that publishes the weights), the rows' maxima over the tile are worked out, and
 // O and l brought to them.  A row that saw tokens but whose sum came out below 2^-60 has scores far below 0: its unit is done again,
 // with first references from the maxima of the first tokens each row sees.
 // A reference is a score rounded to fp32, and what a score exceeds it by comes out of one multiply-add, unrounded.  The two differ by half a
 // step of the score: nothing near 0, but whole powers of two from 2^24 on, and from 2^31 weights that are infinite, or all zero.  So the unit
 // of a row with a reference beyond R_FAR is done again without tensor cores (plain_rows), where a row's largest score is exactly its
-// reference.  (Rounded products beside the others on the tensor path cost every step 3 to 7 % for want of registers.)
+// reference.  The same where values next to the range's upper end, under many weights, add up to more than fp32 or the merge holds; rows whose
+// weights are small and whose values are so too that products may have been lost (all of O below 2^-110) are done again carefully.  O is looked at for
+// that only where the weights' sums allow either.
+// (Rounded products beside the others on the tensor path cost every step 3 to 7 % for want of registers.)
 // The threads that share a token (or channel) share its groups of channels, its pages and its chunks of eight rows.
 // Every wait is bounded; on expiry the CTA reports PASTA_ERR_TIMEOUT, drains and leaves.
 #include <algorithm>
@@ -55,6 +58,8 @@ namespace {
 constexpr float R_SLACK = 10.f;                  // weights are at most 2^10 (bf16 and fp32 keep their precision at any size)
 constexpr float R_FAR = 16777216.f;              // 2^24: beyond it a score and its rounding differ by whole powers of two
 constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing (careful units)
+constexpr float O_PART = 0x1p118f, O_TINY = 0x1p-110f;       // sums of weighted values: at most, in partial rows (2^9 of them are added up); looked at
+constexpr float L_PART = 0x1p4f, L_FINAL = 0x1p14f, L_TINY = 0x1p-16f;      // ... where the weights' sum lets them be more, or less (values: below 2^114)
 constexpr float R_FAINT = 8.7e-19f;              // 2^-60: sums below it may have lost weights to fp32's range
 
 // Sizes of one build: head_dim D, at most NMAX stacked rows.
@@ -197,7 +202,7 @@ __device__ __forceinline__ void cta_wait(uint32_t bar, uint32_t parity, volatile
 
 // A unit's rows without tensor cores, a warp to a row: a lane has half of a token's channels for the scores, and D / 32 channels
 // of V.  o is kept as the mean of the values so far, so nothing leaves the range of what is held.
-template <int D, int kWarps>
+template <int D, int kWarps, bool kCap>
 __device__ __forceinline__ void plain_rows(const PoolView &pv, const TensorArgs &a, const __nv_bfloat16 *q, const UnitInfo &x, int layer) {
   constexpr int E = D / 32, BLOCK = kv4_block_bytes(D);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = pv.n_q_heads / pv.n_kv_heads, g_shift = 31 - __clz(G);
@@ -233,6 +238,7 @@ __device__ __forceinline__ void plain_rows(const PoolView &pv, const TensorArgs 
         }
       }
       s = __fmul_rn(s + __shfl_xor_sync(0xffffffffu, s, 16), a.scale_log2);
+      if (kCap) s = softcap(s * a.cap_inv, pv.softcap_log2);
       if (r >= sees) s = -INFINITY;
       float top = s;
 #pragma unroll
@@ -275,6 +281,13 @@ __device__ __forceinline__ void plain_rows(const PoolView &pv, const TensorArgs 
       }
     } else {
       const int64_t part = static_cast<int64_t>(layer) * pv.rows_per_layer + x.row_base + row;
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(o[e]));
+      if (warp_max(top) * l >= O_PART) {                                         // (l is at most 2^22: a run's tokens)
+        m += 24.f;
+        l *= 0x1p-24f;
+      }
       if (lane == 0) pv.part_ml[part] = make_float2(m, l);
 #pragma unroll
       for (int e = 0; e < E; ++e) pv.part_o[part * D + lane * E + e] = o[e] * l;
@@ -299,7 +312,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   uint32_t *misc = reinterpret_cast<uint32_t *>(sm + L::OFF_MISC);
   int32_t *unit_s = reinterpret_cast<int32_t *>(misc + 4);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(misc + 1);
-  volatile int *far_flag = reinterpret_cast<volatile int *>(misc + 2);        // a row of the unit is_far
+  volatile int *far_flag = reinterpret_cast<volatile int *>(misc + 2);        // the unit is one for plain_rows
   float *ref_s = reinterpret_cast<float *>(sm + L::OFF_REF), *fact_s = reinterpret_cast<float *>(sm + L::OFF_FACT);
   float *warp_s = reinterpret_cast<float *>(sm + L::OFF_WARP);
   int32_t *row_s = reinterpret_cast<int32_t *>(warp_s);
@@ -458,7 +471,7 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   bool careful = false;
 units:
   while (more) {
-    if (!kCap && careful && *far_flag != 0) break;                // to be done without tensor cores
+    if (careful && *far_flag != 0) break;                // to be done without tensor cores
     const int nt = x.tile_end - x.tile_begin;
     const int rows = x.n_threads << g_shift, n = (rows + 15) & ~15;
     const bool fin = x.final_rows != 0;
@@ -853,7 +866,8 @@ units:
       if ((lane & 3) == 0) warp_s[wq * NMAX + 8 * c + (lane >> 2)] = t;
     }
     __syncthreads();
-    bool faint = false;
+    bool faint = false, look_at_o = false, small = false;
+    int32_t *top_s = reinterpret_cast<int32_t *>(warp_s) + NMAX;       // [NMAX] largest magnitude in a row of O (where the thread has read its row's sums)
     if (tid < rows) {
       const float sum = (warp_s[tid] + warp_s[NMAX + tid]) + (warp_s[2 * NMAX + tid] + warp_s[3 * NMAX + tid]);
       const bool spoilt = sum != sum;
@@ -874,12 +888,40 @@ units:
         faint = true;
         *far_flag = 1;
       }
+      small = !careful && sum > 0.f && sum < L_TINY;
+      look_at_o = small || sum > (fin ? L_FINAL : L_PART);
+      top_s[tid] = 0;
       row_s[tid] = at;                                 // (where the thread has read its row's first sum)
     }
     cta_wait(bar + 8 * L::B_PV, (it - 1) & 1, abort_flag, limit);
-    const bool again = __syncthreads_or(faint || *abort_flag != 0);
+    bool again = __syncthreads_or(faint || look_at_o || *abort_flag != 0);
     if (again && __syncthreads_or(*abort_flag != 0)) break;
     tc_fence_after();
+    const uint32_t o_addr = lane_addr + L::COL_O + (D == 64 ? (wq >> 1) * 8 : 0);
+    if (again) {
+#pragma unroll 1
+      for (int c = half; 8 * c < rows; c += H) {
+        uint32_t o[8], mine = 0;
+        tmem_ld8_issue(o_addr + c * 8 * L::OW, o);
+        tmem_ld_wait8(o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t top = __reduce_max_sync(0xffffffffu, o[j] & 0x7fffffffu);
+          if (lane == j) mine = top;
+        }
+        if (lane < 8 && 8 * c + lane < rows) atomicMax(top_s + 8 * c + lane, static_cast<int>(mine));
+      }
+      __syncthreads();
+      if (tid < rows && look_at_o) {
+        const float top = __int_as_float(top_s[tid]);
+        if (!(top < (fin ? INFINITY : O_PART))) {
+          faint = true;
+          *far_flag = 1;
+        }
+        faint |= small && top < O_TINY;
+      }
+      again = __syncthreads_or(faint);
+    }
     // ---- the copies of the unit behind it, under way while this one's rows are written
     const int taken = counted ? unit_s[0] : n_shared;
     if (again) careful = true;
@@ -892,7 +934,6 @@ units:
       first_copies();
     }
     if (again) continue;
-    const uint32_t o_addr = lane_addr + L::COL_O + (D == 64 ? (wq >> 1) * 8 : 0);
     float *sum_s = reinterpret_cast<float *>(sm + L::OFF_P) + (token & 63);
     if constexpr (D == 64) {
       if (wq >= 2) {
@@ -933,9 +974,9 @@ units:
     tc_fence_after();
   }
 
-  if (!kCap && more && *abort_flag == 0) {
-    // ---- a unit with a row that is too far from 0 (out here its code costs the units of the loop no registers)
-    plain_rows<D, L::THREADS / 32>(pv, a, q, x, layer);
+  if (more && *abort_flag == 0) {
+    // ---- a unit with a row that is too far from 0, or too large (out here its code costs the units of the loop no registers)
+    plain_rows<D, L::THREADS / 32, kCap>(pv, a, q, x, layer);
     copies_wait<0>();
     __syncthreads();
     if (tid == 0) *far_flag = 0;
