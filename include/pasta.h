@@ -93,8 +93,9 @@ enum {
  * is appended again.  With the rotary appends K is rotated in 64 bits, rounded to fp32 and then quantised.
  * An element that is not finite is stored as zero (with a rotary append both elements of a rotated pair), and pasta_pool_status reports
  * PASTA_ERR_DEVICE_CHECK: everything in a 4-bit pool is finite.
- * A query row with an element that is not finite, or with a score above the range of fp32, comes out as NaN, its lse not finite,
- * capped or not; other rows are untouched.  A score below that range weighs nothing.
+ * A query row with an element that is not finite comes out as NaN, its lse not finite, capped or not; other rows are untouched.
+ * Without a cap so does a row with a score above the range of fp32, and a score below it weighs nothing (a row of such scores alone
+ * is zeros, its lse minus infinity); under a cap they count as the cap and minus the cap.
  * Every entry point works on such a pool as it does on a bf16 one (same tensors, same shapes: k, v and q are bf16; k, v, q and
  * out have to be 16-byte aligned, else INVALID_ARG).  pasta_kv_bytes is n_layers * n_pages * n_kv_heads * 18 * head_dim.
  * Requests of up to 640 stacked rows (queries of the step x group; 512 with head_dim 64) and 4095 streams run on tensor cores: queries,

@@ -526,9 +526,10 @@ attn_warp_kernel(PoolView pv, int32_t off_wunit, int32_t off_pages, int32_t n_wu
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      const float m_new = fmaxf(m[h], mx);          // finite: nv >= 1
-      const float corr = fast_exp2(m[h] - m_new);   // 0 on the first page
-      const float pj = fast_exp2(sc - m_new);       // 0 for masked rows
+      const float m_new = fmaxf(m[h], mx);          // finite (nv >= 1) but in 4-bit pools, whose scores below the range of fp32 weigh nothing
+      const float ref = kKv4 && m_new == -INFINITY ? 0.f : m_new;
+      const float corr = fast_exp2(m[h] - ref);     // 0 on the first page
+      const float pj = fast_exp2(sc - ref);         // 0 for masked rows
       l[h] = l[h] * corr + (sub == 0 ? pj : 0.f);
       m[h] = m_new;
 #pragma unroll
