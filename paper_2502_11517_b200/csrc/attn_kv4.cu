@@ -421,7 +421,10 @@ attn_kv4_kernel(PoolView pv, TensorArgs a, const __nv_bfloat16 *__restrict__ q) 
   auto copy = [&](int t) {
     const int s = copied % L::STAGES;
     if (lane / PW == t) {
-      if (next_page < -1 || next_page >= pv.n_pages) { report(pv.status, PASTA_ERR_DEVICE_CHECK); next_page = next_meta = -1; }
+      if (next_meta < 0 ? next_page != -1 : next_page < 0 || next_page >= pv.n_pages) {
+        report(pv.status, PASTA_ERR_DEVICE_CHECK);
+        next_page = next_meta = -1;
+      }
       meta_s[s * PASTA_TILE_PAGES + warp * PW + lane % PW] = next_meta;
     }
     const uint8_t *head = pv.kv_base + (a.layer_begin + layer) * pv.layer_stride + static_cast<int64_t>(x.g) * L::BLOCK;
