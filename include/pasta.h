@@ -249,7 +249,7 @@ pasta_status_t pasta_step_positions(pasta_pool_t *pool, int32_t *out_pos, int32_
  * pasta_kv_append with rotary position embedding fused in: every new K vector is rotated by its token's
  * position id before it is stored (rotate-half form: element i pairs with element i + head_dim/2,
  * angle = position * theta^(-2i/head_dim), angles evaluated in double precision, result rounded to bf16);
- * V is copied unchanged.  theta > 1 (10000 for the usual base).
+ * V is copied unchanged.  theta > 1 and finite (10000 for the usual base), here and in every call below, else INVALID_ARG.
  */
 pasta_status_t pasta_kv_append_rope(pasta_pool_t *pool, int32_t layer_begin, int32_t layer_count,
                                     const void *k_new, const void *v_new, float theta, void *stream);

@@ -404,7 +404,8 @@ pasta_status_t pasta_kv_append_rope(pasta_pool_t *p, int32_t layer_begin, int32_
                                     const void *v_new, float theta, void *stream) {
   if (!p) return PASTA_ERR_INVALID_ARG;
   if (p->host_only || !p->plan_valid) return PASTA_ERR_BAD_STATE;
-  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers || !(theta > 1.f))
+  if (layer_begin < 0 || layer_count < 0 || layer_begin + layer_count > p->cfg.n_layers ||
+      !(theta > 1.f && theta < INFINITY))
     return PASTA_ERR_INVALID_ARG;
   const int32_t n_app = p->hdr.w[PH_N_APPEND];
   if (n_app == 0 || layer_count == 0) return PASTA_OK;
@@ -683,7 +684,7 @@ pasta_status_t pasta_kv_append_run(pasta_pool_t *p, int32_t req, int32_t thread,
 
 pasta_status_t pasta_kv_append_run_rope(pasta_pool_t *p, int32_t req, int32_t thread, int32_t m, int32_t layer_begin,
                                         int32_t layer_count, const void *k, const void *v, float theta, void *stream) {
-  if (!(theta > 1.f)) return PASTA_ERR_INVALID_ARG;
+  if (!(theta > 1.f && theta < INFINITY)) return PASTA_ERR_INVALID_ARG;
   return append_run_impl(p, req, thread, m, layer_begin, layer_count, k, v, theta, stream);
 }
 
