@@ -811,8 +811,13 @@ pasta_status_t pasta_kv_read_layers(pasta_pool_t *p, int32_t layer_begin, int32_
   if (!k_out || !v_out || misaligned(p, k_out, v_out)) return PASTA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const auto launch = p->pv.kv8 ? launch_kv8_read_run : p->pv.kv4 ? launch_kv4_read_run : launch_kv_read_run;
-  PASTA_CUDA(launch(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin, layer_count, tokens_stride(p, m),
-                    k_out, v_out, st, &p->launches));
+  constexpr int32_t kMostLayers = 65535;             // of one launch: the layers are the grid's second dimension
+  for (int32_t done = 0; done < layer_count; done += kMostLayers) {
+    const size_t at = size_t(done) * tokens_stride(p, m);
+    PASTA_CUDA(launch(p->pv, sm.pages.data() + start / PASTA_PAGE, start % PASTA_PAGE, m, layer_begin + done,
+                      std::min(kMostLayers, layer_count - done), tokens_stride(p, m), static_cast<uint16_t *>(k_out) + at,
+                      static_cast<uint16_t *>(v_out) + at, st, &p->launches));
+  }
   return PASTA_OK;
 }
 
