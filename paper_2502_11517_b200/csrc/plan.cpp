@@ -47,6 +47,120 @@ struct TUnit {
   int32_t treq, g, tile_begin, tile_end, row_base;
 };
 
+int32_t tiles_of(const TReq &t) { return (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES; }
+
+// What a plan says about who works on which tiles.
+struct Assignment {
+  std::vector<TUnit> tunits, dunits;          // assigned to CTAs in advance; handed out at run time
+  std::vector<int32_t> trange, drange, tcta;
+  int32_t t_rows = 0;
+};
+
+// 4-bit pools: what the t-requests' runs cost (one kv head of one layer, the same for all kv heads).
+struct Kv4Costs {
+  std::vector<double> sums, unit;             // from first[ti] on: a run's tiles, summed up from its first; a unit's beginning and end
+  std::vector<size_t> first;
+  double all = 0, units = 0, longest = 0;     // of all runs and kv heads; of one unit of every t-request; the longest run
+  double run(size_t ti, const std::vector<TReq> &treqs) const { return sums[first[ti] + tiles_of(treqs[ti])] + unit[ti]; }
+};
+
+void kv4_costs(const std::vector<TReq> &treqs, const std::vector<int32_t> &pmeta, const PlanLimits &lim, Kv4Costs *c) {
+  const int32_t G = lim.n_q_heads / lim.n_kv_heads;
+  c->sums.clear(); c->unit.clear(); c->first.clear();
+  c->all = c->units = c->longest = 0;
+  for (size_t ti = 0; ti < treqs.size(); ++ti) {
+    const TReq &t = treqs[ti];
+    const int32_t padded = (t.n_threads * G + 15) & ~15;
+    const double plain = kKv4Tile + (lim.capped ? kKv4CappedRow : kKv4TileRow) * padded;
+    double sum = 0;
+    c->first.push_back(c->sums.size());
+    c->sums.push_back(0);
+    for (int32_t k = 0; k < tiles_of(t); ++k) {
+      bool all = (k + 1) * PASTA_TILE_PAGES <= t.n_pages;
+      for (int32_t j = k * PASTA_TILE_PAGES; all && j < (k + 1) * PASTA_TILE_PAGES; ++j) all = pmeta[t.page_off + j] & PASTA_PMETA_ALL_VISIBLE;
+      c->sums.push_back(sum += all ? plain : plain * kKv4Masked);
+    }
+    c->unit.push_back(kKv4Unit + kKv4UnitRow * padded);
+    c->all += lim.n_kv_heads * (sum + c->unit[ti]);
+    c->units += c->unit[ti];
+    c->longest = std::max(c->longest, c->run(ti, treqs));
+  }
+}
+
+// Runs go to the pool whole, the longest first and all layers of one before the next, so that the short ones even out what CTAs and
+// units take, as long as none takes longer than a launch of that many layers in which every run is cut into shares.  Where some
+// do, they are cut, and only runs much shorter than a share are handed out behind them.  Measured, us, whole and cut: 64 requests of 1 to 9
+// threads 89 and 101 for one layer, 160 and 181 for two; 32 of them 80 and 61; 64 with capped scores 76 and 75, four layers 167 and 235;
+// 1 to 5 threads of head_dim 64 40 and 32, two layers 45 and 50.
+void kv4_whole_runs(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits &lim, int32_t grid, int32_t layers, std::vector<uint8_t> *whole) {
+  whole->assign(treqs.size(), 0);
+  if (lim.tail_percent <= 0) return;
+  const double launch = layers * (c.all / grid + c.units / treqs.size());
+  const double most = c.longest <= kKv4CutLoss * launch + kKv4Merge ? c.longest : kKv4Filling * launch;
+  for (size_t ti = 0; ti < treqs.size(); ++ti) (*whole)[ti] = c.run(ti, treqs) <= most;
+}
+
+// The units of a launch: the whole runs for the pool, the others cut into `shares` even shares in advance.
+void kv4_cut(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits &lim, const std::vector<uint8_t> &whole, int32_t grid,
+             int32_t shares, Assignment *a) {
+  const int32_t G = lim.n_q_heads / lim.n_kv_heads, H = lim.n_kv_heads;
+  a->tunits.clear(); a->dunits.clear(); a->tcta.clear();
+  a->trange.assign(treqs.size() * H * 2, 0);
+  a->drange.assign(treqs.size() * H * 2, 0);
+  a->t_rows = 0;
+  static thread_local std::vector<size_t> order;
+  order.resize(treqs.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = i;
+  std::stable_sort(order.begin(), order.end(), [&](size_t x, size_t y) { return c.run(x, treqs) - c.unit[x] > c.run(y, treqs) - c.unit[y]; });
+  double unassigned = 0, units = 0, left = 0;            // cost of what has no CTA; of the present CTA's share what it has left
+  int64_t runs = 0;
+  for (size_t ti = 0; ti < treqs.size(); ++ti)
+    for (int32_t g = 0; g < H && !whole[ti]; ++g) {
+      ++runs;
+      units += c.unit[ti];
+      unassigned += c.run(ti, treqs);
+    }
+  const double cut = runs ? units / runs : 0;            // about one more unit for every CTA
+  int32_t cta = -1;
+  for (const size_t ti : order) {
+    const int32_t n_tiles = tiles_of(treqs[ti]), rows = treqs[ti].n_threads * G;
+    const double *sums = &c.sums[c.first[ti]], unit = c.unit[ti];
+    for (int32_t g = 0; g < H; ++g) {
+      int32_t *tr = &a->trange[(ti * H + g) * 2], *dr = &a->drange[(ti * H + g) * 2];
+      tr[0] = static_cast<int32_t>(a->tunits.size());
+      dr[0] = static_cast<int32_t>(a->dunits.size());
+      if (whole[ti]) {
+        a->dunits.push_back(TUnit{static_cast<int32_t>(ti), g, 0, n_tiles, a->t_rows});
+        a->t_rows += rows;
+      }
+      for (int32_t begin = whole[ti] ? n_tiles : 0; begin < n_tiles;) {
+        // the next CTA takes an even share of what remains, unless what the present one has left is worth a unit
+        if (cta < 0 || (cta + 1 < shares && left < unit + 0.5 * (sums[begin + 1] - sums[begin]))) {
+          ++cta;
+          left = (unassigned + cut * (shares - cta - 1)) / (shares - cta);
+          a->tcta.push_back(static_cast<int32_t>(a->tunits.size()));
+          a->tcta.push_back(0);
+        }
+        int32_t end = n_tiles;
+        if (cta + 1 < shares) {
+          end = begin + 1;
+          while (end < n_tiles && 0.5 * (sums[end] + sums[end + 1]) - sums[begin] <= left - unit) ++end;
+        }
+        a->tunits.push_back(TUnit{static_cast<int32_t>(ti), g, begin, end, a->t_rows});
+        a->tcta.back() = static_cast<int32_t>(a->tunits.size());
+        a->t_rows += rows;
+        left -= unit + sums[end] - sums[begin];
+        unassigned = std::max(0., unassigned - (sums[end] - sums[begin]) - (end == n_tiles ? unit : 0.));
+        begin = end;
+      }
+      tr[1] = static_cast<int32_t>(a->tunits.size());
+      dr[1] = static_cast<int32_t>(a->dunits.size());
+    }
+  }
+  // every CTA of the grid takes part in handing out, also those that were assigned nothing
+  while (!a->dunits.empty() && static_cast<int32_t>(a->tcta.size() / 2) < grid) a->tcta.insert(a->tcta.end(), 2, static_cast<int32_t>(a->tunits.size()));
+}
+
 }  // namespace
 
 // the same step planned with every tile assigned in advance: what is left when the shared tail does not fit the
@@ -220,49 +334,33 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   }
 
   // ---- t-units: cut the sequence of (t-request, kv head) tile runs into one contiguous range per CTA
-  static thread_local std::vector<TUnit> tunits, dunits;
-  static thread_local std::vector<int32_t> trange, drange, tcta, unit_cta, tail;
+  static thread_local Assignment main;
+  std::vector<TUnit> &tunits = main.tunits, &dunits = main.dunits;
+  std::vector<int32_t> &trange = main.trange, &drange = main.drange, &tcta = main.tcta;
+  static thread_local std::vector<int32_t> unit_cta, tail;
   tunits.clear(); dunits.clear(); tcta.clear(); unit_cta.clear();
   trange.assign(treqs.size() * lim.n_kv_heads * 2, 0);
   drange.assign(treqs.size() * lim.n_kv_heads * 2, 0);
-  int32_t t_rows = 0;
+  int32_t &t_rows = main.t_rows;
+  t_rows = 0;
   bool whole_runs = false;
-  if (!treqs.empty()) {
-    int32_t grid = std::max(1, lim.grid);
-    if (lim.kv4) {
-      int32_t rows = 0;
-      for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
-      grid *= kv4_ctas_per_sm(rows);
-    }
-    // 4-bit pools: what a t-request's tiles cost, summed up from its first, and what all of them cost.
-    static thread_local std::vector<double> cost;
-    static thread_local std::vector<size_t> cost0;
-    cost.clear(); cost0.clear();
-    auto padded = [&](size_t ti) { return (treqs[ti].n_threads * G + 15) & ~15; };
-    auto unit_cost = [&](size_t ti) { return kKv4Unit + kKv4UnitRow * padded(ti); };
-    double all_cost = 0;
-    if (lim.kv4) {
-      for (size_t ti = 0; ti < treqs.size(); ++ti) {
-        const TReq &t = treqs[ti];
-        cost0.push_back(cost.size());
-        const int32_t n_tiles = (t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
-        const double plain = kKv4Tile + (lim.capped ? kKv4CappedRow : kKv4TileRow) * padded(ti);
-        double sum = 0;
-        cost.push_back(0);
-        for (int32_t k = 0; k < n_tiles; ++k) {
-          bool all = (k + 1) * PASTA_TILE_PAGES <= t.n_pages;
-          for (int32_t j = k * PASTA_TILE_PAGES; all && j < (k + 1) * PASTA_TILE_PAGES; ++j) all = pmeta[t.page_off + j] & PASTA_PMETA_ALL_VISIBLE;
-          cost.push_back(sum += all ? plain : plain * kKv4Masked);
-        }
-        all_cost += lim.n_kv_heads * (sum + unit_cost(ti));
-      }
-    }
+  if (lim.kv4 && !treqs.empty()) {
+    static thread_local Kv4Costs cost;
+    static thread_local std::vector<uint8_t> whole;
+    kv4_costs(treqs, pmeta, lim, &cost);
+    int32_t rows = 0;
+    for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
+    const int32_t grid = std::max(1, lim.grid) * kv4_ctas_per_sm(rows);
+    kv4_whole_runs(treqs, cost, lim, grid, lim.layers, &whole);
+    kv4_cut(treqs, cost, lim, whole, grid, grid, &main);
+  } else if (!treqs.empty()) {
+    const int32_t grid = std::max(1, lim.grid);
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
     // run time (equal tile counts do not finish at the same time: SMs differ in the bandwidth they get).  Only when
     // there is enough work for that to matter.
     int64_t all_tiles = 0;
     for (const TReq &t : treqs) all_tiles += int64_t(lim.n_kv_heads) * ((t.n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES);
-    const bool share_tail = !lim.kv4 && lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * grid;
+    const bool share_tail = lim.tail_percent > 0 && lim.tail_tiles > 0 && all_tiles >= 16LL * grid;
     // Runs of a few tiles go to the pool whole, every so often, until the pool holds its share of their tiles (`owed`
     // counts what they still owe it): a whole run is a unit anyway, so sharing it costs no extra cut and no extra
     // partial rows.  Long runs stay assigned: cutting their ends into short units cost more, in unit changes and
@@ -279,40 +377,16 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
       }
     }
-    // 4-bit pools: runs go to the pool whole, the longest first and all layers of one before the next, so that the short ones even out what
-    // CTAs and units take, as long as none takes longer than a launch (of as many layers as the pool's launches have at most) in
-    // which every run is cut into shares.  Where some do, they are cut, and only runs much shorter than a share are handed out behind
-    // them.  Measured, us, whole and cut: 64 requests of 1 to 9 threads 89 and 101 for one layer, 160 and 181 for two; 32 of them 80 and
-    // 61; 64 with capped scores 76 and 75, four layers 167 and 235; 1 to 5 threads of head_dim 64 40 and 32, two layers 45 and 50.
-    if (lim.kv4 && lim.tail_percent > 0 && !treqs.empty()) {
-      double units = 0, longest = 0;
-      auto run_cost = [&](size_t ti) { return cost[cost0[ti] + (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES] + unit_cost(ti); };
-      for (size_t ti = 0; ti < treqs.size(); ++ti) { units += unit_cost(ti); longest = std::max(longest, run_cost(ti)); }
-      const double launch = lim.layers * (all_cost / grid + units / treqs.size());
-      const double most = longest <= kKv4CutLoss * launch + kKv4Merge ? longest : kKv4Filling * launch;
-      for (size_t ti = 0; ti < treqs.size(); ++ti)
-        if (run_cost(ti) <= most)
-          std::fill_n(tail.begin() + ti * lim.n_kv_heads, lim.n_kv_heads, (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES);
-    }
     const double overhead = 1.0;
     const int32_t min_piece = 1;
-    double total = 0, unassigned = 0, left = 0;           // unassigned: cost of what has no CTA; left: of the present CTA's share
-    int32_t cta = -1;
-    int64_t runs = 0;
-    double units = 0;
+    double total = 0;
     for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t n_tiles = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
       for (int32_t g = 0; g < lim.n_kv_heads; ++g) {
         const int32_t kept = n_tiles - tail[ti * lim.n_kv_heads + g];
         if (kept > 0) total += kept + overhead;
-        if (kept > 0 && lim.kv4) {
-          ++runs;
-          units += unit_cost(ti);
-          unassigned += cost[cost0[ti] + kept] + unit_cost(ti);
-        }
       }
     }
-    const double cut = runs ? units / runs : 0;           // about one more unit for every CTA
     const double target = std::max(total, 1.0) / grid;
     double cum = 0;
     // A small step (one response, a few threads, a context of a few hundred tokens) is not cut at all when every run can
@@ -331,7 +405,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       }
       // (8-bit pools: whole runs go to CTAs of six warps, a third as many to an SM)
       const int32_t ctas = lim.even_cuts ? std::max(1, grid / 3) : grid;
-      whole_runs = !lim.kv4 && n_runs > 0 && n_runs <= ctas &&
+      whole_runs = n_runs > 0 && n_runs <= ctas &&
                    longest <= kept_tiles / ctas + (lim.even_cuts ? kEvenWholeSlackTiles : kWholeRunSlackTiles);
     }
     // One CTA per unit (no persistent ranges): a run is cut into equal pieces of at most `piece` tiles, long enough to
@@ -349,14 +423,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
       }
     }
     int32_t run_no = 0;
-    static thread_local std::vector<size_t> order;
-    order.resize(treqs.size());
-    for (size_t i = 0; i < order.size(); ++i) order[i] = i;
-    if (lim.kv4) {
-      auto cost_of = [&](size_t ti) { return cost[cost0[ti] + (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES]; };
-      std::stable_sort(order.begin(), order.end(), [&](size_t a, size_t b) { return cost_of(a) > cost_of(b); });
-    }
-    for (const size_t ti : order) {
+    for (size_t ti = 0; ti < treqs.size(); ++ti) {
       const int32_t all = (treqs[ti].n_pages + PASTA_TILE_PAGES - 1) / PASTA_TILE_PAGES;
       const int32_t rows = treqs[ti].n_threads * G;
       for (int32_t g = 0; g < lim.n_kv_heads; ++g) {
@@ -383,26 +450,6 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
             t_rows += rows;
             break;
           }
-          if (lim.kv4) {
-            const double *sums = &cost[cost0[ti]], unit = unit_cost(ti);
-            // the next CTA takes an even share of what remains, unless what the present one has left is worth a unit
-            if (cta < 0 || (cta + 1 < grid && left < unit + 0.5 * (sums[begin + 1] - sums[begin]))) {
-              ++cta;
-              left = (unassigned + cut * (grid - cta - 1)) / (grid - cta);
-            }
-            int32_t end = n_tiles;
-            if (cta + 1 < grid) {
-              end = begin + 1;
-              while (end < n_tiles && 0.5 * (sums[end] + sums[end + 1]) - sums[begin] <= left - unit) ++end;
-            }
-            tunits.push_back(TUnit{static_cast<int32_t>(ti), g, begin, end, t_rows});
-            unit_cta.push_back(cta);
-            t_rows += rows;
-            left -= unit + sums[end] - sums[begin];
-            unassigned = std::max(0., unassigned - (sums[end] - sums[begin]) - (end == n_tiles ? unit : 0.));
-            begin = end;
-            continue;
-          }
           int32_t c = std::min<int32_t>(grid - 1, static_cast<int32_t>(cum / target));
           if (c + 1 < grid && (c + 1) * target - cum < min_piece) ++c;   // too close to the CTA's end: next one
           int32_t take = remaining;
@@ -419,9 +466,8 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
         }
         trange[(ti * lim.n_kv_heads + g) * 2 + 1] = static_cast<int32_t>(tunits.size());
         drange[(ti * lim.n_kv_heads + g) * 2] = static_cast<int32_t>(dunits.size());
-        const int32_t piece2 = lim.kv4 ? all : lim.tail_tiles;
-        for (int32_t b2 = n_tiles; b2 < all; b2 += piece2) {
-          dunits.push_back(TUnit{static_cast<int32_t>(ti), g, b2, std::min(all, b2 + piece2), t_rows});
+        for (int32_t b2 = n_tiles; b2 < all; b2 += lim.tail_tiles) {
+          dunits.push_back(TUnit{static_cast<int32_t>(ti), g, b2, std::min(all, b2 + lim.tail_tiles), t_rows});
           t_rows += rows;
         }
         drange[(ti * lim.n_kv_heads + g) * 2 + 1] = static_cast<int32_t>(dunits.size());
