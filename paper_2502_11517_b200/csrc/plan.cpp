@@ -161,6 +161,23 @@ void kv4_cut(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits
   while (!a->dunits.empty() && static_cast<int32_t>(a->tcta.size() / 2) < grid) a->tcta.insert(a->tcta.end(), 2, static_cast<int32_t>(a->tunits.size()));
 }
 
+// The same within `max_rows` partial rows (whole runs have theirs counted, too): every cut costs a t-request's rows, so with less room runs are
+// cut into fewer shares, and not at all once shares would be fewer than runs (a CTA per run then does more than a CTA per share).
+void kv4_assign(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits &lim, std::vector<uint8_t> whole, int32_t grid, int64_t max_rows,
+                Assignment *a) {
+  int64_t runs = 0;
+  for (size_t ti = 0; ti < treqs.size(); ++ti) runs += whole[ti] ? 0 : lim.n_kv_heads;
+  for (int32_t shares = grid;;) {
+    kv4_cut(treqs, c, lim, whole, grid, shares, a);
+    if (a->t_rows <= max_rows || runs == 0) return;
+    shares = static_cast<int32_t>(std::min<int64_t>(shares - 1, shares * std::max<int64_t>(0, max_rows) / a->t_rows));
+    if (shares < runs) {
+      std::fill(whole.begin(), whole.end(), 1);
+      runs = 0;
+    }
+  }
+}
+
 }  // namespace
 
 // the same step planned with every tile assigned in advance: what is left when the shared tail does not fit the
@@ -352,7 +369,8 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
     const int32_t grid = std::max(1, lim.grid) * kv4_ctas_per_sm(rows);
     kv4_whole_runs(treqs, cost, lim, grid, lim.layers, &whole);
-    kv4_cut(treqs, cost, lim, whole, grid, grid, &main);
+    // (pieces of the warp path take a set of rows each, at least)
+    kv4_assign(treqs, cost, lim, whole, grid, lim.max_rows - static_cast<int64_t>(wpieces.size()) * lim.n_kv_heads * G, &main);
   } else if (!treqs.empty()) {
     const int32_t grid = std::max(1, lim.grid);
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
@@ -503,7 +521,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     n_wunits = 0;
     for (int32_t i = 0; i < n; ++i) n_wunits += static_cast<int64_t>(q_nw[i]) * lim.n_kv_heads;
     if (t_rows + n_wunits * G <= lim.max_rows) break;
-    // the shared tail costs rows: do without (whole runs, as 4-bit pools hand out, cost none)
+    // the shared tail costs rows: do without (4-bit pools hand out whole runs only, which would take as many if they were assigned)
     if (!dunits.empty() && !lim.kv4) return without_tail(pool, entries, slots, lim, out);
     if (chunk >= (1 << 24)) return PASTA_ERR_CAPACITY;
     chunk *= 2;
