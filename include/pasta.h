@@ -144,7 +144,9 @@ typedef struct {
   int32_t max_segments_per_thread;  /* longest segment list of one thread */
   int32_t max_step_queries;         /* most queries in one step (one per entry, or per new token); 0 = max_requests * 17 */
   int32_t max_partial_rows;         /* split/segment partial results per layer; 0 = derived from max_step_queries */
-  int32_t max_layers_per_launch;    /* layers whose partials fit the workspace at once; 0 = min(n_layers, 8) */
+  int32_t max_layers_per_launch;    /* layers whose partials fit the workspace at once; 0 = min(n_layers, 8).  (On a 4-bit pool a step is
+                                       planned for launches of that many layers and, where those want their runs cut otherwise, for
+                                       launches of one.) */
   int32_t flags;                    /* PASTA_FLAG_* */
   int32_t device;                   /* CUDA device ordinal the pool lives on */
   void *kv_base;                    /* device; pasta_kv_bytes() bytes, 1024-byte aligned, allocated and freed by the caller */

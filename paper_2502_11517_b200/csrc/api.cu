@@ -65,6 +65,8 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                  PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
                  2 * parts * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
                  PU_WORDS * tail_units + 2 * n_treq * c.n_kv_heads + 8;
+  if (int4)                       // a second assignment: header, ranges, units, CTAs
+    d->max_words += PH_WORDS + 4 * n_treq * c.n_kv_heads + PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PU_WORDS * tail_units + 32;
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
   const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0, kv4 = (c.flags & PASTA_FLAG_KV_INT4) != 0;
   if (kv8 && kv4) return PASTA_ERR_INVALID_ARG;
@@ -101,7 +103,7 @@ struct pasta_pool {
   std::vector<StepQuery> queries;   // of the step planned last, in entry order
   std::vector<Slot> slots;          // parallel to queries
   std::vector<int32_t> plan;
-  PlanHeader hdr{};
+  PlanHeader hdr{}, hdr_few{};          // of the step; for launches of fewer than hdr.w[PH_FEWEST_LAYERS] layers
   bool plan_valid = false;
   int64_t launches = 0;
   // the plan of step i is uploaded on a stream of its own into buffer i % 2 while step i - 1 still runs
@@ -209,6 +211,8 @@ cudaError_t append_codes(pasta_pool *p, const int32_t *slots, const int32_t *pos
   const auto launch = p->pv.kv8 ? launch_kv8_append : launch_kv4_append;
   return launch(p->pv, slots, pos, n_tok, layer_begin, layer_count, in_layer_stride, k, v, form, st);
 }
+// the plan of a launch of this many layers
+const PlanHeader &header_for(const pasta_pool *p, int32_t layers) { return layers < p->hdr.w[PH_FEWEST_LAYERS] ? p->hdr_few : p->hdr; }
 // elements between the layers of a dense [layers, n, n_kv_heads, head_dim] array
 int64_t tokens_stride(const pasta_pool *p, int64_t n) { return n * p->cfg.n_kv_heads * p->cfg.head_dim; }
 
@@ -239,13 +243,14 @@ PlanLimits limits_of(const pasta_pool *p) {
 }  // namespace
 
 namespace pasta {
-// for entry points that live in other files
+// for entry points that live in other files, which launch one layer
 bool pool_step_view(pasta_pool_t *p, PoolView *pv, PlanHeader *hdr, int32_t *n_layers, int32_t *head_dim,
                     int32_t *device) {
   if (p->host_only || !p->plan_valid) return false;
   if (p->cfg.flags & PASTA_FLAG_OUT_BF16) return false;      // that entry point writes fp32 only
   *pv = p->pv;
-  *hdr = p->hdr;
+  *hdr = header_for(p, 1);
+  if (hdr->w[PH_ROWS] > PASTA_NOALLOC_MAX_ROWS) *hdr = p->hdr;      // (fewer cuts, perhaps)
   *n_layers = p->cfg.n_layers;
   *head_dim = p->cfg.head_dim;
   *device = p->cfg.device;
@@ -521,6 +526,7 @@ pasta_status_t pasta_step_begin(pasta_pool_t *p, int32_t n, const int32_t *req_i
     return s;
   }
   std::memcpy(p->hdr.w, p->plan.data(), sizeof(p->hdr.w));
+  if (p->hdr.w[PH_FEWEST_LAYERS]) std::memcpy(p->hdr_few.w, p->plan.data() + p->hdr.w[PH_OFF_FEW], sizeof(p->hdr_few.w));
   if (!p->host_only) {
     // Buffer b = i % 2 was last read by the kernels of step i - 2.  Everything the caller had enqueued when step
     // i - 1 began (that is, up to step i - 2) is covered by work_mark[(i - 1) % 2]; the upload waits for that mark
@@ -595,21 +601,22 @@ pasta_status_t pasta_decode_attn(pasta_pool_t *p, int32_t layer_begin, int32_t l
     const bool timed = p->profiling && p->prof_calls < kProfCalls && (p->prof_seen++ % p->prof_stride) == 0;
     cudaEvent_t *ev = timed ? &p->prof_events[4 * p->prof_calls] : nullptr;
     uint8_t mask = 0;
+    const PlanHeader &hdr = header_for(p, cnt);
     if (timed) PASTA_CUDA(cudaEventRecord(ev[0], st));
-    if (p->hdr.w[PH_N_TUNITS] + p->hdr.w[PH_N_DUNITS] > 0) {
-      PASTA_CUDA(launch_attn_units(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
+    if (hdr.w[PH_N_TUNITS] + hdr.w[PH_N_DUNITS] > 0) {
+      PASTA_CUDA(launch_attn_units(p->pv, hdr, layer_begin + done, cnt, qg, sc, og, lg, out_bf16, st));
       p->launches += 1;
       mask |= 1;
     }
     if (timed) PASTA_CUDA(cudaEventRecord(ev[1], st));
-    if (p->hdr.w[PH_N_WUNITS] > 0) {
-      PASTA_CUDA(launch_attn_warp(p->pv, p->hdr, layer_begin + done, cnt, qg, sc, st));
+    if (hdr.w[PH_N_WUNITS] > 0) {
+      PASTA_CUDA(launch_attn_warp(p->pv, hdr, layer_begin + done, cnt, qg, sc, st));
       p->launches += 1;
       mask |= 2;
     }
     if (timed) PASTA_CUDA(cudaEventRecord(ev[2], st));
-    if (plan_needs_merge(p->hdr, p->pv.kv4)) {
-      PASTA_CUDA(launch_merge(p->pv, p->hdr, cnt, og, lg, st, out_bf16));
+    if (plan_needs_merge(hdr, p->pv.kv4)) {
+      PASTA_CUDA(launch_merge(p->pv, hdr, cnt, og, lg, st, out_bf16));
       p->launches += 1;
       mask |= 4;
     }

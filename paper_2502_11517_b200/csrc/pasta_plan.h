@@ -76,6 +76,8 @@ enum {
   PH_N_PARTIAL,       // units that leave partial rows for the merge: t-units and d-units that are not final, and all w-units
   PH_T_MAX_ROWS,      // most stacked rows (threads * group) of any t-request
   PH_WHOLE_RUNS,      // 1: a small step, every run is one unit
+  PH_FEWEST_LAYERS,   // (4-bit pools) launches of fewer layers than this go by the header at PH_OFF_FEW; 0: there is none
+  PH_OFF_FEW,         // a second header: same step, same tables but for the assignment (units, CTAs, ranges, rows)
   PH_WORDS = 32
 };
 

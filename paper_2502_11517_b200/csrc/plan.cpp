@@ -99,6 +99,21 @@ void kv4_whole_runs(const std::vector<TReq> &treqs, const Kv4Costs &c, const Pla
   const double most = c.longest <= kKv4CutLoss * launch + kKv4Merge ? c.longest : kKv4Filling * launch;
   for (size_t ti = 0; ti < treqs.size(); ++ti) (*whole)[ti] = c.run(ti, treqs) <= most;
 }
+// Launches of `layers` layers and of one, where they differ: `one` receives the whole runs of the latter.  Returns the fewest layers that get what
+// `layers` do (more layers never make fewer runs whole), 1 where one layer does.
+int32_t kv4_fewest_layers(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits &lim, int32_t grid, int32_t layers,
+                          const std::vector<uint8_t> &whole, std::vector<uint8_t> *one) {
+  kv4_whole_runs(treqs, c, lim, grid, 1, one);
+  if (*one == whole) return 1;
+  static thread_local std::vector<uint8_t> some;
+  int32_t no = 1, yes = layers;
+  while (yes - no > 1) {
+    const int32_t n = no + (yes - no) / 2;
+    kv4_whole_runs(treqs, c, lim, grid, n, &some);
+    (some == whole ? yes : no) = n;
+  }
+  return yes;
+}
 
 // The units of a launch: the whole runs for the pool, the others cut into `shares` even shares in advance.
 void kv4_cut(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits &lim, const std::vector<uint8_t> &whole, int32_t grid,
@@ -351,7 +366,8 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   }
 
   // ---- t-units: cut the sequence of (t-request, kv head) tile runs into one contiguous range per CTA
-  static thread_local Assignment main;
+  static thread_local Assignment main, few;              // few: for launches of fewer than `fewest` layers (4-bit pools)
+  int32_t fewest = 0;
   std::vector<TUnit> &tunits = main.tunits, &dunits = main.dunits;
   std::vector<int32_t> &trange = main.trange, &drange = main.drange, &tcta = main.tcta;
   static thread_local std::vector<int32_t> unit_cta, tail;
@@ -369,8 +385,15 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
     const int32_t grid = std::max(1, lim.grid) * kv4_ctas_per_sm(rows);
     kv4_whole_runs(treqs, cost, lim, grid, lim.layers, &whole);
-    // (pieces of the warp path take a set of rows each, at least)
-    kv4_assign(treqs, cost, lim, whole, grid, lim.max_rows - static_cast<int64_t>(wpieces.size()) * lim.n_kv_heads * G, &main);
+    const int64_t most_rows = lim.max_rows - static_cast<int64_t>(wpieces.size()) * lim.n_kv_heads * G;      // (pieces of the warp path take a set each, at least)
+    kv4_assign(treqs, cost, lim, whole, grid, most_rows, &main);
+    // A step's plan serves calls of one layer and of all.  Where a launch of few layers wants its runs cut otherwise, it has tables of its own.
+    static thread_local std::vector<uint8_t> one;
+    const int32_t n = kv4_fewest_layers(treqs, cost, lim, grid, lim.layers, whole, &one);
+    if (n > 1) {
+      fewest = n;
+      kv4_assign(treqs, cost, lim, one, grid, most_rows, &few);
+    }
   } else if (!treqs.empty()) {
     const int32_t grid = std::max(1, lim.grid);
     // Some of the work is kept back from the assignment below, as units which the CTAs share out among themselves at
@@ -520,7 +543,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     for (const WPiece &w : wpieces) q_nw[w.query] += (w.vis + chunk - 1) / chunk;
     n_wunits = 0;
     for (int32_t i = 0; i < n; ++i) n_wunits += static_cast<int64_t>(q_nw[i]) * lim.n_kv_heads;
-    if (t_rows + n_wunits * G <= lim.max_rows) break;
+    if (std::max(t_rows, fewest ? few.t_rows : 0) + n_wunits * G <= lim.max_rows) break;
     // the shared tail costs rows: do without (4-bit pools hand out whole runs only, which would take as many if they were assigned)
     if (!dunits.empty() && !lim.kv4) return without_tail(pool, entries, slots, lim, out);
     if (chunk >= (1 << 24)) return PASTA_ERR_CAPACITY;
@@ -563,7 +586,7 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     while (w.size() % 4) w.push_back(0);   // keep every table 16-byte aligned
   };
   static thread_local std::vector<int32_t> app, apos, qpos, qtab, ttab, utab, dtab;
-  app.clear(); apos.clear(); qpos.clear(); ttab.clear(); utab.clear(); dtab.clear();
+  app.clear(); apos.clear(); qpos.clear(); ttab.clear();
   for (int32_t i = 0; i < n; ++i) {
     const int32_t pos = slots[i].pos;
     qpos.push_back(pos);
@@ -591,30 +614,37 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
                                    t.n_threads, t.n_streams, t.vis_off, t.tq_off, final_rows ? 1 : 0};
     tab.insert(tab.end(), rec, rec + PU_WORDS);
   };
-  for (const TUnit &u : tunits) unit_record(u, utab);
-  for (const TUnit &u : dunits) unit_record(u, dtab);
-  int32_t n_partial = static_cast<int32_t>(n_wunits);
-  for (size_t i = PU_FINAL; i < utab.size(); i += PU_WORDS) n_partial += utab[i] == 0;
-  for (size_t i = PU_FINAL; i < dtab.size(); i += PU_WORDS) n_partial += dtab[i] == 0;
   w[PH_MAGIC] = PASTA_PLAN_MAGIC;
-  w[PH_N_DUNITS] = static_cast<int32_t>(dunits.size());
-  w[PH_N_PARTIAL] = n_partial;
   w[PH_WHOLE_RUNS] = whole_runs ? 1 : 0;
   for (const TReq &t : treqs) w[PH_T_MAX_ROWS] = std::max(w[PH_T_MAX_ROWS], t.n_threads * G);
   w[PH_N_QUERIES] = n;
   w[PH_N_APPEND] = n_app;
   w[PH_N_TREQ] = static_cast<int32_t>(treqs.size());
-  w[PH_N_TUNITS] = static_cast<int32_t>(tunits.size());
   w[PH_N_WUNITS] = static_cast<int32_t>(n_wunits);
-  w[PH_T_ROWS] = t_rows;
-  w[PH_ROWS] = t_rows + static_cast<int32_t>(n_wunits) * G;
-  w[PH_T_GRID] = static_cast<int32_t>(tcta.size() / 2);
   put(PH_OFF_APPEND, app);
   put(PH_OFF_QUERY, qtab);
   put(PH_OFF_TREQ, ttab);
-  put(PH_OFF_TRANGE, trange);
-  put(PH_OFF_TUNIT, utab);
-  put(PH_OFF_TCTA, tcta);
+  // an assignment's tables, and what the header says of it
+  auto put_assignment = [&](const Assignment &a) {
+    utab.clear(); dtab.clear();
+    for (const TUnit &u : a.tunits) unit_record(u, utab);
+    for (const TUnit &u : a.dunits) unit_record(u, dtab);
+    int32_t n_partial = static_cast<int32_t>(n_wunits);
+    for (size_t i = PU_FINAL; i < utab.size(); i += PU_WORDS) n_partial += utab[i] == 0;
+    for (size_t i = PU_FINAL; i < dtab.size(); i += PU_WORDS) n_partial += dtab[i] == 0;
+    w[PH_N_TUNITS] = static_cast<int32_t>(a.tunits.size());
+    w[PH_N_DUNITS] = static_cast<int32_t>(a.dunits.size());
+    w[PH_N_PARTIAL] = n_partial;
+    w[PH_T_ROWS] = a.t_rows;
+    w[PH_ROWS] = a.t_rows + static_cast<int32_t>(n_wunits) * G;
+    w[PH_T_GRID] = static_cast<int32_t>(a.tcta.size() / 2);
+    put(PH_OFF_TRANGE, a.trange);
+    put(PH_OFF_TUNIT, utab);
+    put(PH_OFF_TCTA, a.tcta);
+    put(PH_OFF_DUNIT, dtab);
+    put(PH_OFF_DRANGE, a.drange);
+  };
+  put_assignment(main);
   put(PH_OFF_WUNIT, wunits);
   put(PH_OFF_PAGES, pages);
   put(PH_OFF_PMETA, pmeta);
@@ -622,9 +652,16 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   put(PH_OFF_TQ, tq_tab);
   put(PH_OFF_APOS, apos);
   put(PH_OFF_QPOS, qpos);
-  put(PH_OFF_DUNIT, dtab);
-  put(PH_OFF_DRANGE, drange);
   w[PH_TOTAL_WORDS] = static_cast<int32_t>(w.size());
+  if (fewest) {
+    const std::vector<int32_t> header(w.begin(), w.begin() + PH_WORDS);
+    put_assignment(few);
+    std::vector<int32_t> second(w.begin(), w.begin() + PH_WORDS);
+    std::copy(header.begin(), header.end(), w.begin());
+    second[PH_TOTAL_WORDS] = w[PH_TOTAL_WORDS] = static_cast<int32_t>(w.size()) + PH_WORDS;
+    w[PH_FEWEST_LAYERS] = fewest;
+    put(PH_OFF_FEW, second);
+  }
   if (static_cast<int64_t>(w.size()) > lim.max_words) {
     if (!dunits.empty()) return without_tail(pool, entries, slots, lim, out);
     return PASTA_ERR_CAPACITY;
