@@ -65,8 +65,8 @@ pasta_status_t derive(const pasta_pool_config_t &c, Derived *d) {
                  PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PW_WORDS * (int64_t(d->max_rows) / d->group + 1) +
                  2 * parts * int64_t(c.n_pages) + nq * std::min(PASTA_MAX_STREAMS, c.max_threads_per_request) + nq + 64 +
                  PU_WORDS * tail_units + 2 * n_treq * c.n_kv_heads + 8;
-  if (int4)                       // a second assignment: header, ranges, units, CTAs
-    d->max_words += PH_WORDS + 4 * n_treq * c.n_kv_heads + PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PU_WORDS * tail_units + 32;
+  if (int4)                       // two more assignments: header, ranges, units, CTAs
+    d->max_words += 2 * (PH_WORDS + 4 * n_treq * c.n_kv_heads + PU_WORDS * (n_treq * c.n_kv_heads + slots) + 2 * slots + PU_WORDS * tail_units + 32);
   d->staging_words = std::max<int64_t>(d->max_words, 2 * kRunChunk);
   const bool kv8 = (c.flags & PASTA_FLAG_KV_FP8) != 0, kv4 = (c.flags & PASTA_FLAG_KV_INT4) != 0;
   if (kv8 && kv4) return PASTA_ERR_INVALID_ARG;
@@ -103,7 +103,7 @@ struct pasta_pool {
   std::vector<StepQuery> queries;   // of the step planned last, in entry order
   std::vector<Slot> slots;          // parallel to queries
   std::vector<int32_t> plan;
-  PlanHeader hdr{}, hdr_few{};          // of the step; for launches of fewer than hdr.w[PH_FEWEST_LAYERS] layers
+  PlanHeader hdr{}, hdr_few{}, hdr_noalloc{};          // of the step; for launches of fewer than hdr.w[PH_FEWEST_LAYERS] layers; without workspace
   bool plan_valid = false;
   int64_t launches = 0;
   // the plan of step i is uploaded on a stream of its own into buffer i % 2 while step i - 1 still runs
@@ -237,20 +237,20 @@ PlanLimits limits_of(const pasta_pool *p) {
   l.kv4 = (p->cfg.flags & PASTA_FLAG_KV_INT4) != 0;
   l.capped = p->pv.softcap_log2 > 0.f;
   l.layers = p->d.layers_per_launch;
+  if (!(p->cfg.flags & PASTA_FLAG_OUT_BF16)) l.noalloc_rows = PASTA_NOALLOC_MAX_ROWS;      // (that call writes fp32 only)
   return l;
 }
 
 }  // namespace
 
 namespace pasta {
-// for entry points that live in other files, which launch one layer
+// for pasta_decode_attn_noalloc, which lives in another file
 bool pool_step_view(pasta_pool_t *p, PoolView *pv, PlanHeader *hdr, int32_t *n_layers, int32_t *head_dim,
                     int32_t *device) {
   if (p->host_only || !p->plan_valid) return false;
   if (p->cfg.flags & PASTA_FLAG_OUT_BF16) return false;      // that entry point writes fp32 only
   *pv = p->pv;
-  *hdr = header_for(p, 1);
-  if (hdr->w[PH_ROWS] > PASTA_NOALLOC_MAX_ROWS) *hdr = p->hdr;      // (fewer cuts, perhaps)
+  *hdr = p->hdr.w[PH_OFF_NOALLOC] ? p->hdr_noalloc : header_for(p, 1);
   *n_layers = p->cfg.n_layers;
   *head_dim = p->cfg.head_dim;
   *device = p->cfg.device;
@@ -526,7 +526,8 @@ pasta_status_t pasta_step_begin(pasta_pool_t *p, int32_t n, const int32_t *req_i
     return s;
   }
   std::memcpy(p->hdr.w, p->plan.data(), sizeof(p->hdr.w));
-  if (p->hdr.w[PH_FEWEST_LAYERS]) std::memcpy(p->hdr_few.w, p->plan.data() + p->hdr.w[PH_OFF_FEW], sizeof(p->hdr_few.w));
+  if (p->hdr.w[PH_OFF_FEW]) std::memcpy(p->hdr_few.w, p->plan.data() + p->hdr.w[PH_OFF_FEW], sizeof(p->hdr_few.w));
+  if (p->hdr.w[PH_OFF_NOALLOC]) std::memcpy(p->hdr_noalloc.w, p->plan.data() + p->hdr.w[PH_OFF_NOALLOC], sizeof(p->hdr_noalloc.w));
   if (!p->host_only) {
     // Buffer b = i % 2 was last read by the kernels of step i - 2.  Everything the caller had enqueued when step
     // i - 1 began (that is, up to step i - 2) is covered by work_mark[(i - 1) % 2]; the upload waits for that mark

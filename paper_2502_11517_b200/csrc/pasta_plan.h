@@ -78,6 +78,7 @@ enum {
   PH_WHOLE_RUNS,      // 1: a small step, every run is one unit
   PH_FEWEST_LAYERS,   // (4-bit pools) launches of fewer layers than this go by the header at PH_OFF_FEW; 0: there is none
   PH_OFF_FEW,         // a second header: same step, same tables but for the assignment (units, CTAs, ranges, rows)
+  PH_OFF_NOALLOC,     // the same for pasta_decode_attn_noalloc, where the assignment for one layer has too many partial rows for it; 0: none
   PH_WORDS = 32
 };
 

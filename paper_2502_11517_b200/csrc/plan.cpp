@@ -366,8 +366,12 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   }
 
   // ---- t-units: cut the sequence of (t-request, kv head) tile runs into one contiguous range per CTA
-  static thread_local Assignment main, few;              // few: for launches of fewer than `fewest` layers (4-bit pools)
-  int32_t fewest = 0;
+  // 4-bit pools: few is for launches of fewer than `fewest` layers, tight for the one layer of a call that has noalloc_rows partial rows
+  static thread_local Assignment main, few, tight;
+  int32_t fewest = 0, kv4_grid = 0;
+  bool has_tight = false;
+  static thread_local Kv4Costs cost;
+  static thread_local std::vector<uint8_t> whole, one;
   std::vector<TUnit> &tunits = main.tunits, &dunits = main.dunits;
   std::vector<int32_t> &trange = main.trange, &drange = main.drange, &tcta = main.tcta;
   static thread_local std::vector<int32_t> unit_cta, tail;
@@ -378,17 +382,14 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   t_rows = 0;
   bool whole_runs = false;
   if (lim.kv4 && !treqs.empty()) {
-    static thread_local Kv4Costs cost;
-    static thread_local std::vector<uint8_t> whole;
     kv4_costs(treqs, pmeta, lim, &cost);
     int32_t rows = 0;
     for (const TReq &t : treqs) rows = std::max(rows, t.n_threads * G);
-    const int32_t grid = std::max(1, lim.grid) * kv4_ctas_per_sm(rows);
+    const int32_t grid = kv4_grid = std::max(1, lim.grid) * kv4_ctas_per_sm(rows);
     kv4_whole_runs(treqs, cost, lim, grid, lim.layers, &whole);
     const int64_t most_rows = lim.max_rows - static_cast<int64_t>(wpieces.size()) * lim.n_kv_heads * G;      // (pieces of the warp path take a set each, at least)
     kv4_assign(treqs, cost, lim, whole, grid, most_rows, &main);
     // A step's plan serves calls of one layer and of all.  Where a launch of few layers wants its runs cut otherwise, it has tables of its own.
-    static thread_local std::vector<uint8_t> one;
     const int32_t n = kv4_fewest_layers(treqs, cost, lim, grid, lim.layers, whole, &one);
     if (n > 1) {
       fewest = n;
@@ -549,6 +550,10 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
     if (chunk >= (1 << 24)) return PASTA_ERR_CAPACITY;
     chunk *= 2;
   }
+  if (kv4_grid && (fewest ? few : main).t_rows + n_wunits * G > lim.noalloc_rows) {
+    kv4_assign(treqs, cost, lim, one, kv4_grid, lim.noalloc_rows - n_wunits * G, &tight);
+    has_tight = tight.t_rows + n_wunits * G <= lim.noalloc_rows;
+  }
   {
     int32_t w0 = 0;
     for (int32_t i = 0; i < n; ++i) { q_w0[i] = w0; w0 += q_nw[i] * lim.n_kv_heads; }
@@ -653,15 +658,21 @@ pasta_status_t build_plan(const HostPool &pool, const std::vector<StepQuery> &en
   put(PH_OFF_APOS, apos);
   put(PH_OFF_QPOS, qpos);
   w[PH_TOTAL_WORDS] = static_cast<int32_t>(w.size());
-  if (fewest) {
-    const std::vector<int32_t> header(w.begin(), w.begin() + PH_WORDS);
-    put_assignment(few);
-    std::vector<int32_t> second(w.begin(), w.begin() + PH_WORDS);
-    std::copy(header.begin(), header.end(), w.begin());
-    second[PH_TOTAL_WORDS] = w[PH_TOTAL_WORDS] = static_cast<int32_t>(w.size()) + PH_WORDS;
-    w[PH_FEWEST_LAYERS] = fewest;
-    put(PH_OFF_FEW, second);
-  }
+  // further headers, each behind its tables
+  auto put_header = [&](int off_field, const Assignment &a) {
+    const std::vector<int32_t> first(w.begin(), w.begin() + PH_WORDS);
+    put_assignment(a);
+    std::vector<int32_t> header(w.begin(), w.begin() + PH_WORDS);
+    header[PH_FEWEST_LAYERS] = header[PH_OFF_FEW] = header[PH_OFF_NOALLOC] = 0;
+    std::copy(first.begin(), first.end(), w.begin());
+    put(off_field, header);
+    w[PH_TOTAL_WORDS] = static_cast<int32_t>(w.size());
+  };
+  if (fewest) put_header(PH_OFF_FEW, few);
+  if (has_tight) put_header(PH_OFF_NOALLOC, tight);
+  w[PH_FEWEST_LAYERS] = fewest;
+  for (const int off : {PH_OFF_FEW, PH_OFF_NOALLOC})
+    if (w[off]) w[w[off] + PH_TOTAL_WORDS] = w[PH_TOTAL_WORDS];
   if (static_cast<int64_t>(w.size()) > lim.max_words) {
     if (!dunits.empty()) return without_tail(pool, entries, slots, lim, out);
     return PASTA_ERR_CAPACITY;

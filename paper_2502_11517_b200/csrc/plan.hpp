@@ -19,6 +19,7 @@ struct PlanLimits {
   bool kv4 = false;      // 4-bit pool: `grid` is multiplied by kv4_ctas_per_sm of the step's rows
   bool capped = false;      // scores are capped
   int32_t layers = 1;       // layers of a launch, at most
+  int32_t noalloc_rows = INT32_MAX;       // partial rows of a call that brings its own (one layer); 4-bit pools get an assignment that fits
   bool even_cuts = false;   // t-units are launched one per CTA (8-bit pools): runs are cut into pieces of one length
 };
 
