@@ -158,8 +158,12 @@ void kv4_cut(const std::vector<TReq> &treqs, const Kv4Costs &c, const PlanLimits
         }
         int32_t end = n_tiles;
         if (cta + 1 < shares) {
-          end = begin + 1;
-          while (end < n_tiles && 0.5 * (sums[end] + sums[end + 1]) - sums[begin] <= left - unit) ++end;
+          end = begin + 1;                       // a tile more as long as half of it fits (searched for by halves: sums grow)
+          for (int32_t past = n_tiles; end < past;) {
+            const int32_t mid = end + (past - end) / 2;
+            if (0.5 * (sums[mid] + sums[mid + 1]) - sums[begin] <= left - unit) end = mid + 1;
+            else past = mid;
+          }
         }
         a->tunits.push_back(TUnit{static_cast<int32_t>(ti), g, begin, end, a->t_rows});
         a->tcta.back() = static_cast<int32_t>(a->tunits.size());
