@@ -101,7 +101,7 @@ enum {
  * Requests of up to 640 stacked rows (queries of the step x group; 512 with head_dim 64) and 4095 streams run on tensor cores: queries,
  * and K and V as held, enter unrounded, a softmax weight as bf16 (2^-8 of itself; the weights' sum is that of the rounded ones), sums
  * are fp32.  Values of any size that is held are summed without leaving the range of fp32, except that products of weight and value below
- * 2^-149 are lost, which is at most 2^-36 of a row's largest element for every token.  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the
+ * 2^-149 are lost, which is at most 2^-24 of a row's largest element for every token (values of 2^-110; larger ones lose less).  PASTA_FLAG_NO_TENSOR_PATH and larger requests take the
  * warp-shuffle kernel, which rounds no weight, and whose sums hold 2^14 times the largest value.
  */
 

@@ -22,9 +22,9 @@
 // scheduler: some 1800, of which K's codes, V's codes and the softmax are 1000), against the 785 cycles that its 18 KB take at the
 // measured copy bandwidth.  A warp alone issues one every seven cycles, and a tile is a chain (codes, MMA, codes and softmax, MMA), so
 // CTAs share an SM and fill one another's gaps: four of 128 threads and 128 TMEM columns for up to 32 rows, two of 256 threads and
-// 256 columns for up to 80 (64 at head_dim 64); requests with more rows are split by the planner.  Schedulers issue in 53 % of the cycles; a tile takes 2500
-// (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 151 us (39 us for the bytes alone), 8 prefixes of
-// 32768 tokens and 68 rows 232 us (52), 64 capped short responses 157 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
+// 256 columns for up to 80 (64 at head_dim 64); requests with more rows are split by the planner.  Schedulers issue in 55 % of the cycles; a tile takes 2500
+// (68 rows) to 1700 (20 rows) cycles of an SM.  Measured: 64 requests of 4 to 36 rows 155 us (39 us for the bytes alone), 8 prefixes of
+// 32768 tokens and 68 rows 239 us (52), 64 capped short responses 159 us (24), 32 requests of 2 to 10 rows at head_dim 64 46 us (7).
 // Built and measured slower: roles on warps of their own and one CTA to an SM, in three forms (290 to 390 us for the first, 310 to 410
 // for the second: hand-overs and four programs' instruction fetches); twice the threads per CTA at 64 registers (302 and 418); bulk
 // copies in place of 16-byte ones (192 and 277 for 191 and 274 then); one body for the chunks of the softmax instead of one for
@@ -58,8 +58,10 @@ namespace {
 constexpr float R_SLACK = 10.f;                  // weights are at most 2^10 (bf16 and fp32 keep their precision at any size)
 constexpr float R_FAR = 16777216.f;              // 2^24: beyond it a score and its rounding differ by whole powers of two
 constexpr float R_UNSET = 3e38f;                 // minus the reference of a row that has seen nothing (careful units)
-constexpr float O_PART = 0x1p118f, O_TINY = 0x1p-110f;       // sums of weighted values: at most, in partial rows (2^9 of them are added up); looked at
-constexpr float L_PART = 0x1p4f, L_FINAL = 0x1p14f, L_TINY = 0x1p-16f;      // ... where the weights' sum lets them be more, or less (values: below 2^114)
+// Sums of weighted values: at most so much in partial rows (the merge adds up some 2^9 of them), and at least so much in a row's largest, or
+// products may have been lost.  Values are below 2^114, so what the weights' sum is tells where a row can be outside.
+constexpr float O_PART = 0x1p118f, O_TINY = 0x1p-110f;
+constexpr float L_PART = 0x1p4f, L_FINAL = 0x1p14f, L_TINY = 0x1p-16f;
 constexpr float R_FAINT = 8.7e-19f;              // 2^-60: sums below it may have lost weights to fp32's range
 
 // Sizes of one build: head_dim D, at most NMAX stacked rows.

@@ -16,8 +16,8 @@
 //                  (one in about 10^4) compares x - n s, which is exact, with s / 2.
 // An element that is not finite is stored as zero and reported (PASTA_ERR_DEVICE_CHECK), as in an 8-bit pool.
 //
-// One pass: 2 bytes of bf16 in and 9/16 of a byte out per element.  What bounds it: instructions (21 per element and warp in 32768 rotated
-// tokens, half of them the rotation's and its exchange through shared memory), issued in 60 % of the cycles by three CTAs of eight
+// One pass: 2 bytes of bf16 in and 9/16 of a byte out per element.  What bounds it: instructions (20 per element and warp in 32768 rotated
+// tokens, half of them the rotation's and its exchange through shared memory), issued in 57 % of the cycles by three CTAs of eight
 // warps to an SM (two, at 122 registers: 115 us with the read-back in place of 104).  Packed fp32 arithmetic does two elements per
 // instruction (132 to 115 us with the checks gathered per lane).  32768 tokens: 69 us to store, 31 to read back (5.6 TB/s).
 #include <cmath>

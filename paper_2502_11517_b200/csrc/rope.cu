@@ -5,8 +5,8 @@
 // a time, a lane one slot of 16 elements: two 16-byte loads, eight rotations, two 16-byte stores.
 // What bounds it: for long prompts the instructions around the 64-bit rotation (a quarter of them are; conversions and exponents' bits
 // the rest) and the latency of 16 warps per SM (three CTAs in 80 registers spill: 44 to 62 us for the queries), 50 to 60 % of what
-// the bytes take; for a step the chain sine -> rotation -> store.  16384 tokens of a bf16 pool 30 us (26 for the bytes at the copy rate),
-// 1024 query tokens of 8 layers and 32 heads 35 us (20).
+// the bytes take; for a step the chain sine -> rotation -> store.  16384 tokens of a bf16 pool 30 us (20.5 for the bytes at the copy rate),
+// 1024 query tokens of 8 layers and 32 heads 35 us (20.5), in 512 CTAs on 296 places.
 #include <algorithm>
 
 #include "device_common.cuh"
