@@ -383,7 +383,8 @@ pasta_status_t pasta_step_host(pasta_pool_t *pool, int32_t n, const int32_t *req
  * owned by a framework's arena.
  *   - The array holds PASTA_NOALLOC_MAX_ROWS partial rows (about 8 MiB; every GPU that loads the library
  *     carries it until the process exits).  A step whose plan needs more rows is refused with
- *     PASTA_ERR_CAPACITY; use pasta_decode_attn for those.
+ *     PASTA_ERR_CAPACITY; use pasta_decode_attn for those.  (On a 4-bit pool such a step is cut into
+ *     fewer pieces for this call, and refused where it has too many rows uncut.)
  *   - The first call on a device looks up the array's device address (a runtime query, no allocation).
  *     Make that first call outside any stream capture.  The pool's device must be the current device.
  *     The address is kept for the life of the device's primary context: after cudaDeviceReset the library
